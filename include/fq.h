@@ -389,6 +389,66 @@ int fq_gemm_bf16(const void* X, const void* W, int M, int N, int K, void* Y, int
  * ------------------------------------------------------------------------------------------- */
 int fq_gemm_select(int variant);
 
+/* ---------------------------------------------------------------------------------------------
+ * Attention beside the quantized layer (the paper quantizes the linear layers and attention's two products,
+ * fq_bmm_i8; these calls are what a serving program runs between the QKV and the output projection).
+ *
+ * Packed arrays: Q [tokens, heads_q, head_dim], K, V [tokens, heads_kv, head_dim]; heads dense, token stride ldq / ldk / ldv
+ *   elements (views into the rows of a fused projection), a multiple of 16 bytes; heads_q a multiple of heads_kv:
+ *   query head i reads key head i / (heads_q / heads_kv).  head_dim 64, 80, 96 or 128.  Sequence b's rows are
+ *   cu[b] .. cu[b + 1] - 1 (cu int32 [batch + 1], device, ascending from 0); rows behind the last sequence are left as they were.
+ * Cache: pages of page_size (64 or 128) tokens, 8-bit codes with one scale for each page and head,
+ *   k_cache [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size] (transposed within a page:
+ *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv]; an element is code * scale.
+ *   page_table int32 [batch, table_width], device: token t of sequence b lies in page page_table[b, t / page_size], slot
+ *   t % page_size.  table_width * page_size <= 2^30.  Nothing has to be cleared before use: a page's first token starts it anew.
+ * Values on the device cannot be checked when the call is made; the kernels use them within bounds: offsets are clamped to
+ *   [0, tokens], lengths to what the page table reaches, and a page number outside [0, pages) means no page (nothing is stored
+ *   there; its keys are left out as if masked).
+ * batch in 1 .. 65535.  tokens may be 0: nothing is enqueued.  Index arrays need 4-byte alignment only.
+ *
+ * fq_kv_append — positions and cache.  Token t of sequence b's new ones has position past[b] + t.  Elements (x, y) of a pair
+ *   of the head's first rope_dim elements, (i, i + rope_dim / 2) or with interleaved != 0 (2 i, 2 i + 1), become
+ *     x' = fl32(fl32(x c) - fl32(y s)),  y' = fl32(fl32(y c) + fl32(x s)),  c, s = rope_cos / rope_sin[position, i]
+ *   (fp32 [rope_rows, rope_dim / 2]; any scaling for long contexts is in the table); the others stay.  rope_dim = 0: none.
+ *   Q_out, K_out (either may be NULL: not wanted; then Q may be NULL too) receive the rotated rows rounded to x_dtype; each may be its input itself
+ *   (same address and stride), else they must not overlap the inputs.
+ *   Codes come from the unrounded fp32 values.  Per (page, head), over the elements that this call adds, of K and V alike:
+ *     s = fl32(max|x'| / 127), 0 if that is below 2^-126; where the page holds earlier tokens, s = max(s, its scale), and
+ *     if that grows their codes become rne(fl32(code * fl32(old / s)));  code = clamp(rne(fl32(x' * fl32(1 / s))), -127, 127),
+ *     0 for s = 0.  (The codes of a page that filled up in several calls depend on where these calls began.)
+ *   Slots behind a sequence's last token keep what they held.  Tokens at positions that the table of pages or of angles does not reach are left
+ *   out: neither stored nor rotated.  max_new >= every sequence's number of new tokens (further ones are left out).
+ *   x_dtype F32 / F16 / BF16.  No two (sequence, page) places that the call writes may name the same page.
+ *
+ * fq_attn_cache — Y[i] = softmax(scale * Q[i] K^T) V over the cache: with n query tokens of sequence b and lens[b] tokens in the
+ *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
+ *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32, probabilities enter the second
+ *   product as fp16.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they,
+ *   not the lengths on the device, set the launch, so a captured call may be replayed with other lengths within them.
+ *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
+ *   Y may be Q itself (same address and stride), else it must not overlap the inputs.
+ *
+ * fq_attn_prompt — the same over packed K and V: query i of n sees keys 0 .. m - n + i of the sequence's m (causal != 0), or all
+ *   of them; a query that sees none gets 0.  Probabilities enter the second product in x_dtype.  Y as above.  Reads nothing of
+ *   a sequence's neighbours; K and V of one sequence must be finite throughout.
+ * ------------------------------------------------------------------------------------------- */
+int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim,
+                 long long ldq, long long ldk, long long ldv, const int32_t* cu_new, const int32_t* past, int batch, int max_new,
+                 const float* rope_cos, const float* rope_sin, int rope_rows, int rope_dim, int interleaved,
+                 void* Q_out, long long ldqo, void* K_out, long long ldko,
+                 int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale, int pages, int page_size,
+                 const int32_t* page_table, int table_width, void* stream);
+size_t fq_attn_cache_workspace_bytes(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv, int head_dim);
+int fq_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim, long long ldq,
+                  const int32_t* cu_q, const int32_t* lens, int batch, int max_q, int max_len,
+                  const int8_t* k_cache, const int8_t* v_cache, const float* k_scale, const float* v_scale, int pages, int page_size,
+                  const int32_t* page_table, int table_width, float scale, void* Y, long long ldy,
+                  void* workspace, size_t workspace_bytes, void* stream);
+int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int tokens_q, int tokens_k, int heads_q, int heads_kv,
+                   int head_dim, long long ldq, long long ldk, long long ldv, const int32_t* cu_q, const int32_t* cu_k, int batch, int max_q,
+                   int causal, float scale, void* Y, long long ldy, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

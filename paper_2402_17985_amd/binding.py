@@ -26,6 +26,7 @@ SYMBOLS = ["fq_last_error_string", "fq_version", "fq_flatten_plan", "fq_flatten_
            "fq_flatten_plan_xw", "fq_flatten_weights_split", "fq_flatten_quant_act_peel",
            "fq_gemm_i8_bias", "fq_gemm_i4_bias", "fq_linear_bias", "fq_linear_fused_a_i8", "fq_gemm_i4_e3m2",
            "fq_flatten_quant_act_noalloc", "fq_noalloc_scratch_bytes",
+           "fq_kv_append", "fq_attn_cache_workspace_bytes", "fq_attn_cache", "fq_attn_prompt",
            # include/fq_peak.h: measurement hooks
            "fq_peak_mfma", "fq_peak_copy", "fq_peak_gemm_ticks", "fq_peak_wall_clock_khz"]
 FQ_PEAK_I8, FQ_PEAK_BF16, FQ_PEAK_E3M2, FQ_PEAK_I8_NIBBLES = 0, 1, 2, 3
@@ -95,6 +96,15 @@ def lib() -> ctypes.CDLL:
     L.fq_linear_workspace_bytes.restype = c_size_t
     L.fq_linear_workspace_bytes.argtypes = [c_int, c_int, c_int, c_int]
     L.fq_gemm_bf16.argtypes = [vp, vp, c_int, c_int, c_int, vp, c_int, vp]
+    c_ll = ctypes.c_longlong
+    L.fq_kv_append.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, c_int, c_ll, c_ll, c_ll, vp, vp, c_int, c_int, vp, vp, c_int,
+                               c_int, c_int, vp, c_ll, vp, c_ll, vp, vp, vp, vp, c_int, c_int, vp, c_int, vp]
+    L.fq_attn_cache_workspace_bytes.restype = c_size_t
+    L.fq_attn_cache_workspace_bytes.argtypes = [c_int] * 7
+    L.fq_attn_cache.argtypes = [vp, c_int, c_int, c_int, c_int, c_int, c_ll, vp, vp, c_int, c_int, c_int, vp, vp, vp, vp, c_int, c_int, vp,
+                                c_int, c_float, vp, c_ll, vp, c_size_t, vp]
+    L.fq_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, c_ll, c_ll, c_ll, vp, vp, c_int, c_int, c_int, c_float, vp,
+                                 c_ll, vp]
     for name in SYMBOLS:
         getattr(L, name)
     _lib = L
@@ -433,3 +443,121 @@ def fq_gemm_bf16(X, W, Y, stream=None) -> None:
     if X.stride(0) != K or W.stride(0) != K:
         raise ValueError("fq_gemm_bf16 needs densely packed rows")
     _check(lib().fq_gemm_bf16(X.data_ptr(), W.data_ptr(), M, N, K, Y.data_ptr(), Y.stride(0), _stream(stream)))
+
+
+# ------------------------------------------------------------------------------------------
+# attention
+# ------------------------------------------------------------------------------------------
+def _packed(t, name, like=None):
+    """Token stride of a packed [tokens, heads, head_dim] device tensor with dense heads."""
+    if not t.is_cuda or t.dim() != 3:
+        raise ValueError(f"{name} must be a 3-D device tensor [tokens, heads, head_dim]")
+    tokens, heads, dim = t.shape
+    if tokens and ((dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim)):
+        raise ValueError(f"{name} must have dense heads: only its token stride is free")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError(f"{name} must have the shape and type {tuple(like.shape)}, {like.dtype}")
+    return t.stride(0) if tokens > 1 else heads * dim
+
+
+def _int32(t, name, shape):
+    if not t.is_cuda or t.dtype != _torch().int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 device tensor of shape {shape}")
+    return t
+
+
+def _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim):
+    """(pages, page size, table columns) of a paged cache whose tensors fit together."""
+    torch = _torch()
+    if k_cache.dim() != 4 or v_cache.dim() != 4:
+        raise ValueError("k_cache is [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size]")
+    pages, heads, size, d = k_cache.shape
+    for t, name, shape, dtype in ((k_cache, "k_cache", (pages, heads_kv, size, dim), torch.int8), (v_cache, "v_cache", (pages, heads_kv, dim, size), torch.int8),
+                                  (k_scale, "k_scale", (pages, heads_kv), torch.float32), (v_scale, "v_scale", (pages, heads_kv), torch.float32)):
+        if not t.is_cuda or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} device tensor of shape {shape}")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [batch, columns]")
+    _int32(page_table, "page_table", (batch, page_table.shape[1]))
+    return pages, size, page_table.shape[1]
+
+
+def _one_device(*tensors):
+    """The tensors are on the current device, whose stream the kernels go to."""
+    here = _torch().cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+
+
+def fq_kv_append(Q, K, V, cu_new, past, max_new: int, k_cache, v_cache, k_scale, v_scale, page_table, rope_cos=None, rope_sin=None,
+                 interleaved: bool = False, Q_out=None, K_out=None, stream=None) -> None:
+    """Rotate Q [tokens, heads_q, head_dim] into Q_out and K [tokens, heads_kv, head_dim] into K_out (either None: not wanted), and
+    store K and V at positions past[b] .. of each sequence in the paged 8-bit cache, whose codes and scales are updated in place.
+    rope_cos, rope_sin fp32 [positions, rope_dim / 2], or None: no rotation."""
+    ldk, ldv = _packed(K, "K"), _packed(V, "V", K)
+    tokens, heads_kv, dim = K.shape
+    heads_q, ldq, ldqo, ldko = heads_kv, heads_kv * dim, heads_kv * dim, heads_kv * dim
+    if Q_out is not None:
+        if Q is None:
+            raise ValueError("Q_out without Q")
+        ldq, ldqo, heads_q = _packed(Q, "Q"), _packed(Q_out, "Q_out", Q), Q.shape[1]
+        if Q.shape[0] != tokens or Q.shape[2] != dim or Q.dtype != K.dtype:
+            raise ValueError("Q must have K's tokens, head_dim and type")
+    if K_out is not None:
+        ldko = _packed(K_out, "K_out", K)
+    batch = past.numel()
+    _int32(past, "past", (batch,))
+    _int32(cu_new, "cu_new", (batch + 1,))
+    pages, size, width = _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim)
+    rows = half = 0
+    if (rope_cos is None) != (rope_sin is None):
+        raise ValueError("rope_cos and rope_sin go together")
+    if rope_cos is not None:
+        rows, half = rope_cos.shape
+        for t, name in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")):
+            if not t.is_cuda or _dtype_code(t) != FQ_F32 or t.shape != rope_cos.shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous fp32 device tensor [positions, rope_dim / 2]")
+    _one_device(Q if Q_out is not None else None, K, V, cu_new, past, k_cache, v_cache, k_scale, v_scale, page_table, rope_cos, rope_sin, Q_out, K_out)
+    _check(lib().fq_kv_append(_ptr(Q) if Q_out is not None else None, K.data_ptr(), V.data_ptr(), _dtype_code(K), tokens, heads_q, heads_kv,
+                              dim, ldq, ldk, ldv, cu_new.data_ptr(), past.data_ptr(), batch, max_new, _ptr(rope_cos), _ptr(rope_sin), rows,
+                              2 * half, int(bool(interleaved)), _ptr(Q_out), ldqo, _ptr(K_out), ldko, k_cache.data_ptr(), v_cache.data_ptr(),
+                              k_scale.data_ptr(), v_scale.data_ptr(), pages, size, page_table.data_ptr(), width, _stream(stream)))
+
+
+def fq_attn_cache_workspace_bytes(batch: int, tokens: int, max_q: int, max_len: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
+    return lib().fq_attn_cache_workspace_bytes(batch, tokens, max_q, max_len, heads_q, heads_kv, head_dim)
+
+
+def fq_attn_cache(Q, cu_q, lens, max_q: int, max_len: int, k_cache, v_cache, k_scale, v_scale, page_table, scale: float, Y, workspace,
+                  stream=None) -> None:
+    """Y = causal attention of Q [tokens, heads_q, head_dim], the last tokens of each sequence (rows cu_q[b] .. cu_q[b + 1] - 1), over the
+    lens[b] tokens that the paged 8-bit cache holds of it."""
+    ldq, ldy = _packed(Q, "Q"), _packed(Y, "Y", Q)
+    tokens, heads_q, dim = Q.shape
+    batch, heads_kv = lens.numel(), k_cache.shape[1]
+    _int32(lens, "lens", (batch,))
+    _int32(cu_q, "cu_q", (batch + 1,))
+    pages, size, width = _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim)
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    _one_device(Q, cu_q, lens, k_cache, v_cache, k_scale, v_scale, page_table, Y, workspace)
+    _check(lib().fq_attn_cache(Q.data_ptr(), _dtype_code(Q), tokens, heads_q, heads_kv, dim, ldq, cu_q.data_ptr(), lens.data_ptr(), batch, max_q,
+                               max_len, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, size,
+                               page_table.data_ptr(), width, scale, Y.data_ptr(), ldy, workspace.data_ptr(),
+                               workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def fq_attn_prompt(Q, K, V, cu_q, cu_k, max_q: int, scale: float, Y, causal: bool = True, stream=None) -> None:
+    """Y = attention of packed queries Q [tokens_q, heads_q, head_dim] over packed K, V [tokens_k, heads_kv, head_dim], sequence by
+    sequence (rows cu_q[b] .. and cu_k[b] .. belong together); causal: the last query of a sequence sees its last key."""
+    ldq, ldy, ldk, ldv = _packed(Q, "Q"), _packed(Y, "Y", Q), _packed(K, "K"), _packed(V, "V", K)
+    tokens_q, heads_q, dim = Q.shape
+    if K.shape[2] != dim or K.dtype != Q.dtype:
+        raise ValueError("Q, K and V must have the same head_dim and type")
+    batch = cu_q.numel() - 1
+    _int32(cu_q, "cu_q", (batch + 1,))
+    _int32(cu_k, "cu_k", (batch + 1,))
+    _one_device(Q, K, V, cu_q, cu_k, Y)
+    _check(lib().fq_attn_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), tokens_q, K.shape[0], heads_q, K.shape[1], dim, ldq, ldk,
+                                ldv, cu_q.data_ptr(), cu_k.data_ptr(), batch, max_q, int(bool(causal)), scale, Y.data_ptr(), ldy, _stream(stream)))

@@ -1,0 +1,89 @@
+// What the attention kernels take from device-resident lengths and page tables, and their launch rules: plain arithmetic on
+// sizes without HIP types, so that a test can compile it with the host compiler and walk it.  Lengths, offsets and page numbers
+// live on the device and cannot be checked when a call is made; every one that a kernel uses for an address passes through here.
+#pragma once
+#include <algorithm>
+#include <stddef.h>
+#include <stdint.h>
+
+#ifdef __HIPCC__
+#define FQ_BOTH __attribute__((host, device)) inline
+#else
+#define FQ_BOTH inline
+#endif
+
+namespace fq {
+
+constexpr int CACHE_STEP = 64;        // keys that a wave of the cache's attention takes at a time; pages are a multiple of it
+constexpr int MAX_PAGE = 128;
+constexpr int ATTN_DIMS[] = {64, 80, 96, 128};
+
+// Rows [first, first + count) of a packed array of `rows` rows, from two neighbouring offsets; at most `most` of them.
+struct Rows {
+    int first, count;
+};
+FQ_BOTH Rows packed_rows(int from, int to, int rows, int most)
+{
+    const int a = from < 0 ? 0 : from > rows ? rows : from;
+    const int b = to < a ? a : to > rows ? rows : to;
+    return Rows{a, b - a < most ? b - a : most};
+}
+
+// The j-th page that a sequence's new tokens touch: slots [slot0, slot1) of the sequence's page `index` take the rows from
+// `row` on, the first of them at position `pos`.  Tokens at `capacity` or beyond have no place.
+struct Fill {
+    int index, slot0, slot1, row, pos;
+};
+FQ_BOTH Fill page_fill(Rows r, int past, int j, int page, int capacity)
+{
+    const int begin = past < 0 ? 0 : past;
+    const long long end = begin + (long long)r.count < capacity ? begin + (long long)r.count : capacity;
+    const long long index = (long long)(begin / page) + j, base = index * page;
+    const long long lo = base < begin ? begin : base, hi = base + page < end ? base + page : end;
+    if (lo >= hi) return Fill{0, 0, 0, 0, 0};
+    return Fill{(int)index, (int)(lo - base), (int)(hi - base), (int)(r.first + (lo - begin)), (int)lo};
+}
+// Pages that `tokens` tokens can touch, wherever the first one lies in its page.
+inline long long pages_touched(int tokens, int page) { return ((long long)tokens + page - 2) / page + 1; }
+
+// Keys of a sequence that the cache holds and its page table reaches.
+FQ_BOTH int cached_keys(int len, int max_len, int capacity)
+{
+    const int most = max_len < capacity ? max_len : capacity;
+    return len < 0 ? 0 : len > most ? most : len;
+}
+
+// Keys that query i of n sees when the last one sees all `keys` (causal; none: 0).
+FQ_BOTH int visible_keys(int keys, int n, int i)
+{
+    const int v = keys - n + i + 1;
+    return v < 0 ? 0 : v;
+}
+
+// Keys of one share when `keys` are dealt over `splits` workgroups: whole steps for every wave, so that the last shares may be empty.
+constexpr int CACHE_WAVES = 4, CACHE_SHARE = CACHE_WAVES * CACHE_STEP;
+FQ_BOTH int share_keys(int keys, int splits)
+{
+    const long long per = (long long)CACHE_SHARE * splits;
+    const long long rounds = (keys + per - 1) / per;
+    return rounds < 1 ? CACHE_SHARE : (int)(rounds * CACHE_SHARE);
+}
+FQ_BOTH int shares_used(int keys, int share) { return (int)(((long long)keys + share - 1) / share); }
+
+// Columns (query token, head of the group) that one workgroup of the cache's attention takes, in tiles of 16.
+inline int cache_tiles(long long columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
+
+// Workgroups among which a sequence's keys are split, so that few sequences fill the device too.
+inline int cache_splits(int batch, int max_q, int max_len, int heads_q, int heads_kv)
+{
+    const long long columns = (long long)max_q * (heads_q / heads_kv), tile = 16LL * cache_tiles(columns);
+    const long long wgs = (long long)batch * heads_kv * ((columns + tile - 1) / tile);
+    const long long most = ((long long)max_len + CACHE_SHARE - 1) / CACHE_SHARE;
+    return (int)std::max(1LL, std::min({most, (1024 + wgs - 1) / wgs, 256LL}));
+}
+
+// Queries of one head that a workgroup of the prompt's attention takes, 32 a wave.
+constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;
+inline long long prompt_tiles(int max_q) { return ((long long)max_q + PROMPT_ROWS - 1) / PROMPT_ROWS; }
+
+}  // namespace fq

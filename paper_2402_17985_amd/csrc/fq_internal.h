@@ -122,4 +122,18 @@ int launch_gemm_fused_a_i8(const void* X, int ldx, int K, const int32_t* src, co
                            const void* Wq, int M, int N, int Kpad, const float* s_x, const float* s_w, void* Y,
                            int y_dtype, int ldy, const float* bias, hipStream_t stream);
 
+// ---- attention (fq_kv_append, fq_attn_cache, fq_attn_prompt; arguments as in include/fq.h) ----
+int launch_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim,
+                     long long ldq, long long ldk, long long ldv, const int32_t* cu_new, const int32_t* past, int batch, int max_new,
+                     const float* rope_cos, const float* rope_sin, int rope_rows, int rope_dim, int interleaved, void* Q_out,
+                     long long ldqo, void* K_out, long long ldko, int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale,
+                     int pages, int page_size, const int32_t* page_table, int table_width, hipStream_t stream);
+int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim, long long ldq, const int32_t* cu_q,
+                      const int32_t* lens, int batch, int max_q, int max_len, const int8_t* k_cache, const int8_t* v_cache,
+                      const float* k_scale, const float* v_scale, int pages, int page_size, const int32_t* page_table, int table_width,
+                      float scale, void* Y, long long ldy, void* workspace, int splits, hipStream_t stream);
+int launch_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int tokens_q, int tokens_k, int heads_q, int heads_kv,
+                       int head_dim, long long ldq, long long ldk, long long ldv, const int32_t* cu_q, const int32_t* cu_k, int batch, int max_q,
+                       int causal, float scale, void* Y, long long ldy, hipStream_t stream);
+
 }  // namespace fq

@@ -1,0 +1,77 @@
+"""Inputs and error bounds of the attention tests."""
+import numpy as np
+import torch
+
+from oracle import attention as A
+
+DEV = "cuda:0"
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+HALF_STEP = {"bf16": 2.0**-8, "f16": 2.0**-11, "f32": 2.0**-24}
+
+
+def offsets(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+def i32(a, dev=DEV):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(dev)
+
+
+def packed(rng, tokens, heads, dim, x, dev=DEV, pad=0, scale=1.0):
+    """A [tokens, heads, dim] view into wider rows (`pad` elements more), and its values in fp32."""
+    rows = torch.from_numpy(rng.standard_normal((tokens, heads * dim + pad)).astype(np.float32) * np.float32(scale)).to(TYPES[x]).to(dev)
+    t = rows[:, pad // 2:pad // 2 + heads * dim].unflatten(1, (heads, dim))
+    return t, t.float().cpu().numpy()
+
+
+def page_tables(rng, counts, extra=2):
+    """Page numbers for sequences of counts[b] pages, in no order, with a column to spare; unused entries are no pages."""
+    total = int(sum(counts)) + extra
+    order = rng.permutation(total)
+    table, at = np.full((len(counts), max(list(counts) + [1]) + 1), -7, np.int32), 0
+    for b, n in enumerate(counts):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, total
+
+
+def filled_cache(rng, pages, heads, page, dim):
+    k, v = (rng.integers(-128, 128, s, dtype=np.int8) for s in ((pages, heads, page, dim), (pages, heads, dim, page)))
+    ks, vs = (np.exp(rng.standard_normal((pages, heads)) * 0.7).astype(np.float32) / np.float32(60.0) for _ in range(2))
+    return k, v, ks, vs
+
+
+def to_dev(*arrays):
+    return [torch.from_numpy(a.copy()).to(DEV) for a in arrays]
+
+
+def attention_bound(exact, spread, scores, keys, dim, vmax, x, p_half):
+    """How far a result may be from `exact`: spread = sum p |v|, scores = a bound of scale * sum |q| |k|.
+    The output's rounding; a probability's rounding (p_half); the scores' 32-bit sums, which change a probability and the sum that
+    divides it; the second product's 32-bit sum; and what fp16 probabilities lose below their smallest step (2^-25 each)."""
+    fp32 = 2.0**-24
+    in_p = p_half + 2 * (dim + 16) * fp32 * scores + (keys + 16) * fp32
+    off = in_p * spread + (keys * 2.0**-25 * vmax if p_half == HALF_STEP["f16"] else 0.0)
+    return HALF_STEP[x] * (np.abs(exact) + off) + off + 2.0**-24 * (x == "f16") + 1e-30
+
+
+def check(got, exact, bound, where):
+    got = got.float().cpu().numpy().astype(np.float64)
+    assert np.isfinite(got).all(), f"{where}: not finite"
+    off = np.abs(got - exact) / bound
+    worst = np.unravel_index(np.argmax(off), off.shape)
+    assert off.max() <= 1.0, f"{where}: {off.max():.2f} times the bound at {worst}: {got[worst]} for {exact[worst]}"
+
+
+def prompt_case(q, k, v, cu_q, cu_k, scale, causal, x):
+    exact, spread = A.prompt(q, k, v, cu_q, cu_k, scale, causal), A.prompt(q, k, np.abs(v), cu_q, cu_k, scale, causal)
+    g = q.shape[1] // k.shape[1]
+    scores = scale * np.abs(q).max() * np.abs(k).sum(-1).max() if len(k) else 0.0
+    assert g >= 1
+    return exact, attention_bound(exact, spread, scores, int(np.diff(cu_k).max()), q.shape[2], np.abs(v).max() if len(v) else 0.0, x, HALF_STEP[x])
+
+
+def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
+    exact, spread = A.cache(q, cu_q, lens, table, kc, vc, ks, vs, scale), A.cache(q, cu_q, lens, table, kc, np.abs(vc.astype(np.int16)), ks, vs, scale)
+    scores = scale * np.abs(q).max() * 128 * q.shape[2] * ks.max()
+    return exact, attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])

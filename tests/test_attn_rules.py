@@ -1,0 +1,133 @@
+"""What the attention kernels make of device-resident offsets, lengths and page tables (csrc/fq_attn_rules.h), compiled with the host
+compiler and walked on the CPU: every address they form comes from these."""
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2402_17985_amd", "csrc")
+LO, HI = -(2**31), 2**31 - 1
+
+DRIVER = """
+#include "fq_attn_rules.h"
+using namespace fq;
+extern "C" void rows(int from, int to, int rows, int most, int* out)
+{
+    const Rows r = packed_rows(from, to, rows, most);
+    out[0] = r.first; out[1] = r.count;
+}
+extern "C" void fill(int first, int count, int past, int j, int page, int capacity, int* out)
+{
+    const Fill f = page_fill(Rows{first, count}, past, j, page, capacity);
+    out[0] = f.index; out[1] = f.slot0; out[2] = f.slot1; out[3] = f.row; out[4] = f.pos;
+}
+extern "C" long long touched(int tokens, int page) { return pages_touched(tokens, page); }
+extern "C" int keys(int len, int max_len, int capacity) { return cached_keys(len, max_len, capacity); }
+extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i); }
+extern "C" int share(int keys, int splits) { return share_keys(keys, splits); }
+extern "C" int used(int keys, int share) { return shares_used(keys, share); }
+extern "C" int splits(int batch, int max_q, int max_len, int heads_q, int heads_kv) { return cache_splits(batch, max_q, max_len, heads_q, heads_kv); }
+extern "C" int tiles(long long columns) { return cache_tiles(columns); }
+"""
+
+
+@pytest.fixture(scope="module")
+def rules(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("needs g++")
+    d = tmp_path_factory.mktemp("attn_rules")
+    src, so = str(d / "rules.cpp"), str(d / "rules.so")
+    with open(src, "w") as f:
+        f.write(DRIVER)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-static-libubsan",
+                    "-shared", "-fPIC", "-I", CSRC, "-o", so, src], check=True)
+    lib = ctypes.CDLL(so)
+    lib.touched.restype = ctypes.c_longlong
+    return lib
+
+
+@pytest.mark.parametrize("total", [0, 1, 100, HI])
+def test_rows_stay_within_the_array(rules, total):
+    out = (ctypes.c_int * 2)()
+    for a in (LO, -1, 0, 1, 50, 100, 101, HI):
+        for b in (LO, -1, 0, 1, 50, 100, 101, HI):
+            for most in (1, 7, HI):
+                rules.rows(a, b, total, most, out)
+                first, count = out
+                assert 0 <= first <= total and 0 <= count <= min(most, total - first)
+                if 0 <= a <= b <= total and b - a <= most:
+                    assert (first, count) == (a, b - a)
+
+
+@pytest.mark.parametrize("page", [64, 128])
+def test_page_fills_cover_the_new_tokens_once_and_stay_within_a_page(rules, page):
+    out = (ctypes.c_int * 5)()
+    for width in (1, 3, 9):
+        for reach in (width * page, width * page - 37):
+            for past in (0, 1, page - 1, page, 2 * page + 3, 5 * page - 1):
+                for n in (0, 1, 2, page - 1, page, page + 1, 3 * page + 5):
+                    seen = {}
+                    for j in range(rules.touched(max(n, 1), page)):
+                        rules.fill(1000, n, past, j, page, reach, out)
+                        index, s0, s1, row, pos = out
+                        if s1 <= s0:
+                            continue
+                        assert 0 <= index < width and 0 <= s0 < s1 <= page and pos == index * page + s0 and row == 1000 + pos - past
+                        for s in range(s0, s1):
+                            assert index * page + s not in seen
+                            seen[index * page + s] = row + s - s0
+                    assert seen == {p: 1000 + p - past for p in range(past, min(past + n, reach))}
+
+
+@pytest.mark.parametrize("past", [LO, -1, 0, 2**30 - 1, 2**30, HI])
+@pytest.mark.parametrize("capacity", [64, 2**30])
+def test_page_fills_of_wild_lengths_stay_within_the_table(rules, past, capacity):
+    out = (ctypes.c_int * 5)()
+    for n in (0, 1, 200, HI):
+        for j in (0, 1, 5, 2**25, HI // 64):
+            rules.fill(0, n, past, j, 64, capacity, out)
+            index, s0, s1, row, pos = out
+            if s1 > s0:
+                assert 0 <= index < capacity // 64 and 0 <= s0 < s1 <= 64 and 0 <= row and row + s1 - s0 <= n and pos + s1 - s0 <= capacity
+
+
+@pytest.mark.parametrize("n,page,most", [(1, 64, 1), (2, 64, 2), (64, 64, 2), (65, 64, 2), (66, 64, 3), (HI, 64, 2**25 + 1)])
+def test_pages_touched(rules, n, page, most):
+    assert rules.touched(n, page) == most
+
+
+def test_keys_and_visible_keys(rules):
+    for length in (LO, -1, 0, 5, 1000, HI):
+        for max_len in (1, 100, HI):
+            for capacity in (64, 2**30):
+                assert rules.keys(length, max_len, capacity) == max(0, min(length, max_len, capacity))
+    for keys in (0, 1, 5, 2**30):
+        for n in (1, 3, 7, 2**30):
+            for i in {0, 1, n - 1}:
+                assert rules.visible(keys, n, i) == max(0, keys - n + i + 1)
+
+
+def test_shares_cover_all_keys_in_whole_steps(rules):
+    for splits in (1, 2, 3, 7, 64, 256):
+        for keys in (0, 1, 255, 256, 257, 1000, 4096, 131072, 2**30 - 1, 2**30):
+            share = rules.share(keys, splits)
+            assert share >= 256 and share % 256 == 0 and share * splits >= keys
+            used = rules.used(keys, share)
+            assert used <= splits and (used - 1) * share < keys <= used * share or (keys == 0 and used == 0)
+
+
+def test_splits_are_bounded_and_one_where_there_is_work_enough(rules):
+    for batch in (1, 4, 64, 65535):
+        for max_q in (1, 5, 512, 65472):
+            for max_len in (1, 256, 257, 8192, 2**30):
+                for hq, hkv in ((1, 1), (64, 8), (64, 64), (16384, 1)):
+                    if max_q * hq >= 2**30:
+                        continue
+                    s = rules.splits(batch, max_q, max_len, hq, hkv)
+                    columns = max_q * (hq // hkv)
+                    wgs = batch * hkv * -(-columns // (16 * rules.tiles(ctypes.c_longlong(columns))))
+                    assert 1 <= s <= 256 and (s - 1) * 256 < max_len
+                    assert s == 1 or (wgs < 1024 and max_q <= 65535)
