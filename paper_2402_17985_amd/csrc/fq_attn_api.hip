@@ -157,6 +157,7 @@ int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int
     if (!rc) rc = check_indices("cu_q", cu_q);
     if (!rc) rc = check_indices("cu_k", cu_k);
     if (rc) return rc;
+    if (ldk > (1 << 24) || ldv > (1 << 24)) return fail(FQ_ERR_RANGE, "token strides of %lld and %lld elements for K and V: at most 2^24", ldk, ldv);
     const long long places = (long long)batch * heads_q * prompt_tiles(max_q);
     if (places >= (1LL << 31) || !launch_holds(places, PROMPT_THREADS))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);

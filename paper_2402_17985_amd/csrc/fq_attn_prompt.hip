@@ -8,6 +8,8 @@
 //                 reduction is free as long as the values follow, and their transposed reads from LDS take four consecutive
 //                 keys of a dimension, as a lane holds them.
 // P is rounded to the input's type, the row sums are taken before that in 32 bits.
+#include <type_traits>
+
 #include "fq_attn_common.h"
 
 namespace fq {
@@ -39,15 +41,11 @@ template <> struct Mma<FQ_F16> {
     static __device__ __forceinline__ v16f mul(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// Rows of LDS: keys an odd number of 16-byte pieces apart, so that the rows that lanes read together lie on different banks;
-// values 8 or 24 banks (of 32) apart, as four of them are read together, 32 bytes each.
-constexpr int key_row(int D) { return 2 * D + 16; }
-constexpr int value_row(int D)
-{
-    int words = D / 2;
-    while (words % 32 != 8 && words % 32 != 24) words += 4;
-    return 4 * words;
-}
+// A tile in LDS is rows of D elements without gaps, as the direct copies from global memory fill it, with the 16-byte pieces of a
+// row rotated: piece c of row r lies at place (c + turn(r)) mod (D / 8), so that rows that are read together lie on different banks
+// (64 of them, 256 bytes).  Keys are read 16 rows at a time, the same piece of each; values 4 rows at a time, 4 pieces of each.
+constexpr int key_turn(int C, int r) { return C == 16 ? r % 16 : C == 12 ? r % 16 / 4 : C == 10 ? r % 16 / 8 : r % 16 / 2; }
+constexpr int value_turn(int C, int r) { return C == 16 ? r % 4 * 4 : C == 8 ? r % 4 / 2 * 4 : 0; }
 
 // Four 2-byte elements of a column out of row-major LDS: of 16 neighbouring lanes, lanes 4 r .. 4 r + 3 point at 16 consecutive
 // elements of row r, and lane i receives element i of the four rows.
@@ -59,26 +57,64 @@ __device__ __forceinline__ v2u read_transposed(uint32_t lds_address)
     return __builtin_bit_cast(v2u, r);
 }
 
+// 64 lanes times 16 bytes from global memory straight to LDS bytes [lds_base, + 1024) (lds_base is wave-uniform).
+__device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t lane_offset, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(uniform_base), "v"(lane_offset), "s"(lds_base) : "memory");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+// Of the two lanes that share a query, lane and lane + 32.
+__device__ __forceinline__ float over_halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float over_halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A workgroup's sequence.  Of at most 64 it is the one that is nth by its number of keys, longest first: long ones begun last would run on
+// alone.  All offsets are loaded at once, one sequence a lane, so that the order costs no further trip to memory.
+struct PromptSequence {
+    Rows q, k;
+};
+__device__ __forceinline__ PromptSequence nth_sequence(const PromptAttn& a, int nth)
+{
+    const bool sorted = a.batch <= 64;
+    const int lane = threadIdx.x % 64, j = sorted ? min(lane, a.batch - 1) : nth;
+    const Rows k = packed_rows(a.cu_k[j], a.cu_k[j + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[j], a.cu_q[j + 1], a.tokens_q, a.max_q);
+    int from = 0;      // any lane
+    if (sorted && a.batch > 1) {
+        int longer = 0;
+        for (int i = 0; i < a.batch; ++i) {
+            const int other = __builtin_amdgcn_readlane(k.count, i);
+            longer += other > k.count || (other == k.count && i < lane);
+        }
+        from = __builtin_ctzll(__ballot(lane < a.batch && longer == nth));
+    }
+    return {{__builtin_amdgcn_readlane(q.first, from), __builtin_amdgcn_readlane(q.count, from)},
+            {__builtin_amdgcn_readlane(k.first, from), __builtin_amdgcn_readlane(k.count, from)}};
+}
+
 template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, 2) void attn_prompt_kernel(const PromptAttn a)
 {
     typedef Mma<DT> M;
     typedef typename M::T T;
     typedef typename M::v8 v8;
-    constexpr int KS = D / 16, VT = (D + 31) / 32, C = D / 8, KROW = key_row(D), VROW = value_row(D);
-    constexpr int KBYTES = PROMPT_KEYS * KROW, VBYTES = PROMPT_KEYS * VROW, STAGE = KBYTES + VBYTES;
-    constexpr int PIECES = (PROMPT_KEYS * C + PROMPT_THREADS - 1) / PROMPT_THREADS;   // 16-byte pieces of each operand's tile per thread
-    constexpr bool EVEN = PROMPT_KEYS * C % PROMPT_THREADS == 0;
-    // reads of the last 32 dimensions reach beyond a row of 80: within the tile, or the 64 bytes behind the last
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * STAGE + 64];
+    constexpr int KS = D / 16, VT = (D + 31) / 32, C = D / 8, ROW = 2 * D, TILE = PROMPT_KEYS * ROW;
+    constexpr int COPIES = (C + PROMPT_WAVES - 1) / PROMPT_WAVES;   // wave-wide copies per wave, operand and tile
+    // [keys, two stages][values, two stages]; reads of the last 32 dimensions reach behind a row of 80
+    __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE + 64];
 
-    // workgroups of one sequence and key head on one XCD, the longest rows first
-    const unsigned total = gridDim.x, id = blockIdx.x, quot = total >> 3, rem = total & 7, xcd = id & 7, at_xcd = id >> 3;
-    const unsigned logical = xcd < rem ? xcd * (quot + 1) + at_xcd : rem * (quot + 1) + (xcd - rem) * quot + at_xcd;
-    const unsigned per_pair = (unsigned)a.tiles * a.group, pair = logical / per_pair, item = logical - pair * per_pair;
-    const int tile = a.tiles - 1 - (int)(item / a.group), b = pair / a.heads_kv, hk = pair - b * a.heads_kv;
-    const int head = hk * a.group + item % a.group;
+    const PromptPlace at_place = prompt_place(blockIdx.x, (unsigned)a.tiles * a.group, (unsigned)a.batch * a.heads_kv);
+    const int tile = a.tiles - 1 - (int)(at_place.item / a.group), nth = at_place.pair / a.heads_kv, hk = at_place.pair - nth * a.heads_kv;
+    const int head = hk * a.group + at_place.item % a.group;
 
-    const Rows rq = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens_q, a.max_q), rk = packed_rows(a.cu_k[b], a.cu_k[b + 1], a.tokens_k, a.tokens_k);
+    const PromptSequence sequence = nth_sequence(a, nth);
+    const Rows rq = sequence.q, rk = sequence.k;
     const int q0 = tile * PROMPT_ROWS;
     if (q0 >= rq.count) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
@@ -86,116 +122,196 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, 2) void at
     const auto visible = [&](int i) { return a.causal ? visible_keys(keys, rq.count, i) : keys; };
     const int mine = visible(min(row, rq.count - 1)), least = visible(min(q0 + 32 * wave, rq.count - 1));
     const int wave_keys = q0 + 32 * wave >= rq.count ? 0 : visible(min(q0 + 32 * wave + 31, rq.count - 1)), most = visible(min(q0 + PROMPT_ROWS, rq.count) - 1);
+    const int tiles = (most + PROMPT_KEYS - 1) / PROMPT_KEYS;
 
+    // copies into LDS: each lane's places in a tile, and the piece of a row that belongs there (where the waves outnumber what is
+    // left, several copy the same)
+    const T *kp = static_cast<const T*>(a.K) + (size_t)rk.first * a.ldk + (size_t)hk * D, *vp = static_cast<const T*>(a.V) + (size_t)rk.first * a.ldv + (size_t)hk * D;
+    const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    uint32_t from_at[2][COPIES];
+    const auto set_offsets = [&](int values, int i) {      // of tile i; for rows behind the last key that one
+        const int last = min(keys - i * PROMPT_KEYS, PROMPT_KEYS) - 1;
+#pragma unroll
+        for (int p = 0; p < COPIES; ++p) {
+            const int at = 64 * min(wave + PROMPT_WAVES * p, C - 1) + lane, r = at / C, turned = at - r * C - (values ? value_turn(C, r) : key_turn(C, r));
+            from_at[values][p] = (uint32_t)min(r, last) * (uint32_t)(2 * (values ? a.ldv : a.ldk)) + 16 * (turned < 0 ? turned + C : turned);
+        }
+    };
+    const auto copy = [&](int values, int i) {
+        if ((i + 1) * PROMPT_KEYS > keys) set_offsets(values, i);      // the last tile
+        const T* from = (values ? vp : kp) + (size_t)i * PROMPT_KEYS * (values ? a.ldv : a.ldk);
+#pragma unroll
+        for (int p = 0; p < COPIES; ++p)
+            copy_to_lds(from, from_at[values][p], base + (2 * values + i % 2) * TILE + 1024 * min(wave + PROMPT_WAVES * p, C - 1));
+    };
+
+    if (tiles > 0) {
+        set_offsets(0, 0);
+        copy(0, 0);
+    }
     const T* qp = static_cast<const T*>(a.Q) + (rq.first + (size_t)min(row, rq.count - 1)) * a.ldq + (size_t)head * D + 8 * half;
     v8 q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const v8*>(qp + 16 * s);
 
-    // pieces of the tiles that this thread carries
-    const T *kp = static_cast<const T*>(a.K) + (size_t)rk.first * a.ldk + (size_t)hk * D, *vp = static_cast<const T*>(a.V) + (size_t)rk.first * a.ldv + (size_t)hk * D;
-    v4u kreg[PIECES], vreg[PIECES];
-    const auto fetch = [&](int k0) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int i = p * PROMPT_THREADS + tid, r = i / C, c = i - r * C, key = min(k0 + r, keys - 1);   // rows behind the last: it again
-            if (!EVEN && r >= PROMPT_KEYS) continue;
-            kreg[p] = *reinterpret_cast<const v4u*>(kp + (size_t)key * a.ldk + 8 * c);
-            vreg[p] = *reinterpret_cast<const v4u*>(vp + (size_t)key * a.ldv + 8 * c);
-        }
-    };
-    const auto put = [&](int stage) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int i = p * PROMPT_THREADS + tid, r = i / C, c = i - r * C;
-            if (!EVEN && r >= PROMPT_KEYS) continue;
-            *reinterpret_cast<v4u*>(lds + stage * STAGE + r * KROW + 16 * c) = kreg[p];
-            *reinterpret_cast<v4u*>(lds + stage * STAGE + KBYTES + r * VROW + 16 * c) = vreg[p];
-        }
-    };
+    if (tiles > 0) {
+        set_offsets(1, 0);
+        copy(1, 0);
+        if (tiles > 1) copy(0, 1);
+    }
 
-    v16f o[VT];
+    v16f o[VT], s[2];
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.0f;
     float top = -INFINITY, sum = 0.0f;      // of the unscaled scores; the sum over this lane's keys only
+    v8 p[4];                                // 16 keys each
 
-    const uint32_t key_at = col * KROW + 16 * half;
-    const uint32_t value_at = KBYTES + (4 * half + lane % 16 / 4) * VROW + 32 * (lane / 16 % 2) + 8 * (lane % 4);
-    const uint32_t base_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
-    if (most > 0) {
-        fetch(0);
-        put(0);
+    uint32_t key_at[KS], value_at[VT];
+#pragma unroll
+    for (int e = 0; e < KS; ++e) key_at[e] = col * ROW + (2 * e + half + key_turn(C, col)) % C * 16;
+    const int vr = lane % 16 / 4;
+#pragma unroll
+    for (int t = 0; t < VT; ++t) {
+        const int piece = 4 * t + 2 * (lane / 16 % 2) + lane % 4 / 2;
+        value_at[t] = base + 2 * TILE + (4 * half + vr) * ROW + (piece < C ? (piece + value_turn(C, vr)) % C : piece) * 16 + 8 * (lane % 2);
     }
-    for (int k0 = 0, stage = 0; k0 < most; k0 += PROMPT_KEYS, stage ^= 1) {
-        const bool more = k0 + PROMPT_KEYS < most;
-        if (more) fetch(k0 + PROMPT_KEYS);
-        __syncthreads();
-        if (k0 < wave_keys) {
-            const uint8_t* st = lds + stage * STAGE;
-            v16f s[2];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[t][i] = 0.0f;
-#pragma unroll
-                for (int e = 0; e < KS; ++e) s[t] = M::mul(*reinterpret_cast<const v8*>(st + key_at + 32 * t * KROW + 32 * e), q[e], s[t]);
+
+    // The matrix work of a step: O^T += V^T P of tile i (PV), then S^T of tile i + 1 (QK).  Every product's first operand comes from LDS
+    // AHEAD - 1 products early; the order is kept as written.  (Left to the compiler, each pair of transposed reads is awaited before the
+    // next: 5.9e8 busy CU cycles for a causal prompt of 8192 tokens and 64 heads of 128, so 4.5e8.)
+    const auto products = [&](auto with_pv, auto with_qk) {
+        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 5;
+        v8 ring[AHEAD];
+        const auto fetch = [&](int n) {
+            if (n < PV) {
+                const uint32_t v = value_at[n % VT] + 16 * (n / VT) * ROW;
+                const v2u lo = read_transposed(v), hi = read_transposed(v + 8 * ROW);
+                ring[n % AHEAD] = __builtin_bit_cast(v8, (v4u{lo[0], lo[1], hi[0], hi[1]}));
+            } else {
+                ring[n % AHEAD] = *reinterpret_cast<const v8*>(lds + key_at[(n - PV) / 2] + 32 * ((n - PV) % 2) * ROW);
             }
-            // register i of tile t: key 32 t + 8 (i / 4) + 4 half + i % 4
-            if (k0 + PROMPT_KEYS > least) {
+        };
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+        for (int n = 0; n < AHEAD - 1; ++n) fetch(n);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (k0 + 32 * t + 8 * (i / 4) + 4 * half + i % 4 >= mine) s[t][i] = -INFINITY;
+        for (int n = 0; n < N; ++n) {
+            if (n + AHEAD - 1 < N) fetch(n + AHEAD - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n < PV) {
+                o[n % VT] = M::mul(ring[n % AHEAD], p[n / VT], o[n % VT]);
+            } else {
+                const int e = (n - PV) / 2, t = (n - PV) % 2;
+                if (e == 0)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[t][k] = 0.0f;
+                s[t] = M::mul(ring[n % AHEAD], q[e], s[t]);
             }
-            float m = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-            for (int i = 1; i < 16; ++i) m = fmaxf(m, fmaxf(s[0][i], s[1][i]));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            if (__ballot((m - top) * a.factor > SLACK || top == -INFINITY)) {
-                const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - now) * a.factor);
-                top = now;
-                sum *= keep;
-#pragma unroll
-                for (int t = 0; t < VT; ++t) o[t] *= keep;
-            }
-            const float base = top == -INFINITY ? 0.0f : top * a.factor;
-            v8 p[4];      // 16 keys each
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    // its probabilities
+    const auto softmax = [&](int i) {
+        const int k0 = i * PROMPT_KEYS;
+        // register e of tile t: key 32 t + 8 (e / 4) + 4 half + e % 4
+        if (k0 + PROMPT_KEYS > least) {
+            asm volatile("");      // a branch: the comparisons are not worth making where they change nothing
+            const int left = mine - k0 - 4 * half;
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.factor, -base));
-                    sum += e;
-                    p[2 * t + i / 8][i % 8] = (T)e;
-                }
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int t = 0; t < VT; ++t) {
-                    const uint32_t v = base_at + stage * STAGE + value_at + 16 * c * VROW + 64 * t;
-                    const v2u lo = read_transposed(v), hi = read_transposed(v + 8 * VROW);
-                    o[t] = M::mul(__builtin_bit_cast(v8, (v4u{lo[0], lo[1], hi[0], hi[1]})), p[c], o[t]);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (32 * t + 8 * (e / 4) + e % 4 >= left) s[t][e] = -INFINITY;
         }
-        if (more) put(stage ^ 1);
+        float m = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) m = fmaxf(m, fmaxf(s[0][e], s[1][e]));
+        m = over_halves_max(m);
+        if (__ballot(top == -INFINITY || (m - top) * a.factor > SLACK)) {
+            const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - now) * a.factor);
+            top = now;
+            sum *= keep;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) o[t] *= keep;
+        }
+        const float off = top == -INFINITY ? 0.0f : top * a.factor;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.factor, -off));
+                sum += w;
+                p[2 * t + e / 8][e % 8] = (T)w;
+            }
+    };
+    // Step i: copies of the next tiles, PV of tile i, QK and softmax of tile i + 1.  A stage's keys are copied over when QK has read them,
+    // a step before its values.  While one workgroup's wave on a SIMD is at the softmax the other's uses the matrix pipe; the priority of the
+    // products keeps the two apart (1088 -> 1075 us for the prompt above).
+    if (tiles > 0) {
+        wait_copies();
+        __syncthreads();
+        const int own = (wave_keys + PROMPT_KEYS - 1) / PROMPT_KEYS;      // tiles that this wave's queries see
+        if (own > 0) {
+            products(no, yes);
+            softmax(0);
+        }
+        __syncthreads();
+        const auto begin_step = [&](int i) {
+            if (i + 1 < tiles) copy(1, i + 1);
+            if (i + 2 < tiles) copy(0, i + 2);
+        };
+        const auto end_step = [&] {
+            wait_copies();
+            __syncthreads();
+        };
+        int i = 0, other = TILE;      // from one stage to the other
+#pragma unroll
+        for (int e = 0; e < KS; ++e) key_at[e] += TILE;
+        for (; i + 1 < own; ++i) {
+            begin_step(i);
+            __builtin_amdgcn_s_setprio(1);
+            products(yes, yes);
+            __builtin_amdgcn_s_setprio(0);
+            softmax(i + 1);
+#pragma unroll
+            for (int e = 0; e < KS; ++e) key_at[e] -= other;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) value_at[t] += other;
+            other = -other;
+            end_step();
+        }
+        if (own > 0) {
+            begin_step(i);
+            products(yes, no);
+            end_step();
+            ++i;
+        }
+        for (; i < tiles; ++i) {
+            begin_step(i);
+            end_step();
+        }
     }
 
-    sum += __shfl_xor(sum, 32);
+    // a lane holds dimensions 8 j + 4 half + 0..3 of its query: the two halves trade every other four for 16-byte stores
+    sum = over_halves_sum(sum);
     const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
-    if (row >= rq.count) return;
-    T* yp = static_cast<T*>(a.Y) + (rq.first + (size_t)row) * a.ldy + (size_t)head * D + 4 * half;
+    T* yp = static_cast<T*>(a.Y) + (rq.first + (size_t)row) * a.ldy + (size_t)head * D + 8 * half;
 #pragma unroll
     for (int t = 0; t < VT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; i += 2) {
             if (32 * t + 8 * i >= D) continue;
-            typename M::v4 y;
+            typename M::v4 y[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (T)(o[t][4 * i + e] * inv);
-            *reinterpret_cast<typename M::v4*>(yp + 32 * t + 8 * i) = y;
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[j][e] = (T)(o[t][4 * (i + j) + e] * inv);
+            const v2u u0 = __builtin_bit_cast(v2u, y[0]), u1 = __builtin_bit_cast(v2u, y[1]);
+            const auto lo = __builtin_amdgcn_permlane32_swap(u0[0], u1[0], false, false), hi = __builtin_amdgcn_permlane32_swap(u0[1], u1[1], false, false);
+            if (row < rq.count) *reinterpret_cast<v4u*>(yp + 32 * t + 8 * i) = v4u{lo[0], hi[0], lo[1], hi[1]};
         }
 }
 

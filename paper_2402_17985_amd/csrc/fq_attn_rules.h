@@ -86,4 +86,19 @@ inline int cache_splits(int batch, int max_q, int max_len, int heads_q, int head
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;
 inline long long prompt_tiles(int max_q) { return ((long long)max_q + PROMPT_ROWS - 1) / PROMPT_ROWS; }
 
+// Workgroup -> (sequence, key head) pair and one of its `items` (query tiles of the group's heads).  Workgroups are dealt round-robin to
+// the 8 XCDs: a pair stays on one of them, whose L2 then holds its keys and values, and the pairs go round the XCDs too, as
+// neighbouring ones (heads of one sequence) are equally long.  The last few pairs are split among all.
+struct PromptPlace {
+    unsigned pair, item;
+};
+FQ_BOTH PromptPlace prompt_place(unsigned id, unsigned items, unsigned pairs)
+{
+    const unsigned whole = pairs / 8 * 8, at = id / 8, xcd = id % 8;
+    if (id < whole * items) return PromptPlace{at / items * 8 + xcd, at % items};
+    const unsigned rest = (pairs - whole) * items, each = rest / 8, more = rest % 8, i = (id - whole * items) / 8;
+    const unsigned logical = xcd < more ? xcd * (each + 1) + i : more * (each + 1) + (xcd - more) * each + i;
+    return PromptPlace{whole + logical / items, logical % items};
+}
+
 }  // namespace fq

@@ -30,6 +30,11 @@ extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i)
 extern "C" int share(int keys, int splits) { return share_keys(keys, splits); }
 extern "C" int used(int keys, int share) { return shares_used(keys, share); }
 extern "C" int splits(int batch, int max_q, int max_len, int heads_q, int heads_kv) { return cache_splits(batch, max_q, max_len, heads_q, heads_kv); }
+extern "C" void place(unsigned id, unsigned items, unsigned pairs, unsigned* out)
+{
+    const PromptPlace p = prompt_place(id, items, pairs);
+    out[0] = p.pair; out[1] = p.item;
+}
 extern "C" int tiles(long long columns) { return cache_tiles(columns); }
 """
 
@@ -131,3 +136,24 @@ def test_splits_are_bounded_and_one_where_there_is_work_enough(rules):
                     wgs = batch * hkv * -(-columns // (16 * rules.tiles(ctypes.c_longlong(columns))))
                     assert 1 <= s <= 256 and (s - 1) * 256 < max_len
                     assert s == 1 or (wgs < 1024 and max_q <= 65535)
+
+
+@pytest.mark.parametrize("items,pairs", [(1, 1), (1, 7), (3, 8), (5, 9), (16, 23), (2, 64), (7, 1), (64, 3)])
+def test_prompt_places_are_each_taken_once_and_pairs_stay_on_an_xcd(rules, items, pairs):
+    out = (ctypes.c_uint * 2)()
+    seen, xcds = set(), {}
+    for i in range(items * pairs):
+        rules.place(i, items, pairs, out)
+        assert out[0] < pairs and out[1] < items
+        seen.add((out[0], out[1]))
+        xcds.setdefault(out[0], set()).add(i % 8)
+    assert len(seen) == items * pairs
+    assert all(len(xcds[p]) == 1 for p in range(pairs // 8 * 8))
+
+
+def test_prompt_places_of_a_launch_of_2_to_the_31_workgroups(rules):
+    out = (ctypes.c_uint * 2)()
+    for items, pairs in ((2**15, 65535), (2**31 - 1, 1), (1, 2**31 - 1), (2**24, 127)):
+        for i in (0, 7, items * pairs // 2, items * pairs - 1):
+            rules.place(i, items, pairs, out)
+            assert out[0] < pairs and out[1] < items
