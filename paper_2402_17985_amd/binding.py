@@ -116,9 +116,15 @@ def _check(rc: int):
         raise FqError(rc, lib().fq_last_error_string().decode())
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 _codes = None
@@ -448,46 +454,52 @@ def fq_gemm_bf16(X, W, Y, stream=None) -> None:
 # ------------------------------------------------------------------------------------------
 # attention
 # ------------------------------------------------------------------------------------------
-def _packed(t, name, like=None):
-    """Token stride of a packed [tokens, heads, head_dim] device tensor with dense heads."""
-    if not t.is_cuda or t.dim() != 3:
-        raise ValueError(f"{name} must be a 3-D device tensor [tokens, heads, head_dim]")
-    tokens, heads, dim = t.shape
-    if tokens and ((dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim)):
+# The checks of these calls read each tensor's shape, strides and type once: of a small call's 14 us they were 8.
+def _here() -> int:
+    """The current device, whose stream the kernels go to."""
+    global _get_device
+    if _get_device is None:
+        torch = _torch()
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _get_device()
+
+
+_get_device = None
+
+
+def _packed(t, name, here, shape=None, dtype=None):
+    """(shape, token stride) of a packed [tokens, heads, head_dim] tensor with dense heads on device `here`."""
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}: it must be on the current device, cuda:{here}")
+    got, strides = t.shape, t.stride()
+    if len(got) != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
+    tokens, heads, dim = got
+    if shape is not None and (got != shape or t.dtype != dtype):
+        raise ValueError(f"{name} must have the shape and type {tuple(shape)}, {dtype}")
+    if tokens and ((dim > 1 and strides[2] != 1) or (heads > 1 and strides[1] != dim)):
         raise ValueError(f"{name} must have dense heads: only its token stride is free")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise ValueError(f"{name} must have the shape and type {tuple(like.shape)}, {like.dtype}")
-    return t.stride(0) if tokens > 1 else heads * dim
+    return got, strides[0] if tokens > 1 else heads * dim
 
 
-def _int32(t, name, shape):
-    if not t.is_cuda or t.dtype != _torch().int32 or tuple(t.shape) != shape or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 device tensor of shape {shape}")
-    return t
+def _array(t, name, here, dtype, shape):
+    """Address of a contiguous tensor of that type and shape on device `here`."""
+    if t.dtype != dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{here}; it is {t.dtype}, "
+                         f"{tuple(t.shape)}, on {t.device}")
+    return t.data_ptr()
 
 
-def _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim):
-    """(pages, page size, table columns) of a paged cache whose tensors fit together."""
+def _cache(k_cache, v_cache, k_scale, v_scale, page_table, batch, dim, here):
+    """(heads_kv, addresses, pages, page size, address of the table, its columns) of a paged cache whose tensors fit together."""
     torch = _torch()
-    if k_cache.dim() != 4 or v_cache.dim() != 4:
-        raise ValueError("k_cache is [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size]")
-    pages, heads, size, d = k_cache.shape
-    for t, name, shape, dtype in ((k_cache, "k_cache", (pages, heads_kv, size, dim), torch.int8), (v_cache, "v_cache", (pages, heads_kv, dim, size), torch.int8),
-                                  (k_scale, "k_scale", (pages, heads_kv), torch.float32), (v_scale, "v_scale", (pages, heads_kv), torch.float32)):
-        if not t.is_cuda or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous {dtype} device tensor of shape {shape}")
-    if page_table.dim() != 2:
-        raise ValueError("page_table must be [batch, columns]")
-    _int32(page_table, "page_table", (batch, page_table.shape[1]))
-    return pages, size, page_table.shape[1]
-
-
-def _one_device(*tensors):
-    """The tensors are on the current device, whose stream the kernels go to."""
-    here = _torch().cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{here}")
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache is [pages, heads_kv, page_size, head_dim]")
+    pages, heads, size, _ = k_cache.shape
+    width = page_table.shape[-1]
+    return (heads, (_array(k_cache, "k_cache", here, torch.int8, (pages, heads, size, dim)), _array(v_cache, "v_cache", here, torch.int8, (pages, heads, dim, size)),
+                    _array(k_scale, "k_scale", here, torch.float32, (pages, heads)), _array(v_scale, "v_scale", here, torch.float32, (pages, heads)), pages, size,
+                    _array(page_table, "page_table", here, torch.int32, (batch, width)), width))
 
 
 def fq_kv_append(Q, K, V, cu_new, past, max_new: int, k_cache, v_cache, k_scale, v_scale, page_table, rope_cos=None, rope_sin=None,
@@ -495,34 +507,40 @@ def fq_kv_append(Q, K, V, cu_new, past, max_new: int, k_cache, v_cache, k_scale,
     """Rotate Q [tokens, heads_q, head_dim] into Q_out and K [tokens, heads_kv, head_dim] into K_out (either None: not wanted), and
     store K and V at positions past[b] .. of each sequence in the paged 8-bit cache, whose codes and scales are updated in place.
     rope_cos, rope_sin fp32 [positions, rope_dim / 2], or None: no rotation."""
-    ldk, ldv = _packed(K, "K"), _packed(V, "V", K)
-    tokens, heads_kv, dim = K.shape
-    heads_q, ldq, ldqo, ldko = heads_kv, heads_kv * dim, heads_kv * dim, heads_kv * dim
+    torch, here = _torch(), _here()
+    shape, ldk = _packed(K, "K", here)
+    dtype = K.dtype
+    ldv = _packed(V, "V", here, shape, dtype)[1]
+    tokens, heads_kv, dim = shape
+    q = q_out = k_out = cos = sin = None
+    heads_q, ldq, ldqo, ldko, rows, half = heads_kv, heads_kv * dim, heads_kv * dim, heads_kv * dim, 0, 0
     if Q_out is not None:
         if Q is None:
             raise ValueError("Q_out without Q")
-        ldq, ldqo, heads_q = _packed(Q, "Q"), _packed(Q_out, "Q_out", Q), Q.shape[1]
-        if Q.shape[0] != tokens or Q.shape[2] != dim or Q.dtype != K.dtype:
+        q_shape, ldq = _packed(Q, "Q", here)
+        heads_q = q_shape[1]
+        if q_shape[0] != tokens or q_shape[2] != dim or Q.dtype != dtype:
             raise ValueError("Q must have K's tokens, head_dim and type")
+        ldqo = _packed(Q_out, "Q_out", here, q_shape, dtype)[1]
+        q, q_out = Q.data_ptr(), Q_out.data_ptr()
     if K_out is not None:
-        ldko = _packed(K_out, "K_out", K)
+        ldko, k_out = _packed(K_out, "K_out", here, shape, dtype)[1], K_out.data_ptr()
     batch = past.numel()
-    _int32(past, "past", (batch,))
-    _int32(cu_new, "cu_new", (batch + 1,))
-    pages, size, width = _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim)
-    rows = half = 0
+    heads, cache = _cache(k_cache, v_cache, k_scale, v_scale, page_table, batch, dim, here)
+    if heads != heads_kv:
+        raise ValueError(f"K has {heads_kv} heads, the cache {heads}")
     if (rope_cos is None) != (rope_sin is None):
         raise ValueError("rope_cos and rope_sin go together")
     if rope_cos is not None:
+        if rope_cos.dim() != 2:
+            raise ValueError("rope_cos is [positions, rope_dim / 2]")
         rows, half = rope_cos.shape
-        for t, name in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")):
-            if not t.is_cuda or _dtype_code(t) != FQ_F32 or t.shape != rope_cos.shape or not t.is_contiguous():
-                raise ValueError(f"{name} must be a contiguous fp32 device tensor [positions, rope_dim / 2]")
-    _one_device(Q if Q_out is not None else None, K, V, cu_new, past, k_cache, v_cache, k_scale, v_scale, page_table, rope_cos, rope_sin, Q_out, K_out)
-    _check(lib().fq_kv_append(_ptr(Q) if Q_out is not None else None, K.data_ptr(), V.data_ptr(), _dtype_code(K), tokens, heads_q, heads_kv,
-                              dim, ldq, ldk, ldv, cu_new.data_ptr(), past.data_ptr(), batch, max_new, _ptr(rope_cos), _ptr(rope_sin), rows,
-                              2 * half, int(bool(interleaved)), _ptr(Q_out), ldqo, _ptr(K_out), ldko, k_cache.data_ptr(), v_cache.data_ptr(),
-                              k_scale.data_ptr(), v_scale.data_ptr(), pages, size, page_table.data_ptr(), width, _stream(stream)))
+        cos, sin = (_array(x, name, here, torch.float32, (rows, half)) for x, name in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")))
+    rc = (_lib or lib()).fq_kv_append(q, K.data_ptr(), V.data_ptr(), _dtype_code(K), tokens, heads_q, heads_kv, dim, ldq, ldk, ldv,
+                                      _array(cu_new, "cu_new", here, torch.int32, (batch + 1,)), _array(past, "past", here, torch.int32, (batch,)), batch, max_new,
+                                      cos, sin, rows, 2 * half, 1 if interleaved else 0, q_out, ldqo, k_out, ldko, *cache, _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def fq_attn_cache_workspace_bytes(batch: int, tokens: int, max_q: int, max_len: int, heads_q: int, heads_kv: int, head_dim: int) -> int:
@@ -533,31 +551,36 @@ def fq_attn_cache(Q, cu_q, lens, max_q: int, max_len: int, k_cache, v_cache, k_s
                   stream=None) -> None:
     """Y = causal attention of Q [tokens, heads_q, head_dim], the last tokens of each sequence (rows cu_q[b] .. cu_q[b + 1] - 1), over the
     lens[b] tokens that the paged 8-bit cache holds of it."""
-    ldq, ldy = _packed(Q, "Q"), _packed(Y, "Y", Q)
-    tokens, heads_q, dim = Q.shape
-    batch, heads_kv = lens.numel(), k_cache.shape[1]
-    _int32(lens, "lens", (batch,))
-    _int32(cu_q, "cu_q", (batch + 1,))
-    pages, size, width = _pages(k_cache, v_cache, k_scale, v_scale, page_table, batch, heads_kv, dim)
-    if not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
-    _one_device(Q, cu_q, lens, k_cache, v_cache, k_scale, v_scale, page_table, Y, workspace)
-    _check(lib().fq_attn_cache(Q.data_ptr(), _dtype_code(Q), tokens, heads_q, heads_kv, dim, ldq, cu_q.data_ptr(), lens.data_ptr(), batch, max_q,
-                               max_len, k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, size,
-                               page_table.data_ptr(), width, scale, Y.data_ptr(), ldy, workspace.data_ptr(),
-                               workspace.numel() * workspace.element_size(), _stream(stream)))
+    torch, here = _torch(), _here()
+    shape, ldq = _packed(Q, "Q", here)
+    ldy = _packed(Y, "Y", here, shape, Q.dtype)[1]
+    tokens, heads_q, dim = shape
+    batch = lens.numel()
+    heads_kv, cache = _cache(k_cache, v_cache, k_scale, v_scale, page_table, batch, dim, here)
+    if workspace.get_device() != here or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on the current device, cuda:{here}")
+    rc = (_lib or lib()).fq_attn_cache(Q.data_ptr(), _dtype_code(Q), tokens, heads_q, heads_kv, dim, ldq, _array(cu_q, "cu_q", here, torch.int32, (batch + 1,)),
+                                       _array(lens, "lens", here, torch.int32, (batch,)), batch, max_q, max_len, *cache, scale, Y.data_ptr(), ldy,
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+    if rc:
+        _check(rc)
 
 
 def fq_attn_prompt(Q, K, V, cu_q, cu_k, max_q: int, scale: float, Y, causal: bool = True, stream=None) -> None:
     """Y = attention of packed queries Q [tokens_q, heads_q, head_dim] over packed K, V [tokens_k, heads_kv, head_dim], sequence by
     sequence (rows cu_q[b] .. and cu_k[b] .. belong together); causal: the last query of a sequence sees its last key."""
-    ldq, ldy, ldk, ldv = _packed(Q, "Q"), _packed(Y, "Y", Q), _packed(K, "K"), _packed(V, "V", K)
-    tokens_q, heads_q, dim = Q.shape
-    if K.shape[2] != dim or K.dtype != Q.dtype:
+    torch, here = _torch(), _here()
+    shape, ldq = _packed(Q, "Q", here)
+    ldy = _packed(Y, "Y", here, shape, Q.dtype)[1]
+    k_shape, ldk = _packed(K, "K", here)
+    ldv = _packed(V, "V", here, k_shape, K.dtype)[1]
+    tokens_q, heads_q, dim = shape
+    tokens_k, heads_kv, dim_k = k_shape
+    if dim_k != dim or K.dtype != Q.dtype:
         raise ValueError("Q, K and V must have the same head_dim and type")
     batch = cu_q.numel() - 1
-    _int32(cu_q, "cu_q", (batch + 1,))
-    _int32(cu_k, "cu_k", (batch + 1,))
-    _one_device(Q, K, V, cu_q, cu_k, Y)
-    _check(lib().fq_attn_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), tokens_q, K.shape[0], heads_q, K.shape[1], dim, ldq, ldk,
-                                ldv, cu_q.data_ptr(), cu_k.data_ptr(), batch, max_q, int(bool(causal)), scale, Y.data_ptr(), ldy, _stream(stream)))
+    rc = (_lib or lib()).fq_attn_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), tokens_q, tokens_k, heads_q, heads_kv, dim, ldq, ldk, ldv,
+                                        _array(cu_q, "cu_q", here, torch.int32, (batch + 1,)), _array(cu_k, "cu_k", here, torch.int32, (batch + 1,)), batch, max_q,
+                                        1 if causal else 0, scale, Y.data_ptr(), ldy, _stream(stream))
+    if rc:
+        _check(rc)

@@ -16,7 +16,7 @@ SOURCES = [("fq_gemm.hip", ["-DFQ_GEMM_MODE=1"], "fq_gemm_i4.o"),
            ("fq_gemm_skinny.hip", [], "fq_gemm_skinny.o"), ("fq_gemm_stream.hip", [], "fq_gemm_stream.o"),
            ("fq_gemm_ring.hip", [], "fq_gemm_ring.o"), ("fq_linear_decode.hip", [], "fq_linear_decode.o"),
            ("fq_linear_few.hip", [], "fq_linear_few.o"),
-           ("fq_kv_append.hip", [], "fq_kv_append.o"), ("fq_attn_cache.hip", [], "fq_attn_cache.o"),
+           ("fq_kv_append.hip", [], "fq_kv_append.o"), ("fq_attn_cache.hip", ["-fno-honor-nans"], "fq_attn_cache.o"),
            ("fq_attn_prompt.hip", ["-fno-honor-nans"], "fq_attn_prompt.o"), ("fq_attn_api.hip", [], "fq_attn_api.o"),
            ("fq_gemm_select.hip", [], "fq_gemm_select.o"), ("fq_peak.hip", [], "fq_peak.o")]
 # -packed-fp32-ops off: keeps the compiler from forming packed fp32 instructions

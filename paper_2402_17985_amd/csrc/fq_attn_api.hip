@@ -110,7 +110,7 @@ int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int t
 size_t fq_attn_cache_workspace_bytes(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv, int head_dim)
 {
     if (batch <= 0 || tokens < 0 || max_q <= 0 || max_len <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q < heads_kv || head_dim <= 0) return 16;
-    const int splits = cache_splits(batch, max_q, max_len, heads_q, heads_kv);
+    const int splits = cache_plan(batch, max_q, max_len, heads_q, heads_kv).splits;
     return splits > 1 ? round_up((size_t)tokens * heads_q * splits * (head_dim + 2) * sizeof(float), 16) + 16 : 16;
 }
 
@@ -139,7 +139,7 @@ int fq_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads
     if (tokens == 0) return FQ_OK;
     return launch_attn_cache(Q, x_dtype, tokens, heads_q, heads_kv, head_dim, ldq, cu_q, lens, batch, max_q, max_len, k_cache, v_cache, k_scale,
                              v_scale, pages, page_size, page_table, table_width, scale, Y, ldy, workspace,
-                             cache_splits(batch, max_q, max_len, heads_q, heads_kv), static_cast<hipStream_t>(stream));
+                             static_cast<hipStream_t>(stream));
 }
 
 int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int tokens_q, int tokens_k, int heads_q, int heads_kv,

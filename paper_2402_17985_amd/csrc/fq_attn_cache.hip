@@ -25,69 +25,72 @@ struct CacheAttn {
     const float *k_scale, *v_scale;
     float *part, *stat;     // with more than one split: [row, head, split, head_dim] and [row, head, split, (maximum, sum)]
     float scale;
-    int tokens, max_q, max_len, heads_q, heads_kv, group, capacity, pages, page, width, splits;
+    int tokens, max_q, max_len, heads_q, heads_kv, group, capacity, pages, page, page_shift, width, splits, waves;
 };
 
-constexpr int CACHE_THREADS = 64 * CACHE_WAVES;
+// A wave-uniform value that no kernel writes while this one runs, by the scalar path: vector loads would queue behind the keys' and values'.
+template <typename T> __device__ __forceinline__ T scalar(const T* p, size_t i)
+{
+    return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
+}
 
-// Eight signed bytes to fp16: with the sign bit turned a byte is q + 128, which as the low byte of 0x64.. is 1152 + q.
+// Eight signed bytes, each plus 1152, in fp16: with its sign bit turned a byte is v + 128, and that as the low byte of 0x64.. is 1152 + v.
+// What the 1152 add to a product is taken off again by its accumulator's start: a subtraction a step instead of one a pair of values.
 __device__ __forceinline__ v8h widen8(uint32_t lo, uint32_t hi)
 {
     lo ^= 0x80808080u;
     hi ^= 0x80808080u;
-    const v2h off = {(_Float16)1152.0f, (_Float16)1152.0f};
-    union {
-        uint32_t u[4];
-        v2h h[4];
-        v8h all;
-    } r;
-    r.u[0] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u);
-    r.u[1] = __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u);
-    r.u[2] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u);
-    r.u[3] = __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.h[i] -= off;
-    return r.all;
+    const v4u r = {__builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u),
+                   __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)};
+    return __builtin_bit_cast(v8h, r);
 }
+constexpr float WIDEN_BIAS = 1152.0f;
 
+// Over the four lanes of a column, 16 apart.
 __device__ __forceinline__ float over_groups_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 __device__ __forceinline__ float over_groups_sum(float v)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
 // NT tiles of 16 columns.  Grid: x the splits of all column tiles, y the key heads, z the sequences.
-template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) void attn_cache_kernel(const CacheAttn a)
+template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, NT <= 2 ? 2 : 1) void attn_cache_kernel(const CacheAttn a)
 {
+    constexpr int ROUND = CACHE_STEP * WAVES;
     typedef typename Stored<DT>::type T;
     constexpr int KC = (D + 63) / 64, VT = D / 16, ROW = D + 4;   // 64-byte pieces of a key, 16-dimension tiles, LDS row
-    __shared__ float gathered[CACHE_WAVES][16][ROW];
-    __shared__ float tops[CACHE_WAVES][16 * NT], sums[CACHE_WAVES][16 * NT];
+    __shared__ float gathered[WAVES][16][ROW];
+    __shared__ float tops[WAVES][16 * NT], sums[WAVES][16 * NT];
 
     const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, h = blockIdx.y, b = blockIdx.z;
-    const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, col = lane % 16, g = lane / 16;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 16, g = lane / 16;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
     const int columns = rows.count * a.group, c0 = tile * 16 * NT;
     if (c0 >= columns) return;
-    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits);
+    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, WAVES);
     if (split > 0 && split * (long long)share >= keys) return;
     const int last = min(c0 + 16 * NT, columns) - 1;
     const int most = visible_keys(keys, rows.count, last / a.group), least = visible_keys(keys, rows.count, c0 / a.group);
     const int from = split * share, to = min((int)min(from + (long long)share, (long long)most), most);
 
-    // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 8 i + 0..7 of its column's head
-    v8h q[NT][KC][2];
+    // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 0..15 of its column's head, as integers of up to 127 * 128
+    // steps, in two limbs of 8 bits: 128 high + low
+    v4i high[NT][KC], low[NT][KC];
     float factor[NT];
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int c = c0 + 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
-        const T* p = static_cast<const T*>(a.Q) + (rows.first + t) * (size_t)a.ldq + (size_t)(h * a.group + cc - t * a.group) * D;
+        const T* p = static_cast<const T*>(a.Q) + (rows.first + t) * (size_t)a.ldq + (size_t)(h * a.group + cc - t * a.group) * D + 16 * g;
         limit[n] = visible_keys(keys, rows.count, t);
         typedef T v8 __attribute__((ext_vector_type(8)));
         v8 raw[KC][2];
@@ -96,32 +99,33 @@ template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) voi
         for (int j = 0; j < KC; ++j)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int d = 64 * j + 16 * g + 8 * i;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) raw[j][i][e] = (T)0.0f;
-                if (d < D) raw[j][i] = *reinterpret_cast<const v8*>(p + d);
-                if constexpr (DT == FQ_BF16)
+                if (64 * j + 16 * g < D) raw[j][i] = *reinterpret_cast<const v8*>(p + 64 * j + 8 * i);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[j][i][e]));
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[j][i][e]));
             }
-        factor[n] = a.scale * LOG2E;
-        if constexpr (DT == FQ_F16) {
+        // the power of two first: the largest magnitude to [1, 2) (or what there is below), so that no size of query over- or underflows
+        top = over_groups_max(top);
+        const uint32_t power = min(max(__float_as_uint(top) >> 23, 1u), 253u);
+        const float down = __uint_as_float((254u - power) << 23), up = __uint_as_float(power << 23);
+        top *= down;
+        const float steps = top > 0.0f ? 16256.0f / top : 0.0f;
+        factor[n] = a.scale * LOG2E * (top * (1.0f / 16256.0f)) * up;
 #pragma unroll
-            for (int j = 0; j < KC; ++j)
+        for (int j = 0; j < KC; ++j)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) q[n][j][i] = raw[j][i];
-        } else {
-            // the largest magnitude of the head to [1, 4): what fp16 cannot hold then is below 2^-24 of it
-            const uint32_t e = min(__float_as_uint(over_groups_max(top)) >> 23, 253u);
-            const float down = __uint_as_float((254u - e) << 23);
-            factor[n] *= e == 0 ? 0x1p-127f : __uint_as_float(e << 23);
+            for (int w = 0; w < 4; ++w) {
+                uint32_t hi = 0, lo = 0;
 #pragma unroll
-            for (int j = 0; j < KC; ++j)
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e2 = 0; e2 < 8; ++e2) q[n][j][i][e2] = (_Float16)((float)raw[j][i][e2] * down);
-        }
+                for (int e = 0; e < 4; ++e) {
+                    const int v = (int)rintf((float)raw[j][w / 2][4 * (w % 2) + e] * down * steps), top7 = (v + 64) >> 7;
+                    hi |= (uint32_t)(top7 & 0xff) << (8 * e);
+                    lo |= (uint32_t)((v - 128 * top7) & 0xff) << (8 * e);
+                }
+                high[n][j][w] = (int)hi;
+                low[n][j][w] = (int)lo;
+            }
     }
 
     v4f o[NT][VT];
@@ -134,71 +138,114 @@ template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) voi
         for (int t = 0; t < VT; ++t) o[n][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
+    // Where a step's keys lie.  A page that does not exist becomes page 0 with none of its keys visible and scales of 0.
+    struct Step {
+        const int8_t *keys, *values;
+        float k_scale, v_scale;
+        bool exists;
+    };
     const size_t block = (size_t)a.page * D;
     const int32_t* table = a.table + (size_t)b * a.width;
     const int key_at = (16 * (col / 4) + col % 4) * D + 16 * g, value_at = col * a.page + 16 * g;
-    for (int k0 = from + wave * CACHE_STEP; k0 < to; k0 += CACHE_SHARE) {
-        const int index = k0 / a.page, off = k0 - index * a.page, page = table[index];
-        if (page < 0 || page >= a.pages) continue;      // no such page: its keys are left out
-        const size_t at = (size_t)page * a.heads_kv + h;
-        const int8_t* kp = a.k_cache + at * block + (size_t)off * D + key_at;
-        const int8_t* vp = a.v_cache + at * block + off + value_at;
-        const float ks = a.k_scale[at], vs = a.v_scale[at];
-        v4u kraw[4][KC], vraw[VT];
+    const auto place = [&](int k0, int page) {
+        const int off = k0 & (a.page - 1);
+        const bool exists = page >= 0 && page < a.pages;
+        const size_t at = (size_t)(exists ? page : 0) * a.heads_kv + h;
+        return Step{a.k_cache + at * block + (size_t)off * D, a.v_cache + at * block + off, exists ? scalar(a.k_scale, at) : 0.0f, exists ? scalar(a.v_scale, at) : 0.0f, exists};
+    };
+    v4u kraw[4][KC], vraw[VT];
+    const auto load_keys = [&](const Step& at) {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int j = 0; j < KC; ++j) {
-                kraw[t][j] = v4u{0, 0, 0, 0};
-                if (64 * j + 16 * g < D) kraw[t][j] = *reinterpret_cast<const v4u*>(kp + 4 * t * D + 64 * j);
+                if (D % 64 != 0 && j == KC - 1) kraw[t][j] = v4u{0, 0, 0, 0};
+                if (D % 64 == 0 || j < KC - 1 || 64 * j + 16 * g < D) kraw[t][j] = *reinterpret_cast<const v4u*>(at.keys + key_at + 4 * t * D + 64 * j);
             }
+    };
+    const auto load_values = [&](const Step& at) {
 #pragma unroll
-        for (int t = 0; t < VT; ++t) vraw[t] = *reinterpret_cast<const v4u*>(vp + 16 * t * a.page);
+        for (int t = 0; t < VT; ++t) vraw[t] = *reinterpret_cast<const v4u*>(at.values + value_at + 16 * t * a.page);
+    };
+
+    // Both operands of a step are on their way while the step before it is worked on, its page number one step earlier still; behind the
+    // last step it again, which costs less than a branch around the loads (the compiler then waits for all of them on either side).
+    const int first = from + wave * CACHE_STEP, steps = first < to ? (to - 1 - first) / ROUND : -1, final = first + steps * ROUND;
+    Step now{};
+    int page_after = -1;
+    if (steps >= 0) {
+        now = place(first, scalar(table, first >> a.page_shift));
+        load_keys(now);
+        load_values(now);
+        page_after = scalar(table, min(first + ROUND, final) >> a.page_shift);
+    }
+    for (int k0 = first; k0 < to; k0 += ROUND) {
+        const Step next = place(min(k0 + ROUND, final), page_after);
+        page_after = scalar(table, min(k0 + 2 * ROUND, final) >> a.page_shift);
+        const float ks = now.k_scale, vs = now.v_scale;
 
         v4f s[NT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int n = 0; n < NT; ++n) {
+                v4i hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
 #pragma unroll
-            for (int j = 0; j < KC; ++j)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const v8h k = widen8(kraw[t][j][2 * i], kraw[t][j][2 * i + 1]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) s[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[n][j][i], s[n][t], 0, 0, 0);
+                for (int j = 0; j < KC; ++j) {
+                    const v4i k = __builtin_bit_cast(v4i, kraw[t][j]);
+                    hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(k, high[n][j], hi, 0, 0, 0);
+                    lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(k, low[n][j], lo, 0, 0, 0);
                 }
-        }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][t][i] = (float)((hi[i] << 7) + lo[i]);      // below 2^28
+            }
+
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(next);
+        __builtin_amdgcn_sched_barrier(0);
 
         v8h p[NT][2];
+        float step_sum[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float f = factor[n] * ks;
-            float m = -INFINITY;
+            const float f = fmaxf(factor[n] * ks, 0x1p-126f);      // not 0: that times a masked score would be no number
+            if (k0 + CACHE_STEP > least || !now.exists) {
+                asm volatile("");      // a branch
+                const int left = now.exists ? limit[n] - k0 - 16 * g : 0;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (4 * t + i >= left) s[n][t][i] = -INFINITY;
+            }
+            float m = s[n][0][0];
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = s[n][t][i] * f;
-                    if (k0 + CACHE_STEP > least && k0 + 16 * g + 4 * t + i >= limit[n]) v = -INFINITY;
-                    s[n][t][i] = v;
-                    m = fmaxf(m, v);
-                }
-            m = fmaxf(over_groups_max(m), top[n]);
-            const float base = m == -INFINITY ? 0.0f : m, keep = __builtin_amdgcn_exp2f(top[n] - base);
-            top[n] = m;
+                for (int i = 0; i < 4; ++i) m = fmaxf(m, s[n][t][i]);
+            m = over_groups_max(m) * f;
+            if (__ballot(top[n] == -INFINITY || m - top[n] > SLACK)) {
+                const float now_top = fmaxf(m, top[n]), keep = now_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - now_top);
+                top[n] = now_top;
+                sum[n] *= keep;
+#pragma unroll
+                for (int t = 0; t < VT; ++t) o[n][t] *= keep;
+            }
+            const float base = top[n] == -INFINITY ? 0.0f : top[n];
             float add = 0.0f;
+            const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(s[n][t][i] - base);
-                    add += e;
-                    p[n][t / 2][4 * (t % 2) + i] = (_Float16)e;
+                for (int i = 0; i < 4; i += 2) {
+                    const v2h e = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i], f, -base)),
+                                   (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i + 1], f, -base))};
+                    add = __builtin_amdgcn_fdot2(e, ones, add, false);      // of the rounded ones: they weigh the values
+                    p[n][t / 2][4 * (t % 2) + i] = e[0];
+                    p[n][t / 2][4 * (t % 2) + i + 1] = e[1];
                 }
-            sum[n] = sum[n] * keep + add;
-#pragma unroll
-            for (int t = 0; t < VT; ++t) o[n][t] *= keep;
+            step_sum[n] = over_groups_sum(add);
+            sum[n] += step_sum[n];
         }
 
 #pragma unroll
@@ -206,21 +253,25 @@ template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) voi
             const v8h v0 = widen8(vraw[t][0], vraw[t][1]), v1 = widen8(vraw[t][2], vraw[t][3]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                v4f r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][0], v4f{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                const float start = -WIDEN_BIAS * step_sum[n];
+                v4f r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][0], v4f{start, start, start, start}, 0, 0, 0);
                 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[n][1], r, 0, 0, 0);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[n][t][i] = __builtin_fmaf(r[i], vs, o[n][t][i]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        load_values(next);
+        __builtin_amdgcn_sched_barrier(0);
+        now = next;
     }
 
     // the waves' shares meet in LDS, one tile of columns after the other
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const float total = over_groups_sum(sum[n]);
         if (g == 0) {
             tops[wave][16 * n + col] = top[n];
-            sums[wave][16 * n + col] = total;
+            sums[wave][16 * n + col] = sum[n];
         }
     }
 #pragma unroll
@@ -228,20 +279,20 @@ template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) voi
         __syncthreads();
         float m = tops[0][16 * n + col];
 #pragma unroll
-        for (int w = 1; w < CACHE_WAVES; ++w) m = fmaxf(m, tops[w][16 * n + col]);
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][16 * n + col]);
         const float mine = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - m);
 #pragma unroll
         for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f*>(&gathered[wave][col][16 * t + 4 * g]) = o[n][t] * mine;
         __syncthreads();
-        for (int i = tid; i < 16 * (D / 4); i += CACHE_THREADS) {
+        for (int i = tid; i < 16 * (D / 4); i += 64 * WAVES) {
             const int cl = i / (D / 4), d = (i - cl * (D / 4)) * 4, c = c0 + 16 * n + cl;
             if (c >= columns) continue;
             float best = tops[0][16 * n + cl], l = 0.0f;
 #pragma unroll
-            for (int w = 1; w < CACHE_WAVES; ++w) best = fmaxf(best, tops[w][16 * n + cl]);
+            for (int w = 1; w < WAVES; ++w) best = fmaxf(best, tops[w][16 * n + cl]);
             v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int w = 0; w < CACHE_WAVES; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 if (best != -INFINITY) l += sums[w][16 * n + cl] * __builtin_amdgcn_exp2f(tops[w][16 * n + cl] - best);
                 y += *reinterpret_cast<const v4f*>(&gathered[w][cl][d]);
             }
@@ -266,60 +317,91 @@ template <int DT, int D, int NT> __global__ __launch_bounds__(CACHE_THREADS) voi
     }
 }
 
-// The shares of one (row, head) joined by one wave.  Grid: x the query heads in groups of the waves, y the query tokens, z the sequences.
-template <int DT, int D> __global__ __launch_bounds__(CACHE_THREADS) void attn_cache_join_kernel(const CacheAttn a)
+constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES;
+
+// The shares of one (row, head) joined by WAVES waves.  Half a wave reads a share, four of its elements a lane.  Grid: x the (head,
+// wave)s in workgroups, y the query tokens, z the sequences.
+template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) void attn_cache_join_kernel(const CacheAttn a)
 {
     typedef typename Stored<DT>::type T;
-    const int b = blockIdx.z, t = blockIdx.y, head = blockIdx.x * CACHE_WAVES + threadIdx.x / 64, lane = threadIdx.x % 64;
+    constexpr int HEADS = JOIN_WAVES / WAVES, TURNS = MAX_SPLITS / 64;
+    __shared__ v4f met[JOIN_WAVES][32];
+    const int b = blockIdx.z, t = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, head = blockIdx.x * HEADS + wave / WAVES;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
-    if (t >= rows.count || head >= a.heads_q) return;
-    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits), used = shares_used(keys, share);
+    if (t >= rows.count || head >= a.heads_q) return;      // with several waves to a head the whole workgroup
+    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.waves), used = shares_used(keys, share);
     const size_t at = ((size_t)(rows.first + t) * a.heads_q + head) * a.splits;
-    float best = -INFINITY;
-    for (int s = lane; s < used; s += 64) best = fmaxf(best, a.stat[2 * (at + s)]);
+    float top[TURNS], sum[TURNS], best = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) {
+        const int s = 64 * k + lane;
+        top[k] = s < used ? a.stat[2 * (at + s)] : -INFINITY;
+        sum[k] = s < used ? a.stat[2 * (at + s) + 1] : 0.0f;
+        best = fmaxf(best, top[k]);
+    }
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) best = fmaxf(best, __shfl_xor(best, s));
-    float y[2] = {0.0f, 0.0f}, l = 0.0f;
-    const int d = 2 * lane;
-    if (best != -INFINITY)
-#pragma unroll 4
-        for (int s = 0; s < used; ++s) {
-            const float w = __builtin_amdgcn_exp2f(a.stat[2 * (at + s)] - best);
-            l += a.stat[2 * (at + s) + 1] * w;
-            if (d < D) {
-                y[0] += a.part[(at + s) * D + d] * w;
-                y[1] += a.part[(at + s) * D + d + 1] * w;
-            }
+    if (best == -INFINITY) best = 0.0f;
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k) {
+        top[k] = __builtin_amdgcn_exp2f(top[k] - best);      // the share's weight
+        l += sum[k] * top[k];
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) l += __shfl_xor(l, s);
+    v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int d = 4 * (lane % 32), slot = wave % WAVES * 2 + lane / 32;
+#pragma unroll
+    for (int k = 0; k < TURNS; ++k)
+#pragma unroll 8
+        for (int s0 = 64 * k; s0 < min(used, 64 * k + 64); s0 += 2 * WAVES) {
+            const int s = s0 + slot;
+            const float w = __shfl(top[k], s % 64);
+            if (s < used && d < D) y += *reinterpret_cast<const v4f*>(a.part + (at + s) * D + d) * w;
         }
-    if (d >= D) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], 32);
+    if constexpr (WAVES > 1) {
+        if (lane < 32) met[wave][lane] = y;
+        __syncthreads();
+        y = met[0][lane % 32];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) y += met[w][lane % 32];
+    }
+    if (d >= D || slot > 0) return;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-    typedef T v2 __attribute__((ext_vector_type(2)));
-    const v2 out = {(T)(y[0] * inv), (T)(y[1] * inv)};
-    *reinterpret_cast<v2*>(static_cast<T*>(a.Y) + (size_t)(rows.first + t) * a.ldy + (size_t)head * D + d) = out;
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    v4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (T)(y[e] * inv);
+    *reinterpret_cast<v4*>(static_cast<T*>(a.Y) + (size_t)(rows.first + t) * a.ldy + (size_t)head * D + d) = out;
 }
 
-template <int DT, int D> int launch(const CacheAttn& a, int batch, hipStream_t stream)
+template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hipStream_t stream)
 {
     const long long columns = (long long)a.max_q * a.group;
-    const int nt = cache_tiles(columns);
-    const dim3 grid((unsigned)((columns + 16 * nt - 1) / (16 * nt) * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
-    if (nt == 1) attn_cache_kernel<DT, D, 1><<<grid, CACHE_THREADS, 0, stream>>>(a);
-    else if (nt == 2) attn_cache_kernel<DT, D, 2><<<grid, CACHE_THREADS, 0, stream>>>(a);
-    else attn_cache_kernel<DT, D, 4><<<grid, CACHE_THREADS, 0, stream>>>(a);
-    if (a.splits > 1)
-        attn_cache_join_kernel<DT, D><<<dim3((unsigned)((a.heads_q + CACHE_WAVES - 1) / CACHE_WAVES), (unsigned)a.max_q, (unsigned)batch), CACHE_THREADS, 0,
-                                        stream>>>(a);
+    const dim3 grid((unsigned)((columns + 16 * tiles - 1) / (16 * tiles) * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
+    if (tiles == 1 && a.waves == 8) attn_cache_kernel<DT, D, 1, 8><<<grid, 512, 0, stream>>>(a);
+    else if (tiles == 1) attn_cache_kernel<DT, D, 1, 4><<<grid, 256, 0, stream>>>(a);
+    else if (tiles == 2 && a.waves == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
+    else if (tiles == 2) attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
+    else attn_cache_kernel<DT, D, 4, 4><<<grid, 256, 0, stream>>>(a);
+    if (a.splits > 16)
+        attn_cache_join_kernel<DT, D, JOIN_WAVES><<<dim3((unsigned)a.heads_q, (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
+    else if (a.splits > 1)
+        attn_cache_join_kernel<DT, D, 1><<<dim3((unsigned)((a.heads_q + JOIN_WAVES - 1) / JOIN_WAVES), (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0,
+                                           stream>>>(a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
 }
 
-template <int DT> int launch_dim(const CacheAttn& a, int head_dim, int batch, hipStream_t stream)
+template <int DT> int launch_dim(const CacheAttn& a, int tiles, int head_dim, int batch, hipStream_t stream)
 {
     switch (head_dim) {
-    case 64: return launch<DT, 64>(a, batch, stream);
-    case 80: return launch<DT, 80>(a, batch, stream);
-    case 96: return launch<DT, 96>(a, batch, stream);
-    default: return launch<DT, 128>(a, batch, stream);
+    case 64: return launch<DT, 64>(a, tiles, batch, stream);
+    case 80: return launch<DT, 80>(a, tiles, batch, stream);
+    case 96: return launch<DT, 96>(a, tiles, batch, stream);
+    default: return launch<DT, 128>(a, tiles, batch, stream);
     }
 }
 
@@ -328,13 +410,16 @@ template <int DT> int launch_dim(const CacheAttn& a, int head_dim, int batch, hi
 int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim, long long ldq, const int32_t* cu_q,
                       const int32_t* lens, int batch, int max_q, int max_len, const int8_t* k_cache, const int8_t* v_cache,
                       const float* k_scale, const float* v_scale, int pages, int page_size, const int32_t* page_table, int table_width,
-                      float scale, void* Y, long long ldy, void* workspace, int splits, hipStream_t stream)
+                      float scale, void* Y, long long ldy, void* workspace, hipStream_t stream)
 {
+    const CachePlan plan = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
+    const int splits = plan.splits;
     float* part = static_cast<float*>(workspace);
     float* stat = part + (splits > 1 ? (size_t)tokens * heads_q * splits * head_dim : 0);
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
-                      heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size, table_width, splits};
-    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, head_dim, batch, stream);
+                      heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
+                      page_size == 128 ? 7 : 6, table_width, splits, plan.waves};
+    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, stream);
 }
 
 }  // namespace fq

@@ -22,6 +22,7 @@ template <> struct Stored<FQ_F32> { typedef float type; };
 template <> struct Stored<FQ_F16> { typedef _Float16 type; };
 template <> struct Stored<FQ_BF16> { typedef __bf16 type; };
 
+constexpr float SLACK = 8.0f;   // accumulators are rescaled only when a maximum has grown by more than a factor 2^8
 constexpr float LOG2E = 1.44269504088896340736f;
 
 }  // namespace

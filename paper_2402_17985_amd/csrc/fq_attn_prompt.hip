@@ -25,7 +25,6 @@ struct PromptAttn {
 };
 
 constexpr int PROMPT_KEYS = 64;   // a tile
-constexpr float SLACK = 8.0f;   // the accumulators are rescaled only when a maximum has grown by more than a factor 2^8
 
 template <int DT> struct Mma;
 template <> struct Mma<FQ_BF16> {

@@ -60,27 +60,30 @@ FQ_BOTH int visible_keys(int keys, int n, int i)
     return v < 0 ? 0 : v;
 }
 
-// Keys of one share when `keys` are dealt over `splits` workgroups: whole steps for every wave, so that the last shares may be empty.
-constexpr int CACHE_WAVES = 4, CACHE_SHARE = CACHE_WAVES * CACHE_STEP;
-FQ_BOTH int share_keys(int keys, int splits)
+// How fq_attn_cache deals out its work.  A workgroup takes a tile of columns (query token, head of the group; 16 * tiles of them) of one
+// sequence and key head, and of its keys all or one of `splits` shares; its waves take the share's steps in turn.
+constexpr int MAX_SPLITS = 256, CACHE_CUS = 256;
+struct CachePlan {
+    int tiles, waves, splits;
+};
+inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int heads_kv)
 {
-    const long long per = (long long)CACHE_SHARE * splits;
-    const long long rounds = (keys + per - 1) / per;
-    return rounds < 1 ? CACHE_SHARE : (int)(rounds * CACHE_SHARE);
+    const long long columns = (long long)max_q * (heads_q / heads_kv);
+    const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+    const long long wgs = (long long)batch * heads_kv * ((columns + 16 * tiles - 1) / (16 * tiles));
+    const int waves = tiles < 4 && wgs <= CACHE_CUS ? 8 : 4;
+    const long long rounds = ((long long)max_len + CACHE_STEP * waves - 1) / (CACHE_STEP * waves);
+    const long long splits = std::min({rounds, CACHE_CUS / wgs, (long long)MAX_SPLITS});
+    return CachePlan{tiles, waves, rounds > 2 && splits > 1 ? (int)splits : 1};
+}
+
+// Keys of one share when `keys` are dealt over `splits` workgroups: whole steps for every wave, so that the last shares may be empty.
+FQ_BOTH int share_keys(int keys, int splits, int waves)
+{
+    const long long round = CACHE_STEP * waves, rounds = (keys + round * splits - 1) / (round * splits);
+    return rounds < 1 ? (int)round : (int)(rounds * round);
 }
 FQ_BOTH int shares_used(int keys, int share) { return (int)(((long long)keys + share - 1) / share); }
-
-// Columns (query token, head of the group) that one workgroup of the cache's attention takes, in tiles of 16.
-inline int cache_tiles(long long columns) { return columns <= 16 ? 1 : columns <= 32 ? 2 : 4; }
-
-// Workgroups among which a sequence's keys are split, so that few sequences fill the device too.
-inline int cache_splits(int batch, int max_q, int max_len, int heads_q, int heads_kv)
-{
-    const long long columns = (long long)max_q * (heads_q / heads_kv), tile = 16LL * cache_tiles(columns);
-    const long long wgs = (long long)batch * heads_kv * ((columns + tile - 1) / tile);
-    const long long most = ((long long)max_len + CACHE_SHARE - 1) / CACHE_SHARE;
-    return (int)std::max(1LL, std::min({most, (1024 + wgs - 1) / wgs, 256LL}));
-}
 
 // Queries of one head that a workgroup of the prompt's attention takes, 32 a wave.
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;

@@ -131,7 +131,7 @@ int launch_kv_append(const void* Q, const void* K, const void* V, int x_dtype, i
 int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim, long long ldq, const int32_t* cu_q,
                       const int32_t* lens, int batch, int max_q, int max_len, const int8_t* k_cache, const int8_t* v_cache,
                       const float* k_scale, const float* v_scale, int pages, int page_size, const int32_t* page_table, int table_width,
-                      float scale, void* Y, long long ldy, void* workspace, int splits, hipStream_t stream);
+                      float scale, void* Y, long long ldy, void* workspace, hipStream_t stream);
 int launch_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int tokens_q, int tokens_k, int heads_q, int heads_kv,
                        int head_dim, long long ldq, long long ldk, long long ldv, const int32_t* cu_q, const int32_t* cu_k, int batch, int max_q,
                        int causal, float scale, void* Y, long long ldy, hipStream_t stream);

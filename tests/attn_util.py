@@ -72,6 +72,11 @@ def prompt_case(q, k, v, cu_q, cu_k, scale, causal, x):
 
 
 def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
+    """Beyond attention_bound's: queries are rounded to 1 / 16256 of their head's largest magnitude (half a step is 2^-15 of it, below 1 / 32512),
+    which moves a score by 2^-14.9 of `scores` at most and a probability and the sum that divides it by as much each; and a step's product
+    is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two products, four lanes' partial sums) of up to 1280 times the
+    sum of p, in codes."""
     exact, spread = A.cache(q, cu_q, lens, table, kc, vc, ks, vs, scale), A.cache(q, cu_q, lens, table, kc, np.abs(vc.astype(np.int16)), ks, vs, scale)
     scores = scale * np.abs(q).max() * 128 * q.shape[2] * ks.max()
-    return exact, attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
+    bound = attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
+    return exact, bound + 2 * scores / 32512 * spread + 16 * 2.0**-24 * 1280 * vs.max()

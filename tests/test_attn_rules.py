@@ -27,15 +27,18 @@ extern "C" void fill(int first, int count, int past, int j, int page, int capaci
 extern "C" long long touched(int tokens, int page) { return pages_touched(tokens, page); }
 extern "C" int keys(int len, int max_len, int capacity) { return cached_keys(len, max_len, capacity); }
 extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i); }
-extern "C" int share(int keys, int splits) { return share_keys(keys, splits); }
+extern "C" int share(int keys, int splits, int waves) { return share_keys(keys, splits, waves); }
 extern "C" int used(int keys, int share) { return shares_used(keys, share); }
-extern "C" int splits(int batch, int max_q, int max_len, int heads_q, int heads_kv) { return cache_splits(batch, max_q, max_len, heads_q, heads_kv); }
+extern "C" void plan(int batch, int max_q, int max_len, int heads_q, int heads_kv, int* out)
+{
+    const CachePlan p = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
+    out[0] = p.tiles; out[1] = p.waves; out[2] = p.splits;
+}
 extern "C" void place(unsigned id, unsigned items, unsigned pairs, unsigned* out)
 {
     const PromptPlace p = prompt_place(id, items, pairs);
     out[0] = p.pair; out[1] = p.item;
 }
-extern "C" int tiles(long long columns) { return cache_tiles(columns); }
 """
 
 
@@ -115,27 +118,32 @@ def test_keys_and_visible_keys(rules):
                 assert rules.visible(keys, n, i) == max(0, keys - n + i + 1)
 
 
-def test_shares_cover_all_keys_in_whole_steps(rules):
+@pytest.mark.parametrize("waves", [4, 8])
+def test_shares_cover_all_keys_in_whole_steps(rules, waves):
     for splits in (1, 2, 3, 7, 64, 256):
         for keys in (0, 1, 255, 256, 257, 1000, 4096, 131072, 2**30 - 1, 2**30):
-            share = rules.share(keys, splits)
-            assert share >= 256 and share % 256 == 0 and share * splits >= keys
+            share = rules.share(keys, splits, waves)
+            assert share >= 64 * waves and share % (64 * waves) == 0 and share * splits >= keys
             used = rules.used(keys, share)
             assert used <= splits and (used - 1) * share < keys <= used * share or (keys == 0 and used == 0)
 
 
-def test_splits_are_bounded_and_one_where_there_is_work_enough(rules):
+def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
+    out = (ctypes.c_int * 3)()
     for batch in (1, 4, 64, 65535):
         for max_q in (1, 5, 512, 65472):
             for max_len in (1, 256, 257, 8192, 2**30):
                 for hq, hkv in ((1, 1), (64, 8), (64, 64), (16384, 1)):
                     if max_q * hq >= 2**30:
                         continue
-                    s = rules.splits(batch, max_q, max_len, hq, hkv)
+                    rules.plan(batch, max_q, max_len, hq, hkv, out)
+                    tiles, waves, splits = out
                     columns = max_q * (hq // hkv)
-                    wgs = batch * hkv * -(-columns // (16 * rules.tiles(ctypes.c_longlong(columns))))
-                    assert 1 <= s <= 256 and (s - 1) * 256 < max_len
-                    assert s == 1 or (wgs < 1024 and max_q <= 65535)
+                    wgs = batch * hkv * -(-columns // (16 * tiles))
+                    assert tiles in (1, 2, 4) and (tiles == 4 or columns <= 16 * tiles) and waves == (8 if tiles < 4 and wgs <= 256 else 4)
+                    assert 1 <= splits <= 256 and (splits - 1) * 64 * waves < max_len
+                    assert splits == 1 or wgs * splits <= 256
+                    assert -(-columns // (16 * tiles)) * splits * 64 * waves < 2**32 and (splits == 1 or max_q <= 65535)
 
 
 @pytest.mark.parametrize("items,pairs", [(1, 1), (1, 7), (3, 8), (5, 9), (16, 23), (2, 64), (7, 1), (64, 3)])
