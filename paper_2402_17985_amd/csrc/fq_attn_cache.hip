@@ -11,40 +11,10 @@
 // No operand passes through LDS: which key of the page stands in which row of the first product is free, and with key
 // 16 (r / 4) + 4 t + r % 4 in row r of tile t a lane's scores are those of 16 consecutive keys, the very ones whose values it
 // reads as 16 consecutive bytes of a dimension (the cache holds values transposed for that) in the second product.
-#include "fq_attn_common.h"
+#include "fq_attn_cache.h"
 
 namespace fq {
 namespace {
-
-struct CacheAttn {
-    const void* Q;
-    void* Y;
-    long long ldq, ldy;
-    const int32_t *cu_q, *lens, *table;
-    const int8_t *k_cache, *v_cache;
-    const float *k_scale, *v_scale;
-    float *part, *stat;     // with more than one split: [row, head, split, head_dim] and [row, head, split, (maximum, sum)]
-    float scale;
-    int tokens, max_q, max_len, heads_q, heads_kv, group, capacity, pages, page, page_shift, width, splits, waves;
-};
-
-// A wave-uniform value that no kernel writes while this one runs, by the scalar path: vector loads would queue behind the keys' and values'.
-template <typename T> __device__ __forceinline__ T scalar(const T* p, size_t i)
-{
-    return ((const __attribute__((address_space(4))) T*)(uintptr_t)p)[i];
-}
-
-// Eight signed bytes, each plus 1152, in fp16: with its sign bit turned a byte is v + 128, and that as the low byte of 0x64.. is 1152 + v.
-// What the 1152 add to a product is taken off again by its accumulator's start: a subtraction a step instead of one a pair of values.
-__device__ __forceinline__ v8h widen8(uint32_t lo, uint32_t hi)
-{
-    lo ^= 0x80808080u;
-    hi ^= 0x80808080u;
-    const v4u r = {__builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u),
-                   __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u), __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)};
-    return __builtin_bit_cast(v8h, r);
-}
-constexpr float WIDEN_BIAS = 1152.0f;
 
 // Over the four lanes of a column, 16 apart.
 __device__ __forceinline__ float over_groups_max(float v)
@@ -63,7 +33,7 @@ __device__ __forceinline__ float over_groups_sum(float v)
 }
 
 // NT tiles of 16 columns.  Grid: x the splits of all column tiles, y the key heads, z the sequences.
-template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, NT <= 2 ? 2 : 1) void attn_cache_kernel(const CacheAttn a)
+template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(const CacheAttn a)
 {
     constexpr int ROUND = CACHE_STEP * WAVES;
     typedef typename Stored<DT>::type T;
@@ -329,7 +299,7 @@ template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) v
     const int b = blockIdx.z, t = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, head = blockIdx.x * HEADS + wave / WAVES;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
     if (t >= rows.count || head >= a.heads_q) return;      // with several waves to a head the whole workgroup
-    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.waves), used = shares_used(keys, share);
+    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.round), used = shares_used(keys, share);
     const size_t at = ((size_t)(rows.first + t) * a.heads_q + head) * a.splits;
     float top[TURNS], sum[TURNS], best = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -381,11 +351,13 @@ template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hi
 {
     const long long columns = (long long)a.max_q * a.group;
     const dim3 grid((unsigned)((columns + 16 * tiles - 1) / (16 * tiles) * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
-    if (tiles == 1 && a.waves == 8) attn_cache_kernel<DT, D, 1, 8><<<grid, 512, 0, stream>>>(a);
+    if (tiles * 16 == WIDE_COLUMNS) {
+        const int rc = launch_attn_cache_wide(a, DT, D, batch, stream);
+        if (rc) return rc;
+    } else if (tiles == 1 && a.round == 8) attn_cache_kernel<DT, D, 1, 8><<<grid, 512, 0, stream>>>(a);
     else if (tiles == 1) attn_cache_kernel<DT, D, 1, 4><<<grid, 256, 0, stream>>>(a);
-    else if (tiles == 2 && a.waves == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
-    else if (tiles == 2) attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
-    else attn_cache_kernel<DT, D, 4, 4><<<grid, 256, 0, stream>>>(a);
+    else if (a.round == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
+    else attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
     if (a.splits > 16)
         attn_cache_join_kernel<DT, D, JOIN_WAVES><<<dim3((unsigned)a.heads_q, (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
     else if (a.splits > 1)
@@ -418,7 +390,7 @@ int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int h
     float* stat = part + (splits > 1 ? (size_t)tokens * heads_q * splits * head_dim : 0);
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
                       heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
-                      page_size == 128 ? 7 : 6, table_width, splits, plan.waves};
+                      page_size == 128 ? 7 : 6, table_width, splits, plan.round};
     return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, stream);
 }
 

@@ -1,0 +1,334 @@
+// fq_attn_cache for many columns (query token, head of the group): pieces of a prompt that follow what the cache holds.
+//
+// Here every key serves many columns and the matrix pipe bounds the call, so the codes are widened to fp16 once per workgroup, on
+// their way into LDS, and the rest is the prompt's attention (fq_attn_prompt.hip): 128 columns of one sequence and key head, 32 a wave,
+// tiles of 64 keys, S^T = K Q^T and O^T += V^T P with P as it lies in the scores' registers.  A tile lies in one page:
+//   its keys' scale goes into the factor of the scores; the keys stay 1152 too large each (see widen8), which adds 1152 times the sum of
+//     the query's elements to every score of a column and is taken off where the maximum is;
+//   its values' scale goes into P, relative to that of the tiles accumulated so far, as an addend of the exponent; where the two are
+//     more than a factor 64 apart the accumulators change to the new one first, so that fp16 holds every P.
+#include "fq_attn_cache.h"
+
+namespace fq {
+namespace {
+
+constexpr int WIDE_WAVES = WIDE_COLUMNS / 32, WIDE_THREADS = 64 * WIDE_WAVES;
+
+template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn_cache_wide_kernel(const CacheAttn a)
+{
+    typedef typename Stored<DT>::type T;
+    typedef Mma<FQ_F16> M;
+    constexpr int KS = D / 16, VT = (D + 31) / 32, C = D / 8, ROW = 2 * D, KTILE = CACHE_STEP * ROW, VROW = 2 * CACHE_STEP, VTILE = 32 * VT * VROW;
+    constexpr int PIECES = (CACHE_STEP * D / 16 + WIDE_THREADS - 1) / WIDE_THREADS;      // 16 codes each, of keys and of values, per thread
+    constexpr bool EVEN = CACHE_STEP * D / 16 % WIDE_THREADS == 0;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (KTILE + VTILE)];            // [keys, two stages][values, two stages]
+
+    const int block = blockIdx.x / a.splits, split = blockIdx.x - block * a.splits, h = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
+    const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
+    const int columns = rows.count * a.group, c0 = block * WIDE_COLUMNS;
+    if (c0 >= columns) return;
+    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.round);
+    if (split > 0 && split * (long long)share >= keys) return;
+    const auto visible = [&](int c) { return visible_keys(keys, rows.count, min(c, columns - 1) / a.group); };
+    const int w0 = c0 + 32 * wave, c = w0 + col, cc = min(c, columns - 1), token = cc / a.group, head = h * a.group + cc - token * a.group;
+    const int from = split * share, to = (int)min(from + (long long)share, (long long)visible(c0 + WIDE_COLUMNS - 1));
+    const int mine = visible(c), least = visible(w0), tiles = to > from ? (to - from + CACHE_STEP - 1) / CACHE_STEP : 0;
+    const int wave_to = w0 >= columns ? from : min(to, visible(w0 + 31)), own = wave_to > from ? (wave_to - from + CACHE_STEP - 1) / CACHE_STEP : 0;
+
+    // the queries in fp16: lane (col, half) holds elements 16 e + 8 half + 0..7 of its column's head
+    v8h q[KS];
+    float factor = a.scale * LOG2E, bias = 0.0f;
+    {
+        typedef T v8 __attribute__((ext_vector_type(8)));
+        const T* p = static_cast<const T*>(a.Q) + (rows.first + (size_t)token) * a.ldq + (size_t)head * D + 8 * half;
+        v8 raw[KS];
+        float top = 0.0f;
+#pragma unroll
+        for (int e = 0; e < KS; ++e) {
+            raw[e] = *reinterpret_cast<const v8*>(p + 16 * e);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf((float)raw[e][i]));
+        }
+        if constexpr (DT == FQ_F16) {
+#pragma unroll
+            for (int e = 0; e < KS; ++e) q[e] = raw[e];
+        } else {
+            // the largest magnitude to [1, 4): what fp16 cannot hold then is below 2^-24 of it
+            const uint32_t power = min(max(__float_as_uint(over_halves_max(top)) >> 23, 1u), 253u);
+            const float down = __uint_as_float((254u - power) << 23);
+            factor *= __uint_as_float(power << 23);
+#pragma unroll
+            for (int e = 0; e < KS; ++e)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[e][i] = (_Float16)((float)raw[e][i] * down);
+        }
+        const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+        for (int e = 0; e < KS; ++e)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) bias = __builtin_amdgcn_fdot2(v2h{q[e][i], q[e][i + 1]}, ones, bias, false);
+        bias = WIDEN_BIAS * over_halves_sum(bias);
+    }
+
+    // Where a tile lies; behind the last tile it again.  A page that does not exist: page 0 with none of its keys visible and scales of 0.
+    struct Place {
+        const int8_t *keys, *values;
+        float k_scale, v_scale;
+        bool exists;
+    };
+    const size_t page_bytes = (size_t)a.page * D;
+    const int32_t* table = a.table + (size_t)b * a.width;
+    const auto first_key = [&](int i) { return from + CACHE_STEP * min(i, tiles - 1); };
+    const auto page_of = [&](int i) { return scalar(table, first_key(i) >> a.page_shift); };
+    const auto place = [&](int i, int page) {
+        const int off = first_key(i) & (a.page - 1);
+        const bool exists = page >= 0 && page < a.pages;
+        const size_t at = (size_t)(exists ? page : 0) * a.heads_kv + h;
+        return Place{a.k_cache + at * page_bytes + (size_t)off * D, a.v_cache + at * page_bytes + off, exists ? scalar(a.k_scale, at) : 0.0f,
+                     exists ? scalar(a.v_scale, at) : 0.0f, exists};
+    };
+    v4u kreg[PIECES], vreg[PIECES];
+    const auto load_keys = [&](const Place& at) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int i = p * WIDE_THREADS + tid;
+            if (EVEN || i < CACHE_STEP * D / 16) kreg[p] = *reinterpret_cast<const v4u*>(at.keys + 16 * i);
+        }
+    };
+    const auto load_values = [&](const Place& at) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int i = p * WIDE_THREADS + tid;
+            if (EVEN || i < 4 * D) vreg[p] = *reinterpret_cast<const v4u*>(at.values + (i / 4) * a.page + 16 * (i % 4));
+        }
+    };
+    // rows of keys as in the prompt's kernel; a row of values holds the 64 keys of a dimension, of each 16 first 0..3, 8..11, then 4..7, 12..15:
+    // what a lane of either half needs for a product lies together
+    const auto put_keys = [&](int stage) {
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int i = p * WIDE_THREADS + tid, r = i / (D / 16), piece = 2 * (i - r * (D / 16)), turn = key_turn(C, r);
+            if (!EVEN && i >= CACHE_STEP * D / 16) continue;
+            uint8_t* row = lds + stage * KTILE + r * ROW;
+            *reinterpret_cast<v8h*>(row + (piece + turn) % C * 16) = widen8(kreg[p][0], kreg[p][1]);
+            *reinterpret_cast<v8h*>(row + (piece + 1 + turn) % C * 16) = widen8(kreg[p][2], kreg[p][3]);
+        }
+    };
+    const auto put_values = [&](int stage) {
+        const _Float16 off = (_Float16)WIDEN_BIAS;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int i = p * WIDE_THREADS + tid, d = i / 4, piece = 2 * (i % 4), turn = key_turn(8, d);
+            if (!EVEN && i >= 4 * D) continue;
+            uint8_t* row = lds + 2 * KTILE + stage * VTILE + d * VROW;
+            *reinterpret_cast<v8h*>(row + (piece + turn) % 8 * 16) = widen8(vreg[p][0], vreg[p][2]) - off;
+            *reinterpret_cast<v8h*>(row + (piece + 1 + turn) % 8 * 16) = widen8(vreg[p][1], vreg[p][3]) - off;
+        }
+    };
+
+    v16f o[VT], s[2];
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
+    float top = -INFINITY, sum = 0.0f, unit = 0.0f;      // of the scaled scores; over this lane's keys; values' scale that o counts in
+    v8h p[4];                                            // 16 keys each
+
+    uint32_t key_at[KS], value_at[4];
+#pragma unroll
+    for (int e = 0; e < KS; ++e) key_at[e] = col * ROW + (2 * e + half + key_turn(C, col)) % C * 16;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) value_at[n] = 2 * KTILE + col * VROW + (2 * n + half + key_turn(8, col)) % 8 * 16;
+
+    // O^T += V^T P of a tile (PV), then S^T of the next (QK); first operands come from LDS AHEAD - 1 products early, the order is kept
+    const auto products = [&](auto with_pv, auto with_qk) {
+        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 5;
+        v8h ring[AHEAD];
+        const auto fetch = [&](int n) {
+            const uint32_t at = n < PV ? value_at[n / VT] + 32 * (n % VT) * VROW : key_at[(n - PV) / 2] + 32 * ((n - PV) % 2) * ROW;
+            ring[n % AHEAD] = *reinterpret_cast<const v8h*>(lds + at);
+        };
+#pragma unroll
+        for (int n = 0; n < AHEAD - 1; ++n) fetch(n);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            if (n + AHEAD - 1 < N) fetch(n + AHEAD - 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n < PV) {
+                o[n % VT] = M::mul(ring[n % AHEAD], p[n / VT], o[n % VT]);
+            } else {
+                const int e = (n - PV) / 2, t = (n - PV) % 2;
+                if (e == 0)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) s[t][k] = 0.0f;
+                s[t] = M::mul(ring[n % AHEAD], q[e], s[t]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    const auto softmax = [&](int i, const Place& at) {
+        const int k0 = from + CACHE_STEP * i;
+        const float f = fmaxf(factor * at.k_scale, 0x1p-126f), shift = bias * f;      // f is not 0: that times a masked score would be no number
+        if (k0 + CACHE_STEP > least || !at.exists) {
+            asm volatile("");      // a branch
+            const int left = at.exists ? mine - k0 - 4 * half : 0;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (32 * t + 8 * (e / 4) + e % 4 >= left || !at.exists) s[t][e] = -INFINITY;
+        }
+        float m = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) m = fmaxf(m, fmaxf(s[0][e], s[1][e]));
+        m = __builtin_fmaf(over_halves_max(m), f, -shift);
+        if (__ballot(top == -INFINITY || m - top > SLACK)) {
+            const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - now);
+            top = now;
+            sum *= keep;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) o[t] *= keep;
+        }
+        if (at.v_scale > 0.0f && !(at.v_scale <= 64.0f * unit && at.v_scale >= unit * (1.0f / 64))) {
+            asm volatile("");
+            const float change = unit / at.v_scale;
+            unit = at.v_scale;
+#pragma unroll
+            for (int t = 0; t < VT; ++t) o[t] *= change;
+        }
+        // values of scale 0: probabilities too small for fp16, whose sum still counts
+        const float part = at.v_scale > 0.0f ? at.v_scale / unit : 0x1p-60f;
+        const float off = (top == -INFINITY ? 0.0f : top) + shift - __builtin_amdgcn_logf(part);
+        float add = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], f, -off));
+                add += w;
+                p[2 * t + e / 8][e % 8] = (_Float16)w;
+            }
+        sum += add / part;
+    };
+
+    // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), the next is asked for, PV of tile i, QK and softmax of i + 1
+    if (tiles > 0) {
+        Place next = place(0, page_of(0)), after = place(1, page_of(1)), later = place(2, page_of(2));      // tiles i + 1, i + 2, i + 3
+        load_keys(next);
+        load_values(next);
+        put_keys(0);
+        put_values(0);
+        load_keys(after);
+        load_values(after);
+        put_keys(1);
+        load_keys(later);
+        int page_then = page_of(3);
+        __syncthreads();
+        if (own > 0) {
+            products(no, yes);
+            softmax(0, next);
+        }
+        next = after;
+        after = later;
+        later = place(3, page_then);
+        page_then = page_of(4);
+        __syncthreads();
+        int i = 0, key_move = KTILE, value_move = VTILE;
+#pragma unroll
+        for (int e = 0; e < KS; ++e) key_at[e] += KTILE;
+        const auto begin_step = [&] {
+            put_keys(i % 2);
+            put_values((i + 1) % 2);
+            load_keys(later);
+            load_values(after);
+        };
+        const auto end_step = [&] {
+            next = after;
+            after = later;
+            later = place(i + 4, page_then);
+            page_then = page_of(i + 5);
+            ++i;
+            __syncthreads();
+        };
+        while (i + 1 < own) {
+            begin_step();
+            __builtin_amdgcn_s_setprio(1);
+            products(yes, yes);
+            __builtin_amdgcn_s_setprio(0);
+            softmax(i + 1, next);
+#pragma unroll
+            for (int e = 0; e < KS; ++e) key_at[e] -= key_move;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) value_at[n] += value_move;
+            key_move = -key_move;
+            value_move = -value_move;
+            end_step();
+        }
+        if (own > 0) {
+            begin_step();
+            products(yes, no);
+            end_step();
+        }
+        while (i < tiles) {
+            begin_step();
+            end_step();
+        }
+    }
+
+    sum = over_halves_sum(sum);
+    if (c >= columns) return;
+    const size_t row = rows.first + (size_t)token;
+    if (a.splits > 1) {
+        const size_t at = (row * a.heads_q + head) * a.splits + split;
+        if (half == 0) {
+            a.stat[2 * at] = top;
+            a.stat[2 * at + 1] = sum;
+        }
+#pragma unroll
+        for (int t = 0; t < VT; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (32 * t + 8 * e < D) *reinterpret_cast<v4f*>(a.part + at * D + 32 * t + 8 * e + 4 * half) =
+                    v4f{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]} * unit;
+        return;
+    }
+    const float inv = sum > 0.0f ? unit / sum : 0.0f;
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    T* yp = static_cast<T*>(a.Y) + row * (size_t)a.ldy + (size_t)head * D + 4 * half;
+#pragma unroll
+    for (int t = 0; t < VT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (32 * t + 8 * e >= D) continue;
+            v4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = (T)(o[t][4 * e + i] * inv);
+            *reinterpret_cast<v4*>(yp + 32 * t + 8 * e) = y;
+        }
+}
+
+template <int DT> int launch(const CacheAttn& a, int head_dim, int batch, hipStream_t stream)
+{
+    const long long columns = (long long)a.max_q * a.group;
+    const dim3 grid((unsigned)((columns + WIDE_COLUMNS - 1) / WIDE_COLUMNS * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
+    switch (head_dim) {
+    case 64: attn_cache_wide_kernel<DT, 64><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
+    case 80: attn_cache_wide_kernel<DT, 80><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
+    case 96: attn_cache_wide_kernel<DT, 96><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
+    default: attn_cache_wide_kernel<DT, 128><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
+}
+
+}  // namespace
+
+int launch_attn_cache_wide(const CacheAttn& a, int x_dtype, int head_dim, int batch, hipStream_t stream)
+{
+    return x_dtype == FQ_F16 ? launch<FQ_F16>(a, head_dim, batch, stream) : launch<FQ_BF16>(a, head_dim, batch, stream);
+}
+
+}  // namespace fq

@@ -1,5 +1,7 @@
 // What the attention translation units share (GPU code only; everything has internal linkage).
 #pragma once
+#include <type_traits>
+
 #include "fq_attn_rules.h"
 #include "fq_internal.h"
 
@@ -24,6 +26,36 @@ template <> struct Stored<FQ_BF16> { typedef __bf16 type; };
 
 constexpr float SLACK = 8.0f;   // accumulators are rescaled only when a maximum has grown by more than a factor 2^8
 constexpr float LOG2E = 1.44269504088896340736f;
+
+template <int DT> struct Mma;
+template <> struct Mma<FQ_BF16> {
+    typedef __bf16 T;
+    typedef v8bf v8;
+    typedef v4bf v4;
+    static __device__ __forceinline__ v16f mul(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mma<FQ_F16> {
+    typedef _Float16 T;
+    typedef v8h v8;
+    typedef v4h v4;
+    static __device__ __forceinline__ v16f mul(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+// Rows of C 16-byte pieces lie in LDS without gaps; where 16 rows are read at a time, the same piece of each, piece c of row r lies at place
+// (c + key_turn(C, r)) mod C, which spreads them over the 64 banks (256 bytes).
+constexpr int key_turn(int C, int r) { return C == 16 ? r % 16 : C == 12 ? r % 16 / 4 : C == 10 ? r % 16 / 8 : r % 16 / 2; }
+
+// Of the two lanes that share a query, lane and lane + 32.
+__device__ __forceinline__ float over_halves_max(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float over_halves_sum(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 
 }  // namespace
 }  // namespace fq

@@ -8,8 +8,6 @@
 //                 reduction is free as long as the values follow, and their transposed reads from LDS take four consecutive
 //                 keys of a dimension, as a lane holds them.
 // P is rounded to the input's type, the row sums are taken before that in 32 bits.
-#include <type_traits>
-
 #include "fq_attn_common.h"
 
 namespace fq {
@@ -26,24 +24,9 @@ struct PromptAttn {
 
 constexpr int PROMPT_KEYS = 64;   // a tile
 
-template <int DT> struct Mma;
-template <> struct Mma<FQ_BF16> {
-    typedef __bf16 T;
-    typedef v8bf v8;
-    typedef v4bf v4;
-    static __device__ __forceinline__ v16f mul(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
-};
-template <> struct Mma<FQ_F16> {
-    typedef _Float16 T;
-    typedef v8h v8;
-    typedef v4h v4;
-    static __device__ __forceinline__ v16f mul(v8 a, v8 b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-};
-
 // A tile in LDS is rows of D elements without gaps, as the direct copies from global memory fill it, with the 16-byte pieces of a
 // row rotated: piece c of row r lies at place (c + turn(r)) mod (D / 8), so that rows that are read together lie on different banks
 // (64 of them, 256 bytes).  Keys are read 16 rows at a time, the same piece of each; values 4 rows at a time, 4 pieces of each.
-constexpr int key_turn(int C, int r) { return C == 16 ? r % 16 : C == 12 ? r % 16 / 4 : C == 10 ? r % 16 / 8 : r % 16 / 2; }
 constexpr int value_turn(int C, int r) { return C == 16 ? r % 4 * 4 : C == 8 ? r % 4 / 2 * 4 : 0; }
 
 // Four 2-byte elements of a column out of row-major LDS: of 16 neighbouring lanes, lanes 4 r .. 4 r + 3 point at 16 consecutive
@@ -62,18 +45,6 @@ __device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t l
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %0" : : "s"(uniform_base), "v"(lane_offset), "s"(lds_base) : "memory");
 }
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
-
-// Of the two lanes that share a query, lane and lane + 32.
-__device__ __forceinline__ float over_halves_max(float v)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float over_halves_sum(float v)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
 
 // A workgroup's sequence.  Of at most 64 it is the one that is nth by its number of keys, longest first: long ones begun last would run on
 // alone.  All offsets are loaded at once, one sequence a lane, so that the order costs no further trip to memory.

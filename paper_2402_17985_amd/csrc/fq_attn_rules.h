@@ -61,27 +61,29 @@ FQ_BOTH int visible_keys(int keys, int n, int i)
 }
 
 // How fq_attn_cache deals out its work.  A workgroup takes a tile of columns (query token, head of the group; 16 * tiles of them) of one
-// sequence and key head, and of its keys all or one of `splits` shares; its waves take the share's steps in turn.
-constexpr int MAX_SPLITS = 256, CACHE_CUS = 256;
+// sequence and key head, and of its keys all or one of `splits` shares, `round` steps at a time: its waves take the steps of a round in turn, or (many
+// columns) each step together.
+constexpr int MAX_SPLITS = 256, CACHE_CUS = 256, WIDE_COLUMNS = 128;
 struct CachePlan {
-    int tiles, waves, splits;
+    int tiles, round, splits;
 };
 inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int heads_kv)
 {
     const long long columns = (long long)max_q * (heads_q / heads_kv);
-    const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : 4;
+    const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : WIDE_COLUMNS / 16;
+    const bool wide = tiles > 2;
     const long long wgs = (long long)batch * heads_kv * ((columns + 16 * tiles - 1) / (16 * tiles));
-    const int waves = tiles < 4 && wgs <= CACHE_CUS ? 8 : 4;
-    const long long rounds = ((long long)max_len + CACHE_STEP * waves - 1) / (CACHE_STEP * waves);
-    const long long splits = std::min({rounds, CACHE_CUS / wgs, (long long)MAX_SPLITS});
-    return CachePlan{tiles, waves, rounds > 2 && splits > 1 ? (int)splits : 1};
+    const int round = wide ? 1 : wgs <= CACHE_CUS ? 8 : 4;
+    const long long rounds = ((long long)max_len + CACHE_STEP * round - 1) / (CACHE_STEP * round);
+    const long long splits = std::min({wide ? rounds / 4 : rounds, (wide ? 2 * CACHE_CUS : CACHE_CUS) / wgs, (long long)MAX_SPLITS});
+    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1};
 }
 
-// Keys of one share when `keys` are dealt over `splits` workgroups: whole steps for every wave, so that the last shares may be empty.
-FQ_BOTH int share_keys(int keys, int splits, int waves)
+// Keys of one share when `keys` are dealt over `splits` workgroups: whole rounds, so that the last shares may be empty.
+FQ_BOTH int share_keys(int keys, int splits, int round)
 {
-    const long long round = CACHE_STEP * waves, rounds = (keys + round * splits - 1) / (round * splits);
-    return rounds < 1 ? (int)round : (int)(rounds * round);
+    const long long step = CACHE_STEP * round, rounds = (keys + step * splits - 1) / (step * splits);
+    return rounds < 1 ? (int)step : (int)(rounds * step);
 }
 FQ_BOTH int shares_used(int keys, int share) { return (int)(((long long)keys + share - 1) / share); }
 

@@ -56,9 +56,14 @@ def attention_bound(exact, spread, scores, keys, dim, vmax, x, p_half):
 
 
 def check(got, exact, bound, where):
+    """Within the bound; infinite where the result is surely beyond the type (fp16 rounds 65520 and more to infinity), either between."""
+    limit = 65520.0 if got.dtype == torch.float16 else 3.4e38
     got = got.float().cpu().numpy().astype(np.float64)
-    assert np.isfinite(got).all(), f"{where}: not finite"
-    off = np.abs(got - exact) / bound
+    surely = np.abs(exact) - bound >= limit
+    assert (got[surely] == np.sign(exact[surely]) * np.inf).all(), f"{where}: not infinite where the result is beyond the type"
+    fine = np.abs(exact) + bound < limit
+    assert np.isfinite(got[fine]).all() and not np.isnan(got).any(), f"{where}: not finite"
+    off = np.where(fine, np.abs(np.where(fine, got, 0.0) - exact) / bound, 0.0)
     worst = np.unravel_index(np.argmax(off), off.shape)
     assert off.max() <= 1.0, f"{where}: {off.max():.2f} times the bound at {worst}: {got[worst]} for {exact[worst]}"
 
@@ -72,11 +77,14 @@ def prompt_case(q, k, v, cu_q, cu_k, scale, causal, x):
 
 
 def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
-    """Beyond attention_bound's: queries are rounded to 1 / 16256 of their head's largest magnitude (half a step is 2^-15 of it, below 1 / 32512),
-    which moves a score by 2^-14.9 of `scores` at most and a probability and the sum that divides it by as much each; and a step's product
-    is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two products, four lanes' partial sums) of up to 1280 times the
-    sum of p, in codes."""
+    """Beyond attention_bound's, for up to 32 columns (query tokens times heads of a group): queries are rounded to 1 / 16256 of their
+    head's largest magnitude (half a step is below 1 / 32512 of it), which moves a score by `scores` / 32512 at most and a probability and the
+    sum that divides it by as much each; and a step's product is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two
+    products, four lanes' partial sums) of up to 1280 times the sum of p, in codes.
+    For more columns: the scores' 32-bit sums are of codes plus 1152, up to 1280 where `scores` counts 128."""
     exact, spread = A.cache(q, cu_q, lens, table, kc, vc, ks, vs, scale), A.cache(q, cu_q, lens, table, kc, np.abs(vc.astype(np.int16)), ks, vs, scale)
     scores = scale * np.abs(q).max() * 128 * q.shape[2] * ks.max()
     bound = attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
+    if int(np.diff(cu_q).max()) * (q.shape[1] // kc.shape[1]) > 32:
+        return exact, bound + 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread
     return exact, bound + 2 * scores / 32512 * spread + 16 * 2.0**-24 * 1280 * vs.max()

@@ -27,12 +27,12 @@ extern "C" void fill(int first, int count, int past, int j, int page, int capaci
 extern "C" long long touched(int tokens, int page) { return pages_touched(tokens, page); }
 extern "C" int keys(int len, int max_len, int capacity) { return cached_keys(len, max_len, capacity); }
 extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i); }
-extern "C" int share(int keys, int splits, int waves) { return share_keys(keys, splits, waves); }
+extern "C" int share(int keys, int splits, int round) { return share_keys(keys, splits, round); }
 extern "C" int used(int keys, int share) { return shares_used(keys, share); }
 extern "C" void plan(int batch, int max_q, int max_len, int heads_q, int heads_kv, int* out)
 {
     const CachePlan p = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
-    out[0] = p.tiles; out[1] = p.waves; out[2] = p.splits;
+    out[0] = p.tiles; out[1] = p.round; out[2] = p.splits;
 }
 extern "C" void place(unsigned id, unsigned items, unsigned pairs, unsigned* out)
 {
@@ -118,7 +118,7 @@ def test_keys_and_visible_keys(rules):
                 assert rules.visible(keys, n, i) == max(0, keys - n + i + 1)
 
 
-@pytest.mark.parametrize("waves", [4, 8])
+@pytest.mark.parametrize("waves", [1, 4, 8])
 def test_shares_cover_all_keys_in_whole_steps(rules, waves):
     for splits in (1, 2, 3, 7, 64, 256):
         for keys in (0, 1, 255, 256, 257, 1000, 4096, 131072, 2**30 - 1, 2**30):
@@ -137,13 +137,13 @@ def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
                     if max_q * hq >= 2**30:
                         continue
                     rules.plan(batch, max_q, max_len, hq, hkv, out)
-                    tiles, waves, splits = out
+                    tiles, rnd, splits = out
                     columns = max_q * (hq // hkv)
                     wgs = batch * hkv * -(-columns // (16 * tiles))
-                    assert tiles in (1, 2, 4) and (tiles == 4 or columns <= 16 * tiles) and waves == (8 if tiles < 4 and wgs <= 256 else 4)
-                    assert 1 <= splits <= 256 and (splits - 1) * 64 * waves < max_len
-                    assert splits == 1 or wgs * splits <= 256
-                    assert -(-columns // (16 * tiles)) * splits * 64 * waves < 2**32 and (splits == 1 or max_q <= 65535)
+                    assert tiles in (1, 2, 8) and (tiles == 8 or columns <= 16 * tiles) and rnd == (1 if tiles == 8 else 8 if wgs <= 256 else 4)
+                    assert 1 <= splits <= 256 and (splits - 1) * 64 * rnd < max_len
+                    assert splits == 1 or wgs * splits <= (512 if tiles == 8 else 256)
+                    assert -(-columns // (16 * tiles)) * splits * 512 < 2**32 and (splits == 1 or max_q <= 65535)
 
 
 @pytest.mark.parametrize("items,pairs", [(1, 1), (1, 7), (3, 8), (5, 9), (16, 23), (2, 64), (7, 1), (64, 3)])

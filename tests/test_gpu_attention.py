@@ -146,14 +146,18 @@ def test_cache_attention_of_single_tokens(x, dim, page, heads):
     ("f16", 96, 64, (5, 5), [300, 70], [33, 70]),             # every token of a sequence is a query
     ("bf16", 80, 64, (14, 2), [90, 3], [20, 6]),              # more queries than tokens: some see none
     ("bf16", 128, 64, (16, 1), [200], [30]),
-    ("f16", 64, 64, (32, 1), [70, 0, 130], [1, 2, 1])])
+    ("f16", 64, 64, (32, 1), [70, 0, 130], [1, 2, 1]),
+    ("f16", 128, 128, (8, 2), [128, 300, 64, 63], [128, 100, 5, 0]),
+    ("bf16", 96, 64, (3, 3), [200, 0, 400], [129, 40, 33]),
+    ("bf16", 80, 128, (4, 1), [500], [70]), ("f16", 64, 64, (2, 1), [260, 65], [150, 66])])
 def test_cache_attention_of_several_tokens(x, dim, page, heads, lens, queries):
     _cache_both(np.random.default_rng(sum(lens)), x, dim, page, *heads, lens, queries, spare_rows=3)
 
 
 @pytest.mark.parametrize("x,dim,page,heads,lens,queries", [
     ("bf16", 128, 64, (2, 1), [3000], [1]), ("f16", 64, 128, (4, 2), [5000, 1, 0, 2100], [1, 1, 1, 1]),
-    ("bf16", 80, 64, (2, 2), [257, 1025], [3, 1]), ("f16", 128, 64, (12, 1), [1500, 20], [3, 40])])
+    ("bf16", 80, 64, (2, 2), [257, 1025], [3, 1]), ("f16", 128, 64, (12, 1), [1500, 20], [3, 40]),
+    ("bf16", 64, 64, (4, 1), [1100, 600], [70, 9]), ("f16", 96, 128, (6, 2), [2100], [25])])
 def test_cache_attention_split_over_the_keys(x, dim, page, heads, lens, queries):
     rng = np.random.default_rng(sum(lens))
     tokens = sum(queries)
@@ -162,7 +166,25 @@ def test_cache_attention_split_over_the_keys(x, dim, page, heads, lens, queries)
     _cache_both(rng, x, dim, page, *heads, lens, queries, max_len=60000)     # a bound far above the lengths
 
 
+@pytest.mark.parametrize("spread", [1.0, 12.0])
+def test_cache_attention_of_many_columns_over_pages_of_very_different_scales(spread):
+    """Values' scales up to a factor e^24 apart between neighbouring pages, and pages of zeros."""
+    rng, real = np.random.default_rng(9), U.filled_cache
+    def filled(*shape):
+        k, v, ks, vs = real(*shape)
+        vs = np.exp(rng.uniform(-spread, spread, vs.shape)).astype(np.float32)
+        vs[::4], ks[1::5] = 0.0, 0.0
+        return k, v, ks, vs
+    try:
+        U.filled_cache = filled
+        _cache_both(rng, "bf16", 64, 64, 4, 2, [1000, 300], [40, 20])
+        _cache_both(rng, "f16", 64, 64, 4, 2, [1000, 300], [1, 2])
+    finally:
+        U.filled_cache = real
+
+
 def test_cache_attention_leaves_out_pages_that_do_not_exist():
+    _cache_both(np.random.default_rng(5), "f16", 128, 64, 4, 2, [200, 64, 400], [50, 20, 21], bad=((0, 1, -1), (1, 0, 0), (2, 6, 1 << 20), (2, 0, -(1 << 31))))
     _cache_both(np.random.default_rng(5), "bf16", 64, 64, 4, 2, [200, 64, 400], [1, 1, 2], bad=((0, 1, -1), (1, 0, 0), (2, 6, 1 << 20), (2, 0, -(1 << 31))))
 
 
