@@ -132,6 +132,8 @@ int fq_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads
     if (rc) return rc;
     if (max_len <= 0) return fail(FQ_ERR_SHAPE, "max_len = %d must be positive", max_len);
     if ((long long)max_q * heads_q >= (1LL << 30)) return fail(FQ_ERR_RANGE, "max_q = %d queries of %d heads: at most 2^30 together", max_q, heads_q);
+    if (!cache_holds(cache_plan(batch, max_q, max_len, heads_q, heads_kv), batch, max_q, heads_kv))
+        return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);
     if (!workspace) return fail(FQ_ERR_NULL, "workspace is NULL");
     if (!aligned16(workspace)) return fail(FQ_ERR_ALIGN, "workspace is not 16-byte aligned");
     const size_t need = fq_attn_cache_workspace_bytes(batch, tokens, max_q, max_len, heads_q, heads_kv, head_dim);

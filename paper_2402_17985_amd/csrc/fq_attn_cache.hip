@@ -349,8 +349,7 @@ template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) v
 
 template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hipStream_t stream)
 {
-    const long long columns = (long long)a.max_q * a.group;
-    const dim3 grid((unsigned)((columns + 16 * tiles - 1) / (16 * tiles) * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
+    const dim3 grid((unsigned)(a.blocks * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
     if (tiles * 16 == WIDE_COLUMNS) {
         const int rc = launch_attn_cache_wide(a, DT, D, batch, stream);
         if (rc) return rc;
@@ -390,7 +389,7 @@ int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int h
     float* stat = part + (splits > 1 ? (size_t)tokens * heads_q * splits * head_dim : 0);
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
                       heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
-                      page_size == 128 ? 7 : 6, table_width, splits, plan.round};
+                      page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.blocks};
     return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, stream);
 }
 

@@ -14,7 +14,14 @@ namespace {
 
 constexpr int WIDE_WAVES = WIDE_COLUMNS / 32, WIDE_THREADS = 64 * WIDE_WAVES;
 
-template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn_cache_wide_kernel(const CacheAttn a)
+// Where piece 2 e + half of row r lies among its row's C: both the eight lanes that write neighbouring pairs' first (or second) pieces and the
+// 16 rows that are read at a time, the same piece of each, then meet all banks.  (Widths of 10 and 12 pieces are only turned for the reads.)
+constexpr int pair_place(int C, int r, int e, int half)
+{
+    return C == 16 ? (e + r) % 8 + 8 * ((half + r / 8) % 2) : C == 8 ? (e + 4 * ((half + r) % 2) + r / 2) % 8 : (2 * e + half + key_turn(C, r)) % C;
+}
+
+template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn_cache_wide_kernel(const CacheAttn a, int batch)
 {
     typedef typename Stored<DT>::type T;
     typedef Mma<FQ_F16> M;
@@ -23,7 +30,9 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     constexpr bool EVEN = CACHE_STEP * D / 16 % WIDE_THREADS == 0;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (KTILE + VTILE)];            // [keys, two stages][values, two stages]
 
-    const int block = blockIdx.x / a.splits, split = blockIdx.x - block * a.splits, h = blockIdx.y, b = blockIdx.z;
+    // workgroups of one sequence and key head on one XCD, those of one share next to each other
+    const PromptPlace at_place = prompt_place(blockIdx.x, (unsigned)(a.blocks * a.splits), (unsigned)(batch * a.heads_kv));
+    const int split = at_place.item / a.blocks, block = at_place.item - split * a.blocks, b = at_place.pair / a.heads_kv, h = at_place.pair - b * a.heads_kv;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
     const int columns = rows.count * a.group, c0 = block * WIDE_COLUMNS;
@@ -88,42 +97,42 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         return Place{a.k_cache + at * page_bytes + (size_t)off * D, a.v_cache + at * page_bytes + off, exists ? scalar(a.k_scale, at) : 0.0f,
                      exists ? scalar(a.v_scale, at) : 0.0f, exists};
     };
-    v4u kreg[PIECES], vreg[PIECES];
-    const auto load_keys = [&](const Place& at) {
+    // What a thread has under way: two tiles of each, those of even and those of odd number.
+    v4u kreg[2][PIECES], vreg[2][PIECES];
+    const uint32_t key_from = 16 * tid, value_from = tid / 4 * a.page + 16 * (tid % 4);
+    const auto load_keys = [&](const Place& at, v4u (&reg)[PIECES]) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid;
-            if (EVEN || i < CACHE_STEP * D / 16) kreg[p] = *reinterpret_cast<const v4u*>(at.keys + 16 * i);
+            if (EVEN || p * WIDE_THREADS + tid < CACHE_STEP * D / 16) reg[p] = *reinterpret_cast<const v4u*>(at.keys + p * 16 * WIDE_THREADS + key_from);
         }
     };
-    const auto load_values = [&](const Place& at) {
+    const auto load_values = [&](const Place& at, v4u (&reg)[PIECES]) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid;
-            if (EVEN || i < 4 * D) vreg[p] = *reinterpret_cast<const v4u*>(at.values + (i / 4) * a.page + 16 * (i % 4));
+            if (EVEN || p * WIDE_THREADS + tid < 4 * D) reg[p] = *reinterpret_cast<const v4u*>(at.values + p * (WIDE_THREADS / 4) * a.page + value_from);
         }
     };
-    // rows of keys as in the prompt's kernel; a row of values holds the 64 keys of a dimension, of each 16 first 0..3, 8..11, then 4..7, 12..15:
-    // what a lane of either half needs for a product lies together
-    const auto put_keys = [&](int stage) {
+    // A row of keys holds 16-byte pieces of the head's elements; a row of values the 64 keys of a dimension, of each 16 first 0..3, 8..11, then
+    // 4..7, 12..15: what a lane of either half needs for a product lies together.  A thread writes two neighbouring pieces.
+    const auto put_keys = [&](int stage, const v4u (&reg)[PIECES]) {
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid, r = i / (D / 16), piece = 2 * (i - r * (D / 16)), turn = key_turn(C, r);
+            const int i = p * WIDE_THREADS + tid, r = i / (D / 16), e = i - r * (D / 16);
             if (!EVEN && i >= CACHE_STEP * D / 16) continue;
             uint8_t* row = lds + stage * KTILE + r * ROW;
-            *reinterpret_cast<v8h*>(row + (piece + turn) % C * 16) = widen8(kreg[p][0], kreg[p][1]);
-            *reinterpret_cast<v8h*>(row + (piece + 1 + turn) % C * 16) = widen8(kreg[p][2], kreg[p][3]);
+            *reinterpret_cast<v8h*>(row + pair_place(C, r, e, 0) * 16) = widen8(reg[p][0], reg[p][1]);
+            *reinterpret_cast<v8h*>(row + pair_place(C, r, e, 1) * 16) = widen8(reg[p][2], reg[p][3]);
         }
     };
-    const auto put_values = [&](int stage) {
+    const auto put_values = [&](int stage, const v4u (&reg)[PIECES]) {
         const _Float16 off = (_Float16)WIDEN_BIAS;
 #pragma unroll
         for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid, d = i / 4, piece = 2 * (i % 4), turn = key_turn(8, d);
+            const int i = p * WIDE_THREADS + tid, d = i / 4, e = i % 4;
             if (!EVEN && i >= 4 * D) continue;
             uint8_t* row = lds + 2 * KTILE + stage * VTILE + d * VROW;
-            *reinterpret_cast<v8h*>(row + (piece + turn) % 8 * 16) = widen8(vreg[p][0], vreg[p][2]) - off;
-            *reinterpret_cast<v8h*>(row + (piece + 1 + turn) % 8 * 16) = widen8(vreg[p][1], vreg[p][3]) - off;
+            *reinterpret_cast<v8h*>(row + pair_place(8, d, e, 0) * 16) = widen8(reg[p][0], reg[p][2]) - off;
+            *reinterpret_cast<v8h*>(row + pair_place(8, d, e, 1) * 16) = widen8(reg[p][1], reg[p][3]) - off;
         }
     };
 
@@ -137,13 +146,13 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
     uint32_t key_at[KS], value_at[4];
 #pragma unroll
-    for (int e = 0; e < KS; ++e) key_at[e] = col * ROW + (2 * e + half + key_turn(C, col)) % C * 16;
+    for (int e = 0; e < KS; ++e) key_at[e] = col * ROW + pair_place(C, col, e, half) * 16;
 #pragma unroll
-    for (int n = 0; n < 4; ++n) value_at[n] = 2 * KTILE + col * VROW + (2 * n + half + key_turn(8, col)) % 8 * 16;
+    for (int n = 0; n < 4; ++n) value_at[n] = 2 * KTILE + col * VROW + pair_place(8, col, n, half) * 16;
 
     // O^T += V^T P of a tile (PV), then S^T of the next (QK); first operands come from LDS AHEAD - 1 products early, the order is kept
     const auto products = [&](auto with_pv, auto with_qk) {
-        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 5;
+        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 4;
         v8h ring[AHEAD];
         const auto fetch = [&](int n) {
             const uint32_t at = n < PV ? value_at[n / VT] + 32 * (n % VT) * VROW : key_at[(n - PV) / 2] + 32 * ((n - PV) % 2) * ROW;
@@ -214,66 +223,74 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         sum += add / part;
     };
 
-    // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), the next is asked for, PV of tile i, QK and softmax of i + 1
+    // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), more is asked for (keys of i + 4, values of i + 3), PV of
+    // tile i, QK and softmax of i + 1
     if (tiles > 0) {
-        Place next = place(0, page_of(0)), after = place(1, page_of(1)), later = place(2, page_of(2));      // tiles i + 1, i + 2, i + 3
-        load_keys(next);
-        load_values(next);
-        put_keys(0);
-        put_values(0);
-        load_keys(after);
-        load_values(after);
-        put_keys(1);
-        load_keys(later);
-        int page_then = page_of(3);
+        Place now = place(0, page_of(0)), line[3] = {place(1, page_of(1)), place(2, page_of(2)), place(3, page_of(3))};      // line: tiles i + 1 .. i + 3
+        load_keys(now, kreg[0]);
+        load_values(now, vreg[0]);
+        load_keys(line[0], kreg[1]);
+        put_keys(0, kreg[0]);
+        load_keys(line[1], kreg[0]);
+        put_values(0, vreg[0]);
+        load_values(line[0], vreg[1]);
+        load_values(line[1], vreg[0]);
+        put_keys(1, kreg[1]);
+        load_keys(line[2], kreg[1]);
+        Place fourth = place(4, page_of(4));
+        int page_then = page_of(5);
         __syncthreads();
         if (own > 0) {
             products(no, yes);
-            softmax(0, next);
+            softmax(0, now);
         }
-        next = after;
-        after = later;
-        later = place(3, page_then);
-        page_then = page_of(4);
         __syncthreads();
-        int i = 0, key_move = KTILE, value_move = VTILE;
+        int i = 0;
 #pragma unroll
         for (int e = 0; e < KS; ++e) key_at[e] += KTILE;
-        const auto begin_step = [&] {
-            put_keys(i % 2);
-            put_values((i + 1) % 2);
-            load_keys(later);
-            load_values(after);
+        const auto begin_step = [&](auto odd) {
+            constexpr int O = decltype(odd)::value;
+            put_keys(O, kreg[O]);
+            put_values(1 - O, vreg[1 - O]);
+            load_keys(fourth, kreg[O]);
+            load_values(line[2], vreg[1 - O]);
         };
         const auto end_step = [&] {
-            next = after;
-            after = later;
-            later = place(i + 4, page_then);
-            page_then = page_of(i + 5);
+            line[0] = line[1];
+            line[1] = line[2];
+            line[2] = fourth;
+            fourth = place(i + 5, page_then);
+            page_then = page_of(i + 6);
             ++i;
             __syncthreads();
         };
-        while (i + 1 < own) {
-            begin_step();
+        const auto step = [&](auto odd) {
+            constexpr int O = decltype(odd)::value;
+            begin_step(odd);
             __builtin_amdgcn_s_setprio(1);
             products(yes, yes);
             __builtin_amdgcn_s_setprio(0);
-            softmax(i + 1, next);
+            softmax(i + 1, line[0]);
 #pragma unroll
-            for (int e = 0; e < KS; ++e) key_at[e] -= key_move;
+            for (int e = 0; e < KS; ++e) key_at[e] += O ? KTILE : -KTILE;
 #pragma unroll
-            for (int n = 0; n < 4; ++n) value_at[n] += value_move;
-            key_move = -key_move;
-            value_move = -value_move;
+            for (int n = 0; n < 4; ++n) value_at[n] += O ? -VTILE : VTILE;
             end_step();
+        };
+        while (i + 2 < own) {
+            step(no);
+            step(yes);
         }
+        if (i + 1 < own) step(no);
         if (own > 0) {
-            begin_step();
+            if (i % 2) begin_step(yes);
+            else begin_step(no);
             products(yes, no);
             end_step();
         }
         while (i < tiles) {
-            begin_step();
+            if (i % 2) begin_step(yes);
+            else begin_step(no);
             end_step();
         }
     }
@@ -312,13 +329,12 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
 template <int DT> int launch(const CacheAttn& a, int head_dim, int batch, hipStream_t stream)
 {
-    const long long columns = (long long)a.max_q * a.group;
-    const dim3 grid((unsigned)((columns + WIDE_COLUMNS - 1) / WIDE_COLUMNS * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
+    const unsigned grid = (unsigned)((long long)batch * a.heads_kv * a.blocks * a.splits);
     switch (head_dim) {
-    case 64: attn_cache_wide_kernel<DT, 64><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
-    case 80: attn_cache_wide_kernel<DT, 80><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
-    case 96: attn_cache_wide_kernel<DT, 96><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
-    default: attn_cache_wide_kernel<DT, 128><<<grid, WIDE_THREADS, 0, stream>>>(a); break;
+    case 64: attn_cache_wide_kernel<DT, 64><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
+    case 80: attn_cache_wide_kernel<DT, 80><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
+    case 96: attn_cache_wide_kernel<DT, 96><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
+    default: attn_cache_wide_kernel<DT, 128><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));

@@ -65,18 +65,25 @@ FQ_BOTH int visible_keys(int keys, int n, int i)
 // columns) each step together.
 constexpr int MAX_SPLITS = 256, CACHE_CUS = 256, WIDE_COLUMNS = 128;
 struct CachePlan {
-    int tiles, round, splits;
+    int tiles, round, splits, blocks;      // blocks of columns
 };
 inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int heads_kv)
 {
     const long long columns = (long long)max_q * (heads_q / heads_kv);
     const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : WIDE_COLUMNS / 16;
     const bool wide = tiles > 2;
-    const long long wgs = (long long)batch * heads_kv * ((columns + 16 * tiles - 1) / (16 * tiles));
+    const long long blocks = (columns + 16 * tiles - 1) / (16 * tiles), wgs = (long long)batch * heads_kv * blocks;
     const int round = wide ? 1 : wgs <= CACHE_CUS ? 8 : 4;
     const long long rounds = ((long long)max_len + CACHE_STEP * round - 1) / (CACHE_STEP * round);
     const long long splits = std::min({wide ? rounds / 4 : rounds, (wide ? 2 * CACHE_CUS : CACHE_CUS) / wgs, (long long)MAX_SPLITS});
-    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1};
+    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, (int)blocks};
+}
+
+// Whether the launches hold it: the kernel for many columns has all its workgroups along x, the join the query tokens along y.
+inline bool cache_holds(const CachePlan& p, int batch, int max_q, int heads_kv)
+{
+    const long long along_x = (long long)p.blocks * p.splits * (p.tiles > 2 ? (long long)batch * heads_kv : 1);
+    return along_x < (1LL << 31) && along_x * 512 < (1LL << 32) && (p.splits == 1 || max_q <= 65535);
 }
 
 // Keys of one share when `keys` are dealt over `splits` workgroups: whole rounds, so that the last shares may be empty.

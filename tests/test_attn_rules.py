@@ -32,7 +32,7 @@ extern "C" int used(int keys, int share) { return shares_used(keys, share); }
 extern "C" void plan(int batch, int max_q, int max_len, int heads_q, int heads_kv, int* out)
 {
     const CachePlan p = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
-    out[0] = p.tiles; out[1] = p.round; out[2] = p.splits;
+    out[0] = p.tiles; out[1] = p.round; out[2] = p.splits; out[3] = p.blocks; out[4] = cache_holds(p, batch, max_q, heads_kv);
 }
 extern "C" void place(unsigned id, unsigned items, unsigned pairs, unsigned* out)
 {
@@ -129,7 +129,7 @@ def test_shares_cover_all_keys_in_whole_steps(rules, waves):
 
 
 def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
-    out = (ctypes.c_int * 3)()
+    out = (ctypes.c_int * 5)()
     for batch in (1, 4, 64, 65535):
         for max_q in (1, 5, 512, 65472):
             for max_len in (1, 256, 257, 8192, 2**30):
@@ -137,13 +137,14 @@ def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
                     if max_q * hq >= 2**30:
                         continue
                     rules.plan(batch, max_q, max_len, hq, hkv, out)
-                    tiles, rnd, splits = out
+                    tiles, rnd, splits, blocks, holds = out
+                    assert blocks == -(-max_q * (hq // hkv) // (16 * tiles))
                     columns = max_q * (hq // hkv)
                     wgs = batch * hkv * -(-columns // (16 * tiles))
                     assert tiles in (1, 2, 8) and (tiles == 8 or columns <= 16 * tiles) and rnd == (1 if tiles == 8 else 8 if wgs <= 256 else 4)
                     assert 1 <= splits <= 256 and (splits - 1) * 64 * rnd < max_len
                     assert splits == 1 or wgs * splits <= (512 if tiles == 8 else 256)
-                    assert -(-columns // (16 * tiles)) * splits * 512 < 2**32 and (splits == 1 or max_q <= 65535)
+                    assert holds == (blocks * splits * (batch * hkv if tiles == 8 else 1) * 512 < 2**32) and (splits == 1 or max_q <= 65535)
 
 
 @pytest.mark.parametrize("items,pairs", [(1, 1), (1, 7), (3, 8), (5, 9), (16, 23), (2, 64), (7, 1), (64, 3)])
