@@ -141,6 +141,20 @@ def _dtype_code(t) -> int:
 _raw_stream = None
 
 
+def _stream_on(stream, device) -> int:
+    """_stream for callers that have the current device in hand."""
+    if stream is not None:
+        return getattr(stream, "cuda_stream", stream)
+    global _raw_stream_of
+    if _raw_stream_of is None:
+        torch = _torch()
+        _raw_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream_of(device)
+
+
+_raw_stream_of = None
+
+
 def _stream(stream) -> int:
     """Raw handle of a stream, or of the current device's current stream.  The latter is read without building a
     torch.cuda.Stream object where torch offers that: about 2 us of a small call's 13."""
@@ -484,7 +498,7 @@ def _packed(t, name, here, shape=None, dtype=None):
 
 def _array(t, name, here, dtype, shape):
     """Address of a contiguous tensor of that type and shape on device `here`."""
-    if t.dtype != dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the current device, cuda:{here}; it is {t.dtype}, "
                          f"{tuple(t.shape)}, on {t.device}")
     return t.data_ptr()
@@ -535,10 +549,10 @@ def fq_kv_append(Q, K, V, cu_new, past, max_new: int, k_cache, v_cache, k_scale,
         if rope_cos.dim() != 2:
             raise ValueError("rope_cos is [positions, rope_dim / 2]")
         rows, half = rope_cos.shape
-        cos, sin = (_array(x, name, here, torch.float32, (rows, half)) for x, name in ((rope_cos, "rope_cos"), (rope_sin, "rope_sin")))
+        cos, sin = _array(rope_cos, "rope_cos", here, torch.float32, (rows, half)), _array(rope_sin, "rope_sin", here, torch.float32, (rows, half))
     rc = (_lib or lib()).fq_kv_append(q, K.data_ptr(), V.data_ptr(), _dtype_code(K), tokens, heads_q, heads_kv, dim, ldq, ldk, ldv,
                                       _array(cu_new, "cu_new", here, torch.int32, (batch + 1,)), _array(past, "past", here, torch.int32, (batch,)), batch, max_new,
-                                      cos, sin, rows, 2 * half, 1 if interleaved else 0, q_out, ldqo, k_out, ldko, *cache, _stream(stream))
+                                      cos, sin, rows, 2 * half, 1 if interleaved else 0, q_out, ldqo, k_out, ldko, *cache, _stream_on(stream, here))
     if rc:
         _check(rc)
 
@@ -561,7 +575,7 @@ def fq_attn_cache(Q, cu_q, lens, max_q: int, max_len: int, k_cache, v_cache, k_s
         raise ValueError(f"workspace must be contiguous and on the current device, cuda:{here}")
     rc = (_lib or lib()).fq_attn_cache(Q.data_ptr(), _dtype_code(Q), tokens, heads_q, heads_kv, dim, ldq, _array(cu_q, "cu_q", here, torch.int32, (batch + 1,)),
                                        _array(lens, "lens", here, torch.int32, (batch,)), batch, max_q, max_len, *cache, scale, Y.data_ptr(), ldy,
-                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(stream))
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_on(stream, here))
     if rc:
         _check(rc)
 
@@ -581,6 +595,6 @@ def fq_attn_prompt(Q, K, V, cu_q, cu_k, max_q: int, scale: float, Y, causal: boo
     batch = cu_q.numel() - 1
     rc = (_lib or lib()).fq_attn_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), tokens_q, tokens_k, heads_q, heads_kv, dim, ldq, ldk, ldv,
                                         _array(cu_q, "cu_q", here, torch.int32, (batch + 1,)), _array(cu_k, "cu_k", here, torch.int32, (batch + 1,)), batch, max_q,
-                                        1 if causal else 0, scale, Y.data_ptr(), ldy, _stream(stream))
+                                        1 if causal else 0, scale, Y.data_ptr(), ldy, _stream_on(stream, here))
     if rc:
         _check(rc)

@@ -23,8 +23,8 @@ int check_packed(const char* what, const void* p, int dtype, int tokens, int hea
 {
     if (tokens < 0) return fail(FQ_ERR_SHAPE, "%s: %d tokens", what, tokens);
     if (ld < (long long)heads * head_dim) return fail(FQ_ERR_SHAPE, "%s: token stride %lld < %d heads of %d", what, ld, heads, head_dim);
-    if (ld > (1LL << 40) || ld * elem_size(dtype) % 16 != 0)
-        return fail(FQ_ERR_SHAPE, "%s: token stride of %lld elements is not a multiple of 16 bytes (or is beyond 2^40)", what, ld);
+    if (ld > MAX_TOKEN_STRIDE) return fail(FQ_ERR_RANGE, "%s: token stride of %lld elements, at most 2^22", what, ld);
+    if (ld * elem_size(dtype) % 16 != 0) return fail(FQ_ERR_SHAPE, "%s: token stride of %lld elements is not a multiple of 16 bytes", what, ld);
     if (tokens == 0) return FQ_OK;
     if (!p) return fail(FQ_ERR_NULL, "%s is NULL", what);
     if (!aligned16(p)) return fail(FQ_ERR_ALIGN, "%s is not 16-byte aligned", what);
@@ -98,8 +98,8 @@ int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int t
         if (!aligned16(rope_cos) || !aligned16(rope_sin)) return fail(FQ_ERR_ALIGN, "rope_cos or rope_sin is not 16-byte aligned");
         if (rope_rows <= 0) return fail(FQ_ERR_SHAPE, "rope_rows = %d must be positive", rope_rows);
     }
-    const long long places = batch * pages_touched(max_new, page_size);
-    if (places >= (1LL << 31) || !launch_holds(places, 4 * page_size))
+    const long long places = batch * pages_touched(max_new, page_size) * ((Q_out ? 3 : 2) * heads_kv);
+    if (!launch_holds(places, append_plan(max_new, page_size, head_dim).threads))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d new tokens are more than one launch holds", batch, max_new);
     if (tokens == 0) return FQ_OK;
     return launch_kv_append(Q, K, V, x_dtype, tokens, heads_q, heads_kv, head_dim, ldq, ldk, ldv, cu_new, past, batch, max_new, rope_cos, rope_sin,
@@ -159,7 +159,6 @@ int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int
     if (!rc) rc = check_indices("cu_q", cu_q);
     if (!rc) rc = check_indices("cu_k", cu_k);
     if (rc) return rc;
-    if (ldk > (1 << 24) || ldv > (1 << 24)) return fail(FQ_ERR_RANGE, "token strides of %lld and %lld elements for K and V: at most 2^24", ldk, ldv);
     const long long places = (long long)batch * heads_q * prompt_tiles(max_q);
     if (places >= (1LL << 31) || !launch_holds(places, PROMPT_THREADS))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);

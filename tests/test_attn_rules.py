@@ -25,6 +25,11 @@ extern "C" void fill(int first, int count, int past, int j, int page, int capaci
     out[0] = f.index; out[1] = f.slot0; out[2] = f.slot1; out[3] = f.row; out[4] = f.pos;
 }
 extern "C" long long touched(int tokens, int page) { return pages_touched(tokens, page); }
+extern "C" int append(int max_new, int page, int dim)
+{
+    const AppendPlan p = append_plan(max_new, page, dim);
+    return p.few ? p.threads : -p.threads;
+}
 extern "C" int keys(int len, int max_len, int capacity) { return cached_keys(len, max_len, capacity); }
 extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i); }
 extern "C" int share(int keys, int splits, int round) { return share_keys(keys, splits, round); }
@@ -166,3 +171,14 @@ def test_prompt_places_of_a_launch_of_2_to_the_31_workgroups(rules):
         for i in (0, 7, items * pairs // 2, items * pairs - 1):
             rules.place(i, items, pairs, out)
             assert out[0] < pairs and out[1] < items
+
+
+@pytest.mark.parametrize("page", [64, 128])
+@pytest.mark.parametrize("dim", [64, 80, 96, 128])
+def test_append_threads_hold_what_a_call_adds_to_a_page(rules, page, dim):
+    for new in (1, 2, 4, 5, 16, 17, 32, 33, 63, 64, 65, 1000, HI):
+        threads, pieces = rules.append(new, page, dim), min(new, page) * dim // 8
+        few = threads > 0
+        threads = abs(threads)
+        assert threads % 64 == 0 and 64 <= threads <= 512 and pieces <= threads * (1 if few else -(-dim // 8 // 4))
+        assert few == (pieces <= 512)
