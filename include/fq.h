@@ -399,7 +399,7 @@ int fq_gemm_select(int variant);
  *   cu[b] .. cu[b + 1] - 1 (cu int32 [batch + 1], device, ascending from 0); rows behind the last sequence are left as they were.
  * Cache: pages of page_size (64 or 128) tokens, 8-bit codes with one scale for each page and head,
  *   k_cache [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size] (transposed within a page:
- *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv]; an element is code * scale.
+ *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv], finite and not negative; an element is code * scale.
  *   page_table int32 [batch, table_width], device: token t of sequence b lies in page page_table[b, t / page_size], slot
  *   t % page_size.  table_width * page_size <= 2^30.  Nothing has to be cleared before use: a page's first token starts it anew.
  * Values on the device cannot be checked when the call is made; the kernels use them within bounds: offsets are clamped to
@@ -423,10 +423,12 @@ int fq_gemm_select(int variant);
  *
  * fq_attn_cache — Y[i] = softmax(scale * Q[i] K^T) V over the cache: with n query tokens of sequence b and lens[b] tokens in the
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
- *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32, probabilities enter the second
- *   product as fp16.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they,
+ *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider, probabilities enter the second
+ *   product as fp16; with up to 32 columns (query tokens times heads of a group) queries enter the first as integers of 1 / 16256 of their
+ *   head's largest magnitude.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they,
  *   not the lengths on the device, set the launch, so a captured call may be replayed with other lengths within them.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
+ *   Calls that overlap (different streams) need a workspace each; calls and graphs that follow one another may share one.
  *   Y may be Q itself (same address and stride), else it must not overlap the inputs.
  *
  * fq_attn_prompt — the same over packed K and V: query i of n sees keys 0 .. m - n + i of the sequence's m (causal != 0), or all

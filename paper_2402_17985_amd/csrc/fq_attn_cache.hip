@@ -32,6 +32,21 @@ __device__ __forceinline__ float over_groups_sum(float v)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// The sequence of the z-th workgroups, at most 64 of them, by length: longest first, as long ones begun last would run on alone; or, where all
+// workgroups are on the device at once, two to a CU, the longer half so and then the shorter half, shortest first: the second of a CU's is then as
+// short as the first is long.  (64 sequences of 160 to 8192 tokens, 64 heads over 8: 124 us as they come, 106 so.)
+__device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
+{
+    const int lane = threadIdx.x % 64, mine = a.lens[min(lane, batch - 1)], half = (batch + 1) / 2;
+    const int nth = a.order == CACHE_FOLDED && z >= half ? batch - 1 - (z - half) : z;
+    int longer = 0;
+    for (int i = 0; i < batch; ++i) {
+        const int other = __builtin_amdgcn_readlane(mine, i);
+        longer += other > mine || (other == mine && i < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < batch && longer == nth));
+}
+
 // NT tiles of 16 columns.  Grid: x the splits of all column tiles, y the key heads, z the sequences.
 template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(const CacheAttn a)
 {
@@ -41,7 +56,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     __shared__ float gathered[WAVES][16][ROW];
     __shared__ float tops[WAVES][16 * NT], sums[WAVES][16 * NT];
 
-    const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, h = blockIdx.y, b = blockIdx.z;
+    const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, h = blockIdx.y;
+    const int b = a.order != CACHE_AS_GIVEN ? by_length(a, blockIdx.z, gridDim.z) : (int)blockIdx.z;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 16, g = lane / 16;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
     const int columns = rows.count * a.group, c0 = tile * 16 * NT;
@@ -389,7 +405,7 @@ int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int h
     float* stat = part + (splits > 1 ? (size_t)tokens * heads_q * splits * head_dim : 0);
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
                       heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
-                      page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.blocks};
+                      page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.blocks, plan.order};
     return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, stream);
 }
 

@@ -6,7 +6,8 @@
 //   its keys' scale goes into the factor of the scores; the keys stay 1152 too large each (see widen8), which adds 1152 times the sum of
 //     the query's elements to every score of a column and is taken off where the maximum is;
 //   its values' scale goes into P, relative to that of the tiles accumulated so far, as an addend of the exponent; where the two are
-//     more than a factor 64 apart the accumulators change to the new one first, so that fp16 holds every P.
+//     more than a factor 64 apart the accumulators change to the new one first, so that fp16 holds every P.  (Not to one 2^60 times smaller:
+//     what the accumulators hold then outweighs the tile, or is below 2^-25 of its own values, fp16's smallest P.)
 #include "fq_attn_cache.h"
 
 namespace fq {
@@ -201,15 +202,15 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 #pragma unroll
             for (int t = 0; t < VT; ++t) o[t] *= keep;
         }
-        if (at.v_scale > 0.0f && !(at.v_scale <= 64.0f * unit && at.v_scale >= unit * (1.0f / 64))) {
+        if (at.v_scale > 64.0f * unit || (at.v_scale < unit * 0x1p-6f && at.v_scale >= unit * 0x1p-60f && at.v_scale > 0.0f)) {
             asm volatile("");
             const float change = unit / at.v_scale;
             unit = at.v_scale;
 #pragma unroll
             for (int t = 0; t < VT; ++t) o[t] *= change;
         }
-        // values of scale 0: probabilities too small for fp16, whose sum still counts
-        const float part = at.v_scale > 0.0f ? at.v_scale / unit : 0x1p-60f;
+        // far below the unit (or 0): probabilities too small for fp16, whose sum still counts
+        const float part = at.v_scale > 0.0f ? fmaxf(at.v_scale / unit, 0x1p-60f) : 0x1p-60f;
         const float off = (top == -INFINITY ? 0.0f : top) + shift - __builtin_amdgcn_logf(part);
         float add = 0.0f;
 #pragma unroll

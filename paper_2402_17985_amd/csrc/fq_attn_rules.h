@@ -79,8 +79,9 @@ FQ_BOTH int visible_keys(int keys, int n, int i)
 // sequence and key head, and of its keys all or one of `splits` shares, `round` steps at a time: its waves take the steps of a round in turn, or (many
 // columns) each step together.
 constexpr int MAX_SPLITS = 256, CACHE_CUS = 256, WIDE_COLUMNS = 128;
+enum CacheOrder { CACHE_AS_GIVEN, CACHE_LONGEST_FIRST, CACHE_FOLDED };
 struct CachePlan {
-    int tiles, round, splits, blocks;      // blocks of columns
+    int tiles, round, splits, blocks, order;      // blocks of columns; order of the sequences
 };
 inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int heads_kv)
 {
@@ -91,7 +92,9 @@ inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int 
     const int round = wide ? 1 : wgs <= CACHE_CUS ? 8 : 4;
     const long long rounds = ((long long)max_len + CACHE_STEP * round - 1) / (CACHE_STEP * round);
     const long long splits = std::min({wide ? rounds / 4 : rounds, (wide ? 2 * CACHE_CUS : CACHE_CUS) / wgs, (long long)MAX_SPLITS});
-    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, (int)blocks};
+    // ordering them costs each workgroup about 0.4 us, too much for short ones
+    const int order = wide || batch == 1 || batch > 64 || wgs <= CACHE_CUS || max_len < 1024 ? CACHE_AS_GIVEN : wgs <= 2 * CACHE_CUS ? CACHE_FOLDED : CACHE_LONGEST_FIRST;
+    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, (int)blocks, order};
 }
 
 // Whether the launches hold it: the kernel for many columns has all its workgroups along x, the join the query tokens along y.

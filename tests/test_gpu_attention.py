@@ -166,9 +166,18 @@ def test_cache_attention_split_over_the_keys(x, dim, page, heads, lens, queries)
     _cache_both(rng, x, dim, page, *heads, lens, queries, max_len=60000)     # a bound far above the lengths
 
 
-@pytest.mark.parametrize("spread", [1.0, 12.0])
+@pytest.mark.parametrize("batch,heads", [(64, 5), (33, 12), (9, 64), (64, 16)])
+def test_cache_attention_of_many_uneven_sequences(batch, heads):
+    """Enough work for an order by length: longest first, or folded (at most two workgroups per CU)."""
+    rng = np.random.default_rng(batch)
+    lens = [int(n) for n in rng.integers(0, 200, batch)]
+    lens[batch // 2], lens[0] = 200, 200
+    _cache_both(rng, "bf16", 64, 64, heads, heads, lens, [1] * batch, max_len=1024)
+
+
+@pytest.mark.parametrize("spread", [1.0, 12.0, 30.0])
 def test_cache_attention_of_many_columns_over_pages_of_very_different_scales(spread):
-    """Values' scales up to a factor e^24 apart between neighbouring pages, and pages of zeros."""
+    """Values' scales up to a factor e^60 apart between neighbouring pages, and pages of zeros."""
     rng, real = np.random.default_rng(9), U.filled_cache
     def filled(*shape):
         k, v, ks, vs = real(*shape)
@@ -223,6 +232,16 @@ def test_prompt_attention(x, dim, causal, lens):
 @pytest.mark.parametrize("causal", [True, False])
 def test_prompt_attention_of_some_queries_and_rows_without_keys(queries, keys, causal):
     _prompt_both(np.random.default_rng(sum(keys)), "bf16", 128, 6, 2, queries, keys, causal)
+
+
+@pytest.mark.parametrize("batch", [64, 65, 130])
+def test_prompt_attention_of_many_sequences(batch):
+    """Up to 64 go by their length, more as they come."""
+    rng = np.random.default_rng(batch)
+    lens = [int(n) for n in rng.integers(0, 50, batch)]
+    lens[batch // 3] = 150
+    _prompt_both(rng, "bf16", 64, 3, 1, lens, lens, True)
+    _prompt_both(rng, "f16", 64, 1, 1, [n // 2 for n in lens], lens, False)
 
 
 @pytest.mark.parametrize("heads", [(1, 1), (7, 1), (5, 5), (16, 8)])
