@@ -142,7 +142,8 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     for (int t = 0; t < VT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
-    float top = -INFINITY, sum = 0.0f, unit = 0.0f;      // of the scaled scores; over this lane's keys; values' scale that o counts in
+    float top = -INFINITY, sum = 0.0f;                   // of the scaled scores; over this lane's keys
+    float unit = 0.0f, per_unit = 0.0f;                  // values' scale that o counts in
     v8h p[4];                                            // 16 keys each
 
     uint32_t key_at[KS], value_at[4];
@@ -152,11 +153,12 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     for (int n = 0; n < 4; ++n) value_at[n] = 2 * KTILE + col * VROW + pair_place(8, col, n, half) * 16;
 
     // O^T += V^T P of a tile (PV), then S^T of the next (QK); first operands come from LDS AHEAD - 1 products early, the order is kept
-    const auto products = [&](auto with_pv, auto with_qk) {
+    const auto products = [&](auto with_pv, auto with_qk, auto odd) {      // odd: whether the values' tile has an odd number
+        constexpr int VSTAGE = decltype(odd)::value, KSTAGE = 1 - VSTAGE;
         constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 4;
         v8h ring[AHEAD];
         const auto fetch = [&](int n) {
-            const uint32_t at = n < PV ? value_at[n / VT] + 32 * (n % VT) * VROW : key_at[(n - PV) / 2] + 32 * ((n - PV) % 2) * ROW;
+            const uint32_t at = n < PV ? value_at[n / VT] + VSTAGE * VTILE + 32 * (n % VT) * VROW : key_at[(n - PV) / 2] + KSTAGE * KTILE + 32 * ((n - PV) % 2) * ROW;
             ring[n % AHEAD] = *reinterpret_cast<const v8h*>(lds + at);
         };
 #pragma unroll
@@ -206,11 +208,12 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
             asm volatile("");
             const float change = unit / at.v_scale;
             unit = at.v_scale;
+            per_unit = 1.0f / unit;
 #pragma unroll
             for (int t = 0; t < VT; ++t) o[t] *= change;
         }
         // far below the unit (or 0): probabilities too small for fp16, whose sum still counts
-        const float part = at.v_scale > 0.0f ? fmaxf(at.v_scale / unit, 0x1p-60f) : 0x1p-60f;
+        const float part = fmaxf(at.v_scale * per_unit, 0x1p-60f);
         const float off = (top == -INFINITY ? 0.0f : top) + shift - __builtin_amdgcn_logf(part);
         float add = 0.0f;
 #pragma unroll
@@ -221,7 +224,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
                 add += w;
                 p[2 * t + e / 8][e % 8] = (_Float16)w;
             }
-        sum += add / part;
+        sum = __builtin_fmaf(add, __builtin_amdgcn_rcpf(part), sum);
     };
 
     // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), more is asked for (keys of i + 4, values of i + 3), PV of
@@ -242,13 +245,11 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         int page_then = page_of(5);
         __syncthreads();
         if (own > 0) {
-            products(no, yes);
+            products(no, yes, yes);
             softmax(0, now);
         }
         __syncthreads();
         int i = 0;
-#pragma unroll
-        for (int e = 0; e < KS; ++e) key_at[e] += KTILE;
         const auto begin_step = [&](auto odd) {
             constexpr int O = decltype(odd)::value;
             put_keys(O, kreg[O]);
@@ -266,16 +267,11 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
             __syncthreads();
         };
         const auto step = [&](auto odd) {
-            constexpr int O = decltype(odd)::value;
             begin_step(odd);
             __builtin_amdgcn_s_setprio(1);
-            products(yes, yes);
+            products(yes, yes, odd);
             __builtin_amdgcn_s_setprio(0);
             softmax(i + 1, line[0]);
-#pragma unroll
-            for (int e = 0; e < KS; ++e) key_at[e] += O ? KTILE : -KTILE;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) value_at[n] += O ? -VTILE : VTILE;
             end_step();
         };
         while (i + 2 < own) {
@@ -284,9 +280,13 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         }
         if (i + 1 < own) step(no);
         if (own > 0) {
-            if (i % 2) begin_step(yes);
-            else begin_step(no);
-            products(yes, no);
+            if (i % 2) {
+                begin_step(yes);
+                products(yes, no, yes);
+            } else {
+                begin_step(no);
+                products(yes, no, no);
+            }
             end_step();
         }
         while (i < tiles) {

@@ -69,7 +69,7 @@ __device__ __forceinline__ PromptSequence nth_sequence(const PromptAttn& a, int 
             {__builtin_amdgcn_readlane(k.first, from), __builtin_amdgcn_readlane(k.count, from)}};
 }
 
-template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, 2) void attn_prompt_kernel(const PromptAttn a)
+template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 4 : D <= 96 ? 3 : 2) void attn_prompt_kernel(const PromptAttn a)
 {
     typedef Mma<DT> M;
     typedef typename M::T T;
@@ -152,7 +152,7 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, 2) void at
     // AHEAD - 1 products early; the order is kept as written.  (Left to the compiler, each pair of transposed reads is awaited before the
     // next: 5.9e8 busy CU cycles for a causal prompt of 8192 tokens and 64 heads of 128, so 4.5e8.)
     const auto products = [&](auto with_pv, auto with_qk) {
-        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 5;
+        constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = D == 64 ? 4 : 5;
         v8 ring[AHEAD];
         const auto fetch = [&](int n) {
             if (n < PV) {
