@@ -2,15 +2,22 @@
 //
 // The reduction is bound by the cache's bytes: a key and a value byte serve at most the few queries of their group, so the
 // kernel is a stream from HBM into registers, and everything else has to fit beside it.  What a wave does with 64 keys:
-//   S^T = K Q^T   16 keys x 16 columns a product (a column is one query token of one head of the group), 32 elements of the
-//                 head deep.  The 8-bit codes become fp16 exactly; the queries are fp16 too (bf16 ones are brought into its
-//                 range by a power of two per column, which goes back in with the scale).
+//   S^T = K Q^T   16 keys x 16 columns a product (a column is one query token of one head of the group), 64 elements of the head deep, in
+//                 8-bit integers: the codes go into the matrix instruction as they come.  The queries are integers of up to 127 * 128 steps,
+//                 two limbs, so that each product is done twice; the sums are exact.  (Codes widened to fp16 take five instructions
+//                 for four of them: a step of 64 keys is 440 vector instructions so, 700 that way.)
 //   softmax       running maximum and sum per column.  The product leaves a column's 64 scores in four lanes, 16 each.
-//   O^T += V^T P  16 dimensions x 16 columns, 32 keys deep, P rounded to fp16 (values in [0, 1]: half a step is 2^-12, below
-//                 what the 2-byte output keeps).  A step's keys lie in one page, whose scale multiplies its product in 32 bits.
+//   O^T += V^T P  16 dimensions x 16 columns, 32 keys deep, P rounded to fp16: half a step is 2^-11 of each, what an fp16 output is
+//                 rounded by too.  The sum that divides is that of the rounded ones.  A step's keys lie in one page, whose scale multiplies
+//                 its product in 32 bits.
 // No operand passes through LDS: which key of the page stands in which row of the first product is free, and with key
 // 16 (r / 4) + 4 t + r % 4 in row r of tile t a lane's scores are those of 16 consecutive keys, the very ones whose values it
 // reads as 16 consecutive bytes of a dimension (the cache holds values transposed for that) in the second product.
+// Each wave has a step of keys and values under way while it works on the one before, 16 KiB for heads of 128; eight waves a CU, in one workgroup
+// where there are few (its own waves share the keys of one sequence and head, their parts meet in LDS), in two otherwise.
+// Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 189 us, 5.7 TB/s (a large sum reads 6.0); two of 131072 tokens 95 us and
+// 7 for the join of 16 shares, 5.6 TB/s; one of 1001 tokens, 32 heads, 11 us, latency: offsets, table, keys one after the other 2.7 us, two
+// steps 4, the join of eight waves 3.
 #include "fq_attn_cache.h"
 
 namespace fq {
@@ -303,19 +310,67 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     }
 }
 
-constexpr int JOIN_WAVES = 4, JOIN_THREADS = 64 * JOIN_WAVES;
+// The shares of one (row, head) joined: what is left is latency and, for many rows, the parts' bytes.
 
-// The shares of one (row, head) joined by WAVES waves.  Half a wave reads a share, four of its elements a lane.  Grid: x the (head,
-// wave)s in workgroups, y the query tokens, z the sequences.
-template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) void attn_cache_join_kernel(const CacheAttn a)
+// Up to MOST shares: half a wave to a (row, head), four elements a lane, or to COLUMNS heads in a row where there are few shares; every load that
+// a lane makes is on its way before the first is awaited.  Grid: x the heads, y the query tokens, z the sequences.
+constexpr int JOIN_THREADS = 256, JOIN_FEW = 16;
+constexpr int join_columns(int most) { return most == 2 ? 2 : 1; }
+template <int DT, int D, int MOST> __global__ __launch_bounds__(JOIN_THREADS) void attn_cache_join_kernel(const CacheAttn a)
 {
     typedef typename Stored<DT>::type T;
-    constexpr int HEADS = JOIN_WAVES / WAVES, TURNS = MAX_SPLITS / 64;
-    __shared__ v4f met[JOIN_WAVES][32];
-    const int b = blockIdx.z, t = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, head = blockIdx.x * HEADS + wave / WAVES;
-    const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
-    if (t >= rows.count || head >= a.heads_q) return;      // with several waves to a head the whole workgroup
-    const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.round), used = shares_used(keys, share);
+    typedef T v4 __attribute__((ext_vector_type(4)));
+    constexpr int COLUMNS = join_columns(MOST);
+    const int b = blockIdx.z, t = blockIdx.y, d = 4 * (threadIdx.x % 32);
+    const int first = scalar(a.cu_q, b), behind = scalar(a.cu_q, b + 1), len = scalar(a.lens, b);
+    const Rows rows = packed_rows(first, behind, a.tokens, a.max_q);
+    const int head = (blockIdx.x * (JOIN_THREADS / 32) + threadIdx.x / 32) * COLUMNS;
+    if (t >= rows.count || head >= a.heads_q || d >= D) return;
+    const int keys = cached_keys(len, a.max_len, a.capacity), used = shares_used(keys, share_keys(keys, a.splits, a.round));
+
+    v2f stat[COLUMNS][MOST];
+    v4f part[COLUMNS][MOST];
+#pragma unroll
+    for (int c = 0; c < COLUMNS; ++c)
+#pragma unroll
+        for (int s = 0; s < MOST; ++s) {
+            const size_t at = ((size_t)(rows.first + t) * a.heads_q + min(head + c, a.heads_q - 1)) * a.splits + max(min(s, used - 1), 0);
+            stat[c][s] = *reinterpret_cast<const v2f*>(a.stat + 2 * at);
+            part[c][s] = *reinterpret_cast<const v4f*>(a.part + at * D + d);
+        }
+#pragma unroll
+    for (int c = 0; c < COLUMNS; ++c) {
+        float best = -INFINITY, l = 0.0f;
+        v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < MOST; ++s) best = fmaxf(best, s < used ? stat[c][s][0] : -INFINITY);
+        if (best == -INFINITY) best = 0.0f;
+#pragma unroll
+        for (int s = 0; s < MOST; ++s)
+            if (s < used) {
+                const float w = __builtin_amdgcn_exp2f(stat[c][s][0] - best);
+                l += stat[c][s][1] * w;
+                y += part[c][s] * w;
+            }
+        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        v4 out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[e] = (T)(y[e] * inv);
+        if (head + c < a.heads_q) *reinterpret_cast<v4*>(static_cast<T*>(a.Y) + (size_t)(rows.first + t) * a.ldy + (size_t)(head + c) * D + d) = out;
+    }
+}
+
+// More shares: a workgroup to a (row, head), half a wave to a share.  Grid: x the heads, y the query tokens, z the sequences.
+template <int DT, int D> __global__ __launch_bounds__(JOIN_THREADS) void attn_cache_join_many_kernel(const CacheAttn a)
+{
+    typedef typename Stored<DT>::type T;
+    constexpr int WAVES = JOIN_THREADS / 64, TURNS = MAX_SPLITS / 64;
+    __shared__ v4f met[WAVES][32];
+    const int b = blockIdx.z, t = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, head = blockIdx.x;
+    const int first = scalar(a.cu_q, b), behind = scalar(a.cu_q, b + 1), len = scalar(a.lens, b);
+    const Rows rows = packed_rows(first, behind, a.tokens, a.max_q);
+    if (t >= rows.count) return;      // the whole workgroup
+    const int keys = cached_keys(len, a.max_len, a.capacity), used = shares_used(keys, share_keys(keys, a.splits, a.round));
     const size_t at = ((size_t)(rows.first + t) * a.heads_q + head) * a.splits;
     float top[TURNS], sum[TURNS], best = -INFINITY, l = 0.0f;
 #pragma unroll
@@ -336,7 +391,7 @@ template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) v
 #pragma unroll
     for (int s = 1; s < 64; s <<= 1) l += __shfl_xor(l, s);
     v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int d = 4 * (lane % 32), slot = wave % WAVES * 2 + lane / 32;
+    const int d = 4 * (lane % 32), slot = wave * 2 + lane / 32;
 #pragma unroll
     for (int k = 0; k < TURNS; ++k)
 #pragma unroll 8
@@ -347,13 +402,11 @@ template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) v
         }
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], 32);
-    if constexpr (WAVES > 1) {
-        if (lane < 32) met[wave][lane] = y;
-        __syncthreads();
-        y = met[0][lane % 32];
+    if (lane < 32) met[wave][lane] = y;
+    __syncthreads();
+    y = met[0][lane % 32];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) y += met[w][lane % 32];
-    }
+    for (int w = 1; w < WAVES; ++w) y += met[w][lane % 32];
     if (d >= D || slot > 0) return;
     const float inv = l > 0.0f ? 1.0f / l : 0.0f;
     typedef T v4 __attribute__((ext_vector_type(4)));
@@ -361,6 +414,12 @@ template <int DT, int D, int WAVES> __global__ __launch_bounds__(JOIN_THREADS) v
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] = (T)(y[e] * inv);
     *reinterpret_cast<v4*>(static_cast<T*>(a.Y) + (size_t)(rows.first + t) * a.ldy + (size_t)head * D + d) = out;
+}
+
+template <int DT, int D, int MOST> void join(const CacheAttn& a, int batch, hipStream_t stream)
+{
+    const int heads = JOIN_THREADS / 32 * join_columns(MOST);      // of a workgroup
+    attn_cache_join_kernel<DT, D, MOST><<<dim3((unsigned)((a.heads_q + heads - 1) / heads), (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
 }
 
 template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hipStream_t stream)
@@ -373,11 +432,10 @@ template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hi
     else if (tiles == 1) attn_cache_kernel<DT, D, 1, 4><<<grid, 256, 0, stream>>>(a);
     else if (a.round == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
     else attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
-    if (a.splits > 16)
-        attn_cache_join_kernel<DT, D, JOIN_WAVES><<<dim3((unsigned)a.heads_q, (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
-    else if (a.splits > 1)
-        attn_cache_join_kernel<DT, D, 1><<<dim3((unsigned)((a.heads_q + JOIN_WAVES - 1) / JOIN_WAVES), (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0,
-                                           stream>>>(a);
+    if (a.splits > JOIN_FEW) attn_cache_join_many_kernel<DT, D><<<dim3((unsigned)a.heads_q, (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
+    else if (a.splits > 4) join<DT, D, JOIN_FEW>(a, batch, stream);
+    else if (a.splits > 2) join<DT, D, 4>(a, batch, stream);
+    else if (a.splits > 1) join<DT, D, 2>(a, batch, stream);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
 }
