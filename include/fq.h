@@ -424,7 +424,7 @@ int fq_gemm_select(int variant);
  * fq_attn_cache — Y[i] = softmax(scale * Q[i] K^T) V over the cache: with n query tokens of sequence b and lens[b] tokens in the
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
  *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider, probabilities enter the second
- *   product as fp16; with up to 32 columns (query tokens times heads of a group) queries enter the first as integers of 1 / 16256 of their
+ *   product as fp16; with up to 32 columns (query tokens times heads of a group) queries enter the first as integers of 1 / 32512 of their
  *   head's largest magnitude.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they,
  *   not the lengths on the device, set the launch, so a captured call may be replayed with other lengths within them.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.

@@ -3,9 +3,9 @@
 // The reduction is bound by the cache's bytes: a key and a value byte serve at most the few queries of their group, so the
 // kernel is a stream from HBM into registers, and everything else has to fit beside it.  What a wave does with 64 keys:
 //   S^T = K Q^T   16 keys x 16 columns a product (a column is one query token of one head of the group), 64 elements of the head deep, in
-//                 8-bit integers: the codes go into the matrix instruction as they come.  The queries are integers of up to 127 * 128 steps,
+//                 8-bit integers: the codes go into the matrix instruction as they come.  The queries are integers of up to 127 * 256 steps,
 //                 two limbs, so that each product is done twice; the sums are exact.  (Codes widened to fp16 take five instructions
-//                 for four of them: a step of 64 keys is 440 vector instructions so, 700 that way.)
+//                 for four of them; a step of 64 keys is 300 vector instructions beside 32 products as it is.)
 //   softmax       running maximum and sum per column.  The product leaves a column's 64 scores in four lanes, 16 each.
 //   O^T += V^T P  16 dimensions x 16 columns, 32 keys deep, P rounded to fp16: half a step is 2^-11 of each, what an fp16 output is
 //                 rounded by too.  The sum that divides is that of the rounded ones.  A step's keys lie in one page, whose scale multiplies
@@ -16,8 +16,9 @@
 // Each wave has a step of keys and values under way while it works on the one before, 16 KiB for heads of 128; eight waves a CU, in one workgroup
 // where there are few (its own waves share the keys of one sequence and head, their parts meet in LDS), in two otherwise.
 // Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 189 us, 5.7 TB/s (a large sum reads 6.0); two of 131072 tokens 95 us and
-// 7 for the join of 16 shares, 5.6 TB/s; one of 1001 tokens, 32 heads, 11 us, latency: offsets, table, keys one after the other 2.7 us, two
-// steps 4, the join of eight waves 3.
+// 5 for the join of 16 shares, 5.6 TB/s; one of 1001 tokens, 32 heads, 11.7 us: 2.5 to the first scores, then 3 for each round of 512 keys (128
+// KiB through one CU), 0.8 until the waves have met.  Two steps under way instead of one, or the first step's loads before the queries', took up to
+// 1 us more on short sequences, as longer code has to come in first, and no less on long ones.
 #include "fq_attn_cache.h"
 
 namespace fq {
@@ -75,8 +76,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     const int most = visible_keys(keys, rows.count, last / a.group), least = visible_keys(keys, rows.count, c0 / a.group);
     const int from = split * share, to = min((int)min(from + (long long)share, (long long)most), most);
 
-    // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 0..15 of its column's head, as integers of up to 127 * 128
-    // steps, in two limbs of 8 bits: 128 high + low
+    // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 0..15 of its column's head, as integers of up to 127 * 256
+    // steps, in two limbs of 8 bits: 256 high + low
     v4i high[NT][KC], low[NT][KC];
     float factor[NT];
     int limit[NT];
@@ -87,7 +88,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         limit[n] = visible_keys(keys, rows.count, t);
         typedef T v8 __attribute__((ext_vector_type(8)));
         v8 raw[KC][2];
-        float top = 0.0f;
+        typedef uint16_t bits8 __attribute__((ext_vector_type(8)));
+        bits8 most8 = {0, 0, 0, 0, 0, 0, 0, 0};      // magnitudes: without the sign the 16 bits of either type are in the order of their values
 #pragma unroll
         for (int j = 0; j < KC; ++j)
 #pragma unroll
@@ -95,29 +97,32 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
 #pragma unroll
                 for (int e = 0; e < 8; ++e) raw[j][i][e] = (T)0.0f;
                 if (64 * j + 16 * g < D) raw[j][i] = *reinterpret_cast<const v8*>(p + 64 * j + 8 * i);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf((float)raw[j][i][e]));
+                most8 = __builtin_elementwise_max(most8, __builtin_bit_cast(bits8, raw[j][i]) & (uint16_t)0x7fff);
             }
+        uint16_t most_bits = most8[0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) most_bits = max(most_bits, most8[e]);
+        float top = (float)__builtin_bit_cast(T, most_bits);
         // the power of two first: the largest magnitude to [1, 2) (or what there is below), so that no size of query over- or underflows
         top = over_groups_max(top);
         const uint32_t power = min(max(__float_as_uint(top) >> 23, 1u), 253u);
         const float down = __uint_as_float((254u - power) << 23), up = __uint_as_float(power << 23);
         top *= down;
-        const float steps = top > 0.0f ? 16256.0f / top : 0.0f;
-        factor[n] = a.scale * LOG2E * (top * (1.0f / 16256.0f)) * up;
+        const float steps = top > 0.0f ? 32512.0f / top : 0.0f;
+        factor[n] = a.scale * LOG2E * (top * (1.0f / 32512.0f)) * up;
 #pragma unroll
         for (int j = 0; j < KC; ++j)
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                uint32_t hi = 0, lo = 0;
+                // rounded to integers by the addition of 1.5 * 2^23, whose sums have steps of 1: the value's low bits are the integer's.  With
+                // 128 more the second byte is the high limb and the first the low one, plus 128.
+                uint32_t v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int v = (int)rintf((float)raw[j][w / 2][4 * (w % 2) + e] * down * steps), top7 = (v + 64) >> 7;
-                    hi |= (uint32_t)(top7 & 0xff) << (8 * e);
-                    lo |= (uint32_t)((v - 128 * top7) & 0xff) << (8 * e);
-                }
-                high[n][j][w] = (int)hi;
-                low[n][j][w] = (int)lo;
+                for (int e = 0; e < 4; ++e)
+                    v[e] = __float_as_uint(__builtin_fmaf((float)raw[j][w / 2][4 * (w % 2) + e] * down, steps, 0x1.8p23f + 128.0f));
+                const uint32_t front = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), back = __builtin_amdgcn_perm(v[3], v[2], 0x05010400u);
+                low[n][j][w] = (int)(__builtin_amdgcn_perm(back, front, 0x05040100u) ^ 0x80808080u);
+                high[n][j][w] = (int)__builtin_amdgcn_perm(back, front, 0x07060302u);
             }
     }
 
@@ -190,7 +195,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
                     lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(k, low[n][j], lo, 0, 0, 0);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][t][i] = (float)((hi[i] << 7) + lo[i]);      // below 2^28
+                for (int i = 0; i < 4; ++i) s[n][t][i] = (float)((hi[i] << 8) + lo[i]);      // below 2^30
             }
 
         __builtin_amdgcn_sched_barrier(0);

@@ -107,10 +107,10 @@ inline bool cache_holds(const CachePlan& p, int batch, int max_q, int heads_kv)
 // Keys of one share when `keys` are dealt over `splits` workgroups: whole rounds, so that the last shares may be empty.
 FQ_BOTH int share_keys(int keys, int splits, int round)
 {
-    const long long step = CACHE_STEP * round, rounds = (keys + step * splits - 1) / (step * splits);
-    return rounds < 1 ? (int)step : (int)(rounds * step);
+    const unsigned step = CACHE_STEP * round, rounds = ((unsigned)keys + step * splits - 1) / (step * splits);
+    return (int)(rounds < 1 ? step : rounds * step);
 }
-FQ_BOTH int shares_used(int keys, int share) { return (int)(((long long)keys + share - 1) / share); }
+FQ_BOTH int shares_used(int keys, int share) { return (int)(((unsigned)keys + share - 1) / share); }
 
 // Queries of one head that a workgroup of the prompt's attention takes, 32 a wave.
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;

@@ -77,8 +77,8 @@ def prompt_case(q, k, v, cu_q, cu_k, scale, causal, x):
 
 
 def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
-    """Beyond attention_bound's, for up to 32 columns (query tokens times heads of a group): queries are rounded to 1 / 16256 of their
-    head's largest magnitude (half a step is below 1 / 32512 of it), which moves a score by `scores` / 32512 at most and a probability and the
+    """Beyond attention_bound's, for up to 32 columns (query tokens times heads of a group): queries are rounded to 1 / 32512 of their
+    head's largest magnitude (half a step is 1 / 65024 of it), which moves a score by `scores` / 65024 at most and a probability and the
     sum that divides it by as much each; and a step's product is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two
     products, four lanes' partial sums) of up to 1280 times the sum of p, in codes.
     For more columns: the scores' 32-bit sums are of codes plus 1152, up to 1280 where `scores` counts 128."""
@@ -87,4 +87,4 @@ def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
     bound = attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
     if int(np.diff(cu_q).max()) * (q.shape[1] // kc.shape[1]) > 32:
         return exact, bound + 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread
-    return exact, bound + 2 * scores / 32512 * spread + 16 * 2.0**-24 * 1280 * vs.max()
+    return exact, bound + 2 * scores / 65024 * spread + 16 * 2.0**-24 * 1280 * vs.max()
