@@ -159,7 +159,7 @@ int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int
     if (!rc) rc = check_indices("cu_q", cu_q);
     if (!rc) rc = check_indices("cu_k", cu_k);
     if (rc) return rc;
-    const long long places = (long long)batch * heads_q * prompt_tiles(max_q);
+    const long long places = prompt_workgroups(prompt_places(tokens_q, batch, max_q), heads_q, heads_kv);
     if (places >= (1LL << 31) || !launch_holds(places, PROMPT_THREADS))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);
     if (tokens_q == 0) return FQ_OK;

@@ -47,11 +47,11 @@ __device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
 {
     const int lane = threadIdx.x % 64, mine = a.lens[min(lane, batch - 1)], half = (batch + 1) / 2;
     const int nth = a.order == CACHE_FOLDED && z >= half ? batch - 1 - (z - half) : z;
+    const uint32_t key = lane < batch ? length_key(mine) : 0;
     int longer = 0;
-    for (int i = 0; i < batch; ++i) {
-        const int other = __builtin_amdgcn_readlane(mine, i);
-        longer += other > mine || (other == mine && i < lane);
-    }
+    for (int i0 = 0; i0 < batch; i0 += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) longer += (uint32_t)__builtin_amdgcn_readlane((int)key, i0 + i) > key;
     return __builtin_ctzll(__ballot(lane < batch && longer == nth));
 }
 

@@ -58,5 +58,11 @@ __device__ __forceinline__ float over_halves_sum(float v)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// What orders up to 64 sequences, one a lane, by their lengths: no two are equal.  (Lengths of 2^26 and more count as equally long.)
+__device__ __forceinline__ uint32_t length_key(int length)
+{
+    return (uint32_t)min(max(length, 0), (1 << 26) - 1) << 6 | (63 - threadIdx.x % 64);
+}
+
 }  // namespace
 }  // namespace fq

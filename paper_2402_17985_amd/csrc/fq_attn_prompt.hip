@@ -25,7 +25,7 @@ struct PromptAttn {
     long long ldq, ldk, ldv, ldy;
     const int32_t *cu_q, *cu_k;
     float factor;            // scale * log2(e), positive
-    int tokens_q, tokens_k, max_q, heads_q, heads_kv, group, causal, batch, tiles;
+    int tokens_q, tokens_k, max_q, heads_q, heads_kv, group, causal, batch;
 };
 
 constexpr int PROMPT_KEYS = 64;   // a tile
@@ -52,27 +52,46 @@ __device__ __forceinline__ void copy_to_lds(const void* uniform_base, uint32_t l
 }
 __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
 
-// A workgroup's sequence.  Of at most 64 it is the one that is nth by its number of keys, longest first: long ones begun last would run on
-// alone.  All offsets are loaded at once, one sequence a lane, so that the order costs no further trip to memory.
-struct PromptSequence {
+// The tile of queries at a place; of none: -1.  Of at most 64 sequences those with the most keys come first: long ones begun last would run on
+// alone (8 uneven prompts: 293 us as they come, 280 so).  All offsets are loaded at once, one sequence a lane, so that the order costs no further
+// trip to memory; of more sequences the one at the place is searched, 64 probes at a time.
+struct PromptTile {
     Rows q, k;
+    int tile;
 };
-__device__ __forceinline__ PromptSequence nth_sequence(const PromptAttn& a, int nth)
+__device__ __forceinline__ PromptTile tile_at(const PromptAttn& a, int place)
 {
-    const bool sorted = a.batch <= 64;
-    const int lane = threadIdx.x % 64, j = sorted ? min(lane, a.batch - 1) : nth;
-    const Rows k = packed_rows(a.cu_k[j], a.cu_k[j + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[j], a.cu_q[j + 1], a.tokens_q, a.max_q);
-    int from = 0;      // any lane
-    if (sorted && a.batch > 1) {
-        int longer = 0;
-        for (int i = 0; i < a.batch; ++i) {
-            const int other = __builtin_amdgcn_readlane(k.count, i);
-            longer += other > k.count || (other == k.count && i < lane);
-        }
-        from = __builtin_ctzll(__ballot(lane < a.batch && longer == nth));
+    const int lane = threadIdx.x % 64;
+    const auto tiles_of = [](const Rows& q) { return (int)(((unsigned)q.count + PROMPT_ROWS - 1) / PROMPT_ROWS); };
+    if (a.batch <= PROMPT_SORTED) {
+        const int j = min(lane, a.batch - 1);
+        const Rows k = packed_rows(a.cu_k[j], a.cu_k[j + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[j], a.cu_q[j + 1], a.tokens_q, a.max_q);
+        const int tiles = lane < a.batch ? tiles_of(q) : 0;
+        const uint32_t key = length_key(k.count);
+        int before = 0;
+        for (int i0 = 0; i0 < a.batch; i0 += 4)      // lanes without a sequence have no tiles
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int its = __builtin_amdgcn_readlane(tiles, i0 + i);
+                before += (uint32_t)__builtin_amdgcn_readlane((int)key, i0 + i) > key ? its : 0;
+            }
+        const uint64_t here = __ballot(place >= before && place - before < tiles);
+        const int from = here ? __builtin_ctzll(here) : 0, nth = place - __builtin_amdgcn_readlane(before, from);
+        return {{__builtin_amdgcn_readlane(q.first, from), __builtin_amdgcn_readlane(q.count, from)},
+                {__builtin_amdgcn_readlane(k.first, from), __builtin_amdgcn_readlane(k.count, from)},
+                here ? __builtin_amdgcn_readlane(tiles, from) - 1 - nth : -1};
     }
-    return {{__builtin_amdgcn_readlane(q.first, from), __builtin_amdgcn_readlane(q.count, from)},
-            {__builtin_amdgcn_readlane(k.first, from), __builtin_amdgcn_readlane(k.count, from)}};
+    int b = 0;
+    for (int n = a.batch; n > 1;) {      // it is one of n from b on
+        const int apart = (n + 63) / 64, probe = b + lane * apart;
+        const bool reached = lane * apart < n && prompt_first_place(a.cu_q[min(probe, a.batch - 1)], a.tokens_q, probe) <= place;
+        const int skip = max((int)__builtin_popcountll(__ballot(reached)) - 1, 0) * apart;
+        b += skip;
+        n = min(apart, n - skip);
+    }
+    const Rows k = packed_rows(a.cu_k[b], a.cu_k[b + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens_q, a.max_q);
+    const int tiles = tiles_of(q), nth = place - prompt_first_place(a.cu_q[b], a.tokens_q, b);
+    return {q, k, nth >= 0 && nth < tiles ? tiles - 1 - nth : -1};
 }
 
 template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 4 : D <= 96 ? 3 : 2) void attn_prompt_kernel(const PromptAttn a)
@@ -85,14 +104,12 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
     // [keys, two stages][values, two stages]; reads of the last 32 dimensions reach behind a row of 80
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE + 64];
 
-    const PromptPlace at_place = prompt_place(blockIdx.x, (unsigned)a.tiles * a.group, (unsigned)a.batch * a.heads_kv);
-    const int tile = a.tiles - 1 - (int)(at_place.item / a.group), nth = at_place.pair / a.heads_kv, hk = at_place.pair - nth * a.heads_kv;
-    const int head = hk * a.group + at_place.item % a.group;
-
-    const PromptSequence sequence = nth_sequence(a, nth);
-    const Rows rq = sequence.q, rk = sequence.k;
-    const int q0 = tile * PROMPT_ROWS;
-    if (q0 >= rq.count) return;
+    const PromptUnit unit = prompt_unit(blockIdx.x, (unsigned)a.group, (unsigned)a.heads_kv);
+    const int hk = unit.head_kv, head = hk * a.group + unit.member;
+    const PromptTile at = tile_at(a, unit.place);
+    if (at.tile < 0) return;
+    const Rows rq = at.q, rk = at.k;
+    const int q0 = at.tile * PROMPT_ROWS;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
     const int row = q0 + 32 * wave + col, keys = rk.count;
     const auto visible = [&](int i) { return a.causal ? visible_keys(keys, rq.count, i) : keys; };
@@ -293,7 +310,7 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
 
 template <int DT> int launch(const PromptAttn& a, int head_dim, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)(a.batch * (long long)a.heads_q * a.tiles);
+    const unsigned grid = (unsigned)prompt_workgroups(prompt_places(a.tokens_q, a.batch, a.max_q), a.heads_q, a.heads_kv);
     switch (head_dim) {
     case 64: attn_prompt_kernel<DT, 64><<<grid, PROMPT_THREADS, 0, stream>>>(a); break;
     case 80: attn_prompt_kernel<DT, 80><<<grid, PROMPT_THREADS, 0, stream>>>(a); break;
@@ -311,7 +328,7 @@ int launch_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype,
                        int causal, float scale, void* Y, long long ldy, hipStream_t stream)
 {
     const PromptAttn a{Q, K, V, Y, ldq, ldk, ldv, ldy, cu_q, cu_k, scale * LOG2E, tokens_q, tokens_k, max_q, heads_q, heads_kv, heads_q / heads_kv,
-                       causal, batch, (int)prompt_tiles(max_q)};
+                       causal, batch};
     return x_dtype == FQ_F16 ? launch<FQ_F16>(a, head_dim, stream) : launch<FQ_BF16>(a, head_dim, stream);
 }
 

@@ -116,6 +116,31 @@ FQ_BOTH int shares_used(int keys, int share) { return (int)(((unsigned)keys + sh
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;
 inline long long prompt_tiles(int max_q) { return ((long long)max_q + PROMPT_ROWS - 1) / PROMPT_ROWS; }
 
+// Places for tiles of queries: at least as many as packed sequences of `tokens` rows in all can have tiles.  Their number, not the longest sequence
+// times the sequences, sets the launch: most of that would be workgroups without work where lengths differ.  Of up to 64 sequences, which the
+// kernel orders by their lengths, the tiles follow one another without gaps; of more, sequence b's begin at place cu_q[b] / 128 + b, which leaves
+// room for its last, partly filled one and is found without adding up the others.
+constexpr int PROMPT_SORTED = 64;
+inline long long prompt_places(int tokens, int batch, int max_q)
+{
+    const long long by_rows = tokens / PROMPT_ROWS + (long long)batch, by_length = batch * prompt_tiles(max_q);
+    return batch <= PROMPT_SORTED ? std::min(by_rows, by_length) : by_rows;
+}
+FQ_BOTH int prompt_first_place(int from, int tokens, int b) { return (from < 0 ? 0 : from > tokens ? tokens : from) / PROMPT_ROWS + b; }
+
+// Workgroup -> place, key head and head of its group.  Workgroups are dealt round-robin to the 8 XCDs.  The (place, key head)s go round them as
+// well, the heads of a group stay together: with a multiple of 8 key heads each head's keys and values are in one XCD's L2, and with any number all
+// XCDs have tiles of the longest sequence.
+struct PromptUnit {
+    unsigned place, head_kv, member;
+};
+FQ_BOTH PromptUnit prompt_unit(unsigned id, unsigned group, unsigned heads_kv)
+{
+    const unsigned at = id / 8, unit = at / group * 8 + id % 8, place = unit / heads_kv;
+    return PromptUnit{place, unit - place * heads_kv, at - at / group * group};
+}
+inline long long prompt_workgroups(long long places, int heads_q, int heads_kv) { return (places * heads_kv + 7) / 8 * 8 * (heads_q / heads_kv); }
+
 // Workgroup -> (sequence, key head) pair and one of its `items` (query tiles of the group's heads).  Workgroups are dealt round-robin to
 // the 8 XCDs: a pair stays on one of them, whose L2 then holds its keys and values, and the pairs go round the XCDs too, as
 // neighbouring ones (heads of one sequence) are equally long.  The last few pairs are split among all.
