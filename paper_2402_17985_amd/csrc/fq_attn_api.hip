@@ -110,7 +110,7 @@ int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int t
 size_t fq_attn_cache_workspace_bytes(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv, int head_dim)
 {
     if (batch <= 0 || tokens < 0 || max_q <= 0 || max_len <= 0 || heads_q <= 0 || heads_kv <= 0 || heads_q < heads_kv || head_dim <= 0) return 16;
-    const int splits = cache_plan(batch, max_q, max_len, heads_q, heads_kv).splits;
+    const int splits = cache_plan(batch, tokens, max_q, max_len, heads_q, heads_kv).splits;
     return splits > 1 ? round_up((size_t)tokens * heads_q * splits * (head_dim + 2) * sizeof(float), 16) + 16 : 16;
 }
 
@@ -132,7 +132,7 @@ int fq_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads
     if (rc) return rc;
     if (max_len <= 0) return fail(FQ_ERR_SHAPE, "max_len = %d must be positive", max_len);
     if ((long long)max_q * heads_q >= (1LL << 30)) return fail(FQ_ERR_RANGE, "max_q = %d queries of %d heads: at most 2^30 together", max_q, heads_q);
-    if (!cache_holds(cache_plan(batch, max_q, max_len, heads_q, heads_kv), batch, max_q, heads_kv))
+    if (!cache_holds(cache_plan(batch, tokens, max_q, max_len, heads_q, heads_kv), heads_kv))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);
     if (!workspace) return fail(FQ_ERR_NULL, "workspace is NULL");
     if (!aligned16(workspace)) return fail(FQ_ERR_ALIGN, "workspace is not 16-byte aligned");
@@ -159,7 +159,7 @@ int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int
     if (!rc) rc = check_indices("cu_q", cu_q);
     if (!rc) rc = check_indices("cu_k", cu_k);
     if (rc) return rc;
-    const long long places = prompt_workgroups(prompt_places(tokens_q, batch, max_q), heads_q, heads_kv);
+    const long long places = prompt_workgroups(tokens_q, batch, max_q, heads_q, heads_kv);
     if (places >= (1LL << 31) || !launch_holds(places, PROMPT_THREADS))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d queries of %d heads are more than one launch holds", batch, max_q, heads_q);
     if (tokens_q == 0) return FQ_OK;

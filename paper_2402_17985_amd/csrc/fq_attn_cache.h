@@ -13,11 +13,11 @@ struct CacheAttn {
     const float *k_scale, *v_scale;
     float *part, *stat;     // with more than one split: [row, head, split, head_dim] and [row, head, split, (maximum, sum)]
     float scale;
-    int tokens, max_q, max_len, heads_q, heads_kv, group, capacity, pages, page, page_shift, width, splits, round, blocks, order;      // blocks of columns
+    int tokens, max_q, max_len, heads_q, heads_kv, group, capacity, pages, page, page_shift, width, splits, round, order;
 };
 
 // The kernel for many columns (fq_attn_cache_wide.hip)
-int launch_attn_cache_wide(const CacheAttn& a, int x_dtype, int head_dim, int batch, hipStream_t stream);
+int launch_attn_cache_wide(const CacheAttn& a, int x_dtype, int head_dim, int batch, unsigned grid, hipStream_t stream);
 
 namespace {
 

@@ -48,14 +48,11 @@ __device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
     const int lane = threadIdx.x % 64, mine = a.lens[min(lane, batch - 1)], half = (batch + 1) / 2;
     const int nth = a.order == CACHE_FOLDED && z >= half ? batch - 1 - (z - half) : z;
     const uint32_t key = lane < batch ? length_key(mine) : 0;
-    int longer = 0;
-    for (int i0 = 0; i0 < batch; i0 += 4)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) longer += (uint32_t)__builtin_amdgcn_readlane((int)key, i0 + i) > key;
+    const int longer = sum_of_longer(key, 1, batch);
     return __builtin_ctzll(__ballot(lane < batch && longer == nth));
 }
 
-// NT tiles of 16 columns.  Grid: x the splits of all column tiles, y the key heads, z the sequences.
+// NT tiles of 16 columns, which all of a sequence and key head's have room in.  Grid: x the shares of the keys, y the key heads, z the sequences.
 template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(const CacheAttn a)
 {
     constexpr int ROUND = CACHE_STEP * WAVES;
@@ -64,16 +61,15 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     __shared__ float gathered[WAVES][16][ROW];
     __shared__ float tops[WAVES][16 * NT], sums[WAVES][16 * NT];
 
-    const int tile = blockIdx.x / a.splits, split = blockIdx.x - tile * a.splits, h = blockIdx.y;
+    const int split = blockIdx.x, h = blockIdx.y;
     const int b = a.order != CACHE_AS_GIVEN ? by_length(a, blockIdx.z, gridDim.z) : (int)blockIdx.z;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 16, g = lane / 16;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
-    const int columns = rows.count * a.group, c0 = tile * 16 * NT;
-    if (c0 >= columns) return;
+    const int columns = rows.count * a.group;
+    if (columns == 0) return;
     const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, WAVES);
     if (split > 0 && split * (long long)share >= keys) return;
-    const int last = min(c0 + 16 * NT, columns) - 1;
-    const int most = visible_keys(keys, rows.count, last / a.group), least = visible_keys(keys, rows.count, c0 / a.group);
+    const int most = visible_keys(keys, rows.count, rows.count - 1), least = visible_keys(keys, rows.count, 0);
     const int from = split * share, to = min((int)min(from + (long long)share, (long long)most), most);
 
     // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 0..15 of its column's head, as integers of up to 127 * 256
@@ -83,7 +79,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int c = c0 + 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
+        const int c = 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
         const T* p = static_cast<const T*>(a.Q) + (rows.first + t) * (size_t)a.ldq + (size_t)(h * a.group + cc - t * a.group) * D + 16 * g;
         limit[n] = visible_keys(keys, rows.count, t);
         typedef T v8 __attribute__((ext_vector_type(8)));
@@ -283,7 +279,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f*>(&gathered[wave][col][16 * t + 4 * g]) = o[n][t] * mine;
         __syncthreads();
         for (int i = tid; i < 16 * (D / 4); i += 64 * WAVES) {
-            const int cl = i / (D / 4), d = (i - cl * (D / 4)) * 4, c = c0 + 16 * n + cl;
+            const int cl = i / (D / 4), d = (i - cl * (D / 4)) * 4, c = 16 * n + cl;
             if (c >= columns) continue;
             float best = tops[0][16 * n + cl], l = 0.0f;
 #pragma unroll
@@ -369,7 +365,7 @@ template <int DT, int D, int MOST> __global__ __launch_bounds__(JOIN_THREADS) vo
 template <int DT, int D> __global__ __launch_bounds__(JOIN_THREADS) void attn_cache_join_many_kernel(const CacheAttn a)
 {
     typedef typename Stored<DT>::type T;
-    constexpr int WAVES = JOIN_THREADS / 64, TURNS = MAX_SPLITS / 64;
+    constexpr int WAVES = JOIN_THREADS / 64, SLOTS = 2 * WAVES, TURNS = MAX_SPLITS / 64;
     __shared__ v4f met[WAVES][32];
     const int b = blockIdx.z, t = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, head = blockIdx.x;
     const int first = scalar(a.cu_q, b), behind = scalar(a.cu_q, b + 1), len = scalar(a.lens, b);
@@ -398,13 +394,17 @@ template <int DT, int D> __global__ __launch_bounds__(JOIN_THREADS) void attn_ca
     v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
     const int d = 4 * (lane % 32), slot = wave * 2 + lane / 32;
 #pragma unroll
-    for (int k = 0; k < TURNS; ++k)
-#pragma unroll 8
-        for (int s0 = 64 * k; s0 < min(used, 64 * k + 64); s0 += 2 * WAVES) {
-            const int s = s0 + slot;
-            const float w = __shfl(top[k], s % 64);
-            if (s < used && d < D) y += *reinterpret_cast<const v4f*>(a.part + (at + s) * D + d) * w;
+    for (int k = 0; k < TURNS; ++k) {
+        if (64 * k >= used) break;
+        v4f part[64 / SLOTS];
+#pragma unroll
+        for (int i = 0; i < 64 / SLOTS; ++i) part[i] = *reinterpret_cast<const v4f*>(a.part + (at + min(64 * k + SLOTS * i + slot, used - 1)) * D + min(d, D - 4));
+#pragma unroll
+        for (int i = 0; i < 64 / SLOTS; ++i) {
+            const float w = __shfl(top[k], SLOTS * i + slot);
+            if (64 * k + SLOTS * i + slot < used) y += part[i] * w;
         }
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] += __shfl_xor(y[e], 32);
     if (lane < 32) met[wave][lane] = y;
@@ -424,20 +424,20 @@ template <int DT, int D> __global__ __launch_bounds__(JOIN_THREADS) void attn_ca
 template <int DT, int D, int MOST> void join(const CacheAttn& a, int batch, hipStream_t stream)
 {
     const int heads = JOIN_THREADS / 32 * join_columns(MOST);      // of a workgroup
-    attn_cache_join_kernel<DT, D, MOST><<<dim3((unsigned)((a.heads_q + heads - 1) / heads), (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
+    attn_cache_join_kernel<DT, D, MOST><<<dim3((unsigned)((a.heads_q + heads - 1) / heads), (unsigned)std::min(a.max_q, a.tokens), (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
 }
 
-template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hipStream_t stream)
+template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, unsigned wide_grid, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.blocks * a.splits), (unsigned)a.heads_kv, (unsigned)batch);
+    const dim3 grid((unsigned)a.splits, (unsigned)a.heads_kv, (unsigned)batch);
     if (tiles * 16 == WIDE_COLUMNS) {
-        const int rc = launch_attn_cache_wide(a, DT, D, batch, stream);
+        const int rc = launch_attn_cache_wide(a, DT, D, batch, wide_grid, stream);
         if (rc) return rc;
     } else if (tiles == 1 && a.round == 8) attn_cache_kernel<DT, D, 1, 8><<<grid, 512, 0, stream>>>(a);
     else if (tiles == 1) attn_cache_kernel<DT, D, 1, 4><<<grid, 256, 0, stream>>>(a);
     else if (a.round == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
     else attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
-    if (a.splits > JOIN_FEW) attn_cache_join_many_kernel<DT, D><<<dim3((unsigned)a.heads_q, (unsigned)a.max_q, (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
+    if (a.splits > JOIN_FEW) attn_cache_join_many_kernel<DT, D><<<dim3((unsigned)a.heads_q, (unsigned)std::min(a.max_q, a.tokens), (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
     else if (a.splits > 4) join<DT, D, JOIN_FEW>(a, batch, stream);
     else if (a.splits > 2) join<DT, D, 4>(a, batch, stream);
     else if (a.splits > 1) join<DT, D, 2>(a, batch, stream);
@@ -445,13 +445,13 @@ template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, hi
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
 }
 
-template <int DT> int launch_dim(const CacheAttn& a, int tiles, int head_dim, int batch, hipStream_t stream)
+template <int DT> int launch_dim(const CacheAttn& a, int tiles, int head_dim, int batch, unsigned wide_grid, hipStream_t stream)
 {
     switch (head_dim) {
-    case 64: return launch<DT, 64>(a, tiles, batch, stream);
-    case 80: return launch<DT, 80>(a, tiles, batch, stream);
-    case 96: return launch<DT, 96>(a, tiles, batch, stream);
-    default: return launch<DT, 128>(a, tiles, batch, stream);
+    case 64: return launch<DT, 64>(a, tiles, batch, wide_grid, stream);
+    case 80: return launch<DT, 80>(a, tiles, batch, wide_grid, stream);
+    case 96: return launch<DT, 96>(a, tiles, batch, wide_grid, stream);
+    default: return launch<DT, 128>(a, tiles, batch, wide_grid, stream);
     }
 }
 
@@ -462,14 +462,16 @@ int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int h
                       const float* k_scale, const float* v_scale, int pages, int page_size, const int32_t* page_table, int table_width,
                       float scale, void* Y, long long ldy, void* workspace, hipStream_t stream)
 {
-    const CachePlan plan = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
+    const CachePlan plan = cache_plan(batch, tokens, max_q, max_len, heads_q, heads_kv);
     const int splits = plan.splits;
     float* part = static_cast<float*>(workspace);
     float* stat = part + (splits > 1 ? (size_t)tokens * heads_q * splits * head_dim : 0);
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
                       heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
-                      page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.blocks, plan.order};
-    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, stream) : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, stream);
+                      page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.order};
+    const unsigned wide_grid = (unsigned)tile_workgroups(plan.places, splits, heads_kv);
+    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, wide_grid, stream)
+                             : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, wide_grid, stream);
 }
 
 }  // namespace fq

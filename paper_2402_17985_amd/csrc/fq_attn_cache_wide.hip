@@ -25,6 +25,25 @@ constexpr int pair_place(int C, int r, int e, int half)
     return C == 16 ? (e + r) % 8 + 8 * ((half + r / 8) % 2) : C == 8 ? (e + 4 * ((half + r) % 2) + r / 2) % 8 : (2 * e + half + key_turn(C, r)) % C;
 }
 
+// The tile of columns at a place: of which sequence; of none: -1.  Of at most 64 sequences the longest come first.
+struct WideTile {
+    int sequence, nth;
+};
+__device__ __forceinline__ WideTile tile_at(const CacheAttn& a, int batch, int place)
+{
+    const int lane = threadIdx.x % 64;
+    const auto tiles_of = [&](int b) { return (packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q).count * a.group + WIDE_COLUMNS - 1) / WIDE_COLUMNS; };
+    if (batch <= SORTED_SEQUENCES) {
+        const int j = min(lane, batch - 1), len = a.lens[j], tiles = lane < batch ? tiles_of(j) : 0, before = sum_of_longer(length_key(len), tiles, batch);
+        const uint64_t here = __ballot(place >= before && place - before < tiles);
+        const int from = here ? __builtin_ctzll(here) : 0;
+        return {here ? from : -1, place - __builtin_amdgcn_readlane(before, from)};
+    }
+    const auto first = [&](int b) { return first_place((long long)min(max(a.cu_q[b], 0), a.tokens) * a.group, WIDE_COLUMNS, b); };
+    const int b = sequence_at(place, batch, first), nth = place - first(b);
+    return {nth >= 0 && nth < tiles_of(b) ? b : -1, nth};
+}
+
 template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn_cache_wide_kernel(const CacheAttn a, int batch)
 {
     typedef typename Stored<DT>::type T;
@@ -34,13 +53,17 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     constexpr bool EVEN = CACHE_STEP * D / 16 % WIDE_THREADS == 0;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (KTILE + VTILE)];            // [keys, two stages][values, two stages]
 
-    // workgroups of one sequence and key head on one XCD, those of one share next to each other
-    const PromptPlace at_place = prompt_place(blockIdx.x, (unsigned)(a.blocks * a.splits), (unsigned)(batch * a.heads_kv));
-    const int split = at_place.item / a.blocks, block = at_place.item - split * a.blocks, b = at_place.pair / a.heads_kv, h = at_place.pair - b * a.heads_kv;
+    // The tiles of a share next to each other: 64 tokens behind 8128, 64 heads over 8, 39 us; the shares of a tile so, 42.
+    const unsigned of_share = gridDim.x / a.splits;      // whole eights
+    const int split = blockIdx.x / of_share;
+    const TileUnit work = tile_unit(blockIdx.x - split * of_share, 1, (unsigned)a.heads_kv);
+    const int h = work.head_kv;
+    const WideTile at_tile = tile_at(a, batch, work.place);
+    const int b = at_tile.sequence;
+    if (b < 0) return;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 32, half = lane / 32;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
-    const int columns = rows.count * a.group, c0 = block * WIDE_COLUMNS;
-    if (c0 >= columns) return;
+    const int columns = rows.count * a.group, c0 = at_tile.nth * WIDE_COLUMNS;
     const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, a.round);
     if (split > 0 && split * (long long)share >= keys) return;
     const auto visible = [&](int c) { return visible_keys(keys, rows.count, min(c, columns - 1) / a.group); };
@@ -331,9 +354,8 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         }
 }
 
-template <int DT> int launch(const CacheAttn& a, int head_dim, int batch, hipStream_t stream)
+template <int DT> int launch(const CacheAttn& a, int head_dim, int batch, unsigned grid, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)((long long)batch * a.heads_kv * a.blocks * a.splits);
     switch (head_dim) {
     case 64: attn_cache_wide_kernel<DT, 64><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
     case 80: attn_cache_wide_kernel<DT, 80><<<grid, WIDE_THREADS, 0, stream>>>(a, batch); break;
@@ -346,9 +368,9 @@ template <int DT> int launch(const CacheAttn& a, int head_dim, int batch, hipStr
 
 }  // namespace
 
-int launch_attn_cache_wide(const CacheAttn& a, int x_dtype, int head_dim, int batch, hipStream_t stream)
+int launch_attn_cache_wide(const CacheAttn& a, int x_dtype, int head_dim, int batch, unsigned grid, hipStream_t stream)
 {
-    return x_dtype == FQ_F16 ? launch<FQ_F16>(a, head_dim, batch, stream) : launch<FQ_BF16>(a, head_dim, batch, stream);
+    return x_dtype == FQ_F16 ? launch<FQ_F16>(a, head_dim, batch, grid, stream) : launch<FQ_BF16>(a, head_dim, batch, grid, stream);
 }
 
 }  // namespace fq

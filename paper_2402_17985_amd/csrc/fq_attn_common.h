@@ -64,5 +64,33 @@ __device__ __forceinline__ uint32_t length_key(int length)
     return (uint32_t)min(max(length, 0), (1 << 26) - 1) << 6 | (63 - threadIdx.x % 64);
 }
 
+// The sum of `value` over the lanes of the batch with a larger key (a lane without a sequence has key 0 or value 0).
+__device__ __forceinline__ int sum_of_longer(uint32_t key, int value, int batch)
+{
+    int sum = 0;
+    for (int i0 = 0; i0 < batch; i0 += 4)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int its = __builtin_amdgcn_readlane(value, i0 + i);
+            sum += (uint32_t)__builtin_amdgcn_readlane((int)key, i0 + i) > key ? its : 0;
+        }
+    return sum;
+}
+
+// The sequence of a batch whose tiles lie at `place` where sequence b's begin at first(b), which does not fall: 64 probes at a time.
+template <typename First> __device__ __forceinline__ int sequence_at(int place, int batch, First first)
+{
+    const int lane = threadIdx.x % 64;
+    int b = 0;
+    for (int n = batch; n > 1;) {      // it is one of n from b on
+        const int apart = (n + 63) / 64, probe = b + lane * apart;
+        const bool reached = lane * apart < n && first(min(probe, batch - 1)) <= place;
+        const int skip = max((int)__builtin_popcountll(__ballot(reached)) - 1, 0) * apart;
+        b += skip;
+        n = min(apart, n - skip);
+    }
+    return b;
+}
+
 }  // namespace
 }  // namespace fq

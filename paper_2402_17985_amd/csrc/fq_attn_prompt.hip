@@ -54,7 +54,7 @@ __device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)
 
 // The tile of queries at a place; of none: -1.  Of at most 64 sequences those with the most keys come first: long ones begun last would run on
 // alone (8 uneven prompts: 293 us as they come, 280 so).  All offsets are loaded at once, one sequence a lane, so that the order costs no further
-// trip to memory; of more sequences the one at the place is searched, 64 probes at a time.
+// trip to memory; of more sequences the one at the place is searched.
 struct PromptTile {
     Rows q, k;
     int tile;
@@ -63,34 +63,21 @@ __device__ __forceinline__ PromptTile tile_at(const PromptAttn& a, int place)
 {
     const int lane = threadIdx.x % 64;
     const auto tiles_of = [](const Rows& q) { return (int)(((unsigned)q.count + PROMPT_ROWS - 1) / PROMPT_ROWS); };
-    if (a.batch <= PROMPT_SORTED) {
+    if (a.batch <= SORTED_SEQUENCES) {
         const int j = min(lane, a.batch - 1);
         const Rows k = packed_rows(a.cu_k[j], a.cu_k[j + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[j], a.cu_q[j + 1], a.tokens_q, a.max_q);
         const int tiles = lane < a.batch ? tiles_of(q) : 0;
-        const uint32_t key = length_key(k.count);
-        int before = 0;
-        for (int i0 = 0; i0 < a.batch; i0 += 4)      // lanes without a sequence have no tiles
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int its = __builtin_amdgcn_readlane(tiles, i0 + i);
-                before += (uint32_t)__builtin_amdgcn_readlane((int)key, i0 + i) > key ? its : 0;
-            }
+        const int before = sum_of_longer(length_key(k.count), tiles, a.batch);
         const uint64_t here = __ballot(place >= before && place - before < tiles);
         const int from = here ? __builtin_ctzll(here) : 0, nth = place - __builtin_amdgcn_readlane(before, from);
         return {{__builtin_amdgcn_readlane(q.first, from), __builtin_amdgcn_readlane(q.count, from)},
                 {__builtin_amdgcn_readlane(k.first, from), __builtin_amdgcn_readlane(k.count, from)},
                 here ? __builtin_amdgcn_readlane(tiles, from) - 1 - nth : -1};
     }
-    int b = 0;
-    for (int n = a.batch; n > 1;) {      // it is one of n from b on
-        const int apart = (n + 63) / 64, probe = b + lane * apart;
-        const bool reached = lane * apart < n && prompt_first_place(a.cu_q[min(probe, a.batch - 1)], a.tokens_q, probe) <= place;
-        const int skip = max((int)__builtin_popcountll(__ballot(reached)) - 1, 0) * apart;
-        b += skip;
-        n = min(apart, n - skip);
-    }
+    const auto first = [&](int b) { return first_place(min(max(a.cu_q[b], 0), a.tokens_q), PROMPT_ROWS, b); };
+    const int b = sequence_at(place, a.batch, first);
     const Rows k = packed_rows(a.cu_k[b], a.cu_k[b + 1], a.tokens_k, a.tokens_k), q = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens_q, a.max_q);
-    const int tiles = tiles_of(q), nth = place - prompt_first_place(a.cu_q[b], a.tokens_q, b);
+    const int tiles = tiles_of(q), nth = place - first(b);
     return {q, k, nth >= 0 && nth < tiles ? tiles - 1 - nth : -1};
 }
 
@@ -104,7 +91,7 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
     // [keys, two stages][values, two stages]; reads of the last 32 dimensions reach behind a row of 80
     __shared__ __attribute__((aligned(16))) uint8_t lds[4 * TILE + 64];
 
-    const PromptUnit unit = prompt_unit(blockIdx.x, (unsigned)a.group, (unsigned)a.heads_kv);
+    const TileUnit unit = tile_unit(blockIdx.x, (unsigned)a.group, (unsigned)a.heads_kv);
     const int hk = unit.head_kv, head = hk * a.group + unit.member;
     const PromptTile at = tile_at(a, unit.place);
     if (at.tile < 0) return;
@@ -310,7 +297,7 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
 
 template <int DT> int launch(const PromptAttn& a, int head_dim, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)prompt_workgroups(prompt_places(a.tokens_q, a.batch, a.max_q), a.heads_q, a.heads_kv);
+    const unsigned grid = (unsigned)prompt_workgroups(a.tokens_q, a.batch, a.max_q, a.heads_q, a.heads_kv);
     switch (head_dim) {
     case 64: attn_prompt_kernel<DT, 64><<<grid, PROMPT_THREADS, 0, stream>>>(a); break;
     case 80: attn_prompt_kernel<DT, 80><<<grid, PROMPT_THREADS, 0, stream>>>(a); break;

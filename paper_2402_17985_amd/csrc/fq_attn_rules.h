@@ -75,33 +75,61 @@ FQ_BOTH int visible_keys(int keys, int n, int i)
     return v < 0 ? 0 : v;
 }
 
+// Places for the tiles of `rows` rows each that packed sequences of `tokens` rows in all have, at least as many as there can be.  Their number, not
+// the longest sequence times the sequences, sets a launch: most of that would be workgroups without work where lengths differ.  Of up to 64 sequences,
+// which the kernels order by their lengths, the tiles follow one another without gaps; of more, sequence b's begin at place (its first row) / rows + b,
+// which leaves room for its last, partly filled one and is found without adding up the others.
+constexpr int SORTED_SEQUENCES = 64;
+inline long long tile_places(long long tokens, int batch, long long longest, int rows)
+{
+    const long long by_rows = tokens / rows + batch, by_length = batch * ((longest + rows - 1) / rows);
+    return batch <= SORTED_SEQUENCES ? std::min(by_rows, by_length) : by_rows;
+}
+FQ_BOTH int first_place(long long row, int rows, int b) { return (int)(row / rows) + b; }
+
+// Workgroup -> place, key head and one of its `members` (heads of the group).  Workgroups are dealt round-robin to the 8 XCDs.
+// The (place, key head)s go round them as well, with their members together: with a multiple of 8 key heads each head's keys and values are in one
+// XCD's L2, and with any number all XCDs have tiles of the longest sequence.
+struct TileUnit {
+    unsigned place, head_kv, member;
+};
+FQ_BOTH TileUnit tile_unit(unsigned id, unsigned members, unsigned heads_kv)
+{
+    const unsigned at = id / 8, unit = at / members * 8 + id % 8, place = unit / heads_kv;
+    return TileUnit{place, unit - place * heads_kv, at - at / members * members};
+}
+inline long long tile_workgroups(long long places, int members, int heads_kv) { return (places * heads_kv + 7) / 8 * 8 * members; }
+
 // How fq_attn_cache deals out its work.  A workgroup takes a tile of columns (query token, head of the group; 16 * tiles of them) of one
 // sequence and key head, and of its keys all or one of `splits` shares, `round` steps at a time: its waves take the steps of a round in turn, or (many
 // columns) each step together.
 constexpr int MAX_SPLITS = 256, CACHE_CUS = 256, WIDE_COLUMNS = 128;
 enum CacheOrder { CACHE_AS_GIVEN, CACHE_LONGEST_FIRST, CACHE_FOLDED };
 struct CachePlan {
-    int tiles, round, splits, blocks, order;      // blocks of columns; order of the sequences
+    int tiles, round, splits, order;      // order of the sequences
+    long long places;                     // many columns: for the tiles of all sequences, else 1
 };
-inline CachePlan cache_plan(int batch, int max_q, int max_len, int heads_q, int heads_kv)
+inline CachePlan cache_plan(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv)
 {
     const long long columns = (long long)max_q * (heads_q / heads_kv);
     const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : WIDE_COLUMNS / 16;
     const bool wide = tiles > 2;
-    const long long blocks = (columns + 16 * tiles - 1) / (16 * tiles), wgs = (long long)batch * heads_kv * blocks;
+    const long long places = wide ? tile_places((long long)tokens * (heads_q / heads_kv), batch, columns, WIDE_COLUMNS) : 1;
+    const long long wgs = std::max((wide ? places : batch) * heads_kv, 1LL);
     const int round = wide ? 1 : wgs <= CACHE_CUS ? 8 : 4;
     const long long rounds = ((long long)max_len + CACHE_STEP * round - 1) / (CACHE_STEP * round);
     const long long splits = std::min({wide ? rounds / 4 : rounds, (wide ? 2 * CACHE_CUS : CACHE_CUS) / wgs, (long long)MAX_SPLITS});
     // ordering them costs each workgroup about 0.4 us, too much for short ones
     const int order = wide || batch == 1 || batch > 64 || wgs <= CACHE_CUS || max_len < 1024 ? CACHE_AS_GIVEN : wgs <= 2 * CACHE_CUS ? CACHE_FOLDED : CACHE_LONGEST_FIRST;
-    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, (int)blocks, order};
+    return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, order, places};
 }
 
-// Whether the launches hold it: the kernel for many columns has all its workgroups along x, the join the query tokens along y.
-inline bool cache_holds(const CachePlan& p, int batch, int max_q, int heads_kv)
+// Whether the launches hold it.  (The kernel for many columns has all its workgroups along x.  The join has a sequence's query tokens along y: no more
+// than there are tokens, 32768 at most where there are shares to join.)
+inline bool cache_holds(const CachePlan& p, int heads_kv)
 {
-    const long long along_x = (long long)p.blocks * p.splits * (p.tiles > 2 ? (long long)batch * heads_kv : 1);
-    return along_x < (1LL << 31) && along_x * 512 < (1LL << 32) && (p.splits == 1 || max_q <= 65535);
+    const long long along_x = p.tiles > 2 ? tile_workgroups(p.places, p.splits, heads_kv) : p.splits;
+    return along_x * 512 < (1LL << 32);
 }
 
 // Keys of one share when `keys` are dealt over `splits` workgroups: whole rounds, so that the last shares may be empty.
@@ -114,46 +142,9 @@ FQ_BOTH int shares_used(int keys, int share) { return (int)(((unsigned)keys + sh
 
 // Queries of one head that a workgroup of the prompt's attention takes, 32 a wave.
 constexpr int PROMPT_WAVES = 4, PROMPT_ROWS = 32 * PROMPT_WAVES, PROMPT_THREADS = 64 * PROMPT_WAVES;
-inline long long prompt_tiles(int max_q) { return ((long long)max_q + PROMPT_ROWS - 1) / PROMPT_ROWS; }
-
-// Places for tiles of queries: at least as many as packed sequences of `tokens` rows in all can have tiles.  Their number, not the longest sequence
-// times the sequences, sets the launch: most of that would be workgroups without work where lengths differ.  Of up to 64 sequences, which the
-// kernel orders by their lengths, the tiles follow one another without gaps; of more, sequence b's begin at place cu_q[b] / 128 + b, which leaves
-// room for its last, partly filled one and is found without adding up the others.
-constexpr int PROMPT_SORTED = 64;
-inline long long prompt_places(int tokens, int batch, int max_q)
+inline long long prompt_workgroups(int tokens, int batch, int max_q, int heads_q, int heads_kv)
 {
-    const long long by_rows = tokens / PROMPT_ROWS + (long long)batch, by_length = batch * prompt_tiles(max_q);
-    return batch <= PROMPT_SORTED ? std::min(by_rows, by_length) : by_rows;
-}
-FQ_BOTH int prompt_first_place(int from, int tokens, int b) { return (from < 0 ? 0 : from > tokens ? tokens : from) / PROMPT_ROWS + b; }
-
-// Workgroup -> place, key head and head of its group.  Workgroups are dealt round-robin to the 8 XCDs.  The (place, key head)s go round them as
-// well, the heads of a group stay together: with a multiple of 8 key heads each head's keys and values are in one XCD's L2, and with any number all
-// XCDs have tiles of the longest sequence.
-struct PromptUnit {
-    unsigned place, head_kv, member;
-};
-FQ_BOTH PromptUnit prompt_unit(unsigned id, unsigned group, unsigned heads_kv)
-{
-    const unsigned at = id / 8, unit = at / group * 8 + id % 8, place = unit / heads_kv;
-    return PromptUnit{place, unit - place * heads_kv, at - at / group * group};
-}
-inline long long prompt_workgroups(long long places, int heads_q, int heads_kv) { return (places * heads_kv + 7) / 8 * 8 * (heads_q / heads_kv); }
-
-// Workgroup -> (sequence, key head) pair and one of its `items` (query tiles of the group's heads).  Workgroups are dealt round-robin to
-// the 8 XCDs: a pair stays on one of them, whose L2 then holds its keys and values, and the pairs go round the XCDs too, as
-// neighbouring ones (heads of one sequence) are equally long.  The last few pairs are split among all.
-struct PromptPlace {
-    unsigned pair, item;
-};
-FQ_BOTH PromptPlace prompt_place(unsigned id, unsigned items, unsigned pairs)
-{
-    const unsigned whole = pairs / 8 * 8, at = id / 8, xcd = id % 8;
-    if (id < whole * items) return PromptPlace{at / items * 8 + xcd, at % items};
-    const unsigned rest = (pairs - whole) * items, each = rest / 8, more = rest % 8, i = (id - whole * items) / 8;
-    const unsigned logical = xcd < more ? xcd * (each + 1) + i : more * (each + 1) + (xcd - more) * each + i;
-    return PromptPlace{whole + logical / items, logical % items};
+    return tile_workgroups(tile_places(tokens, batch, max_q, PROMPT_ROWS), heads_q / heads_kv, heads_kv);
 }
 
 }  // namespace fq

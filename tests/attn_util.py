@@ -76,7 +76,7 @@ def prompt_case(q, k, v, cu_q, cu_k, scale, causal, x):
     return exact, attention_bound(exact, spread, scores, int(np.diff(cu_k).max()), q.shape[2], np.abs(v).max() if len(v) else 0.0, x, HALF_STEP[x])
 
 
-def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
+def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, max_q=None):
     """Beyond attention_bound's, for up to 32 columns (query tokens times heads of a group): queries are rounded to 1 / 32512 of their
     head's largest magnitude (half a step is 1 / 65024 of it), which moves a score by `scores` / 65024 at most and a probability and the
     sum that divides it by as much each; and a step's product is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two
@@ -85,6 +85,6 @@ def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x):
     exact, spread = A.cache(q, cu_q, lens, table, kc, vc, ks, vs, scale), A.cache(q, cu_q, lens, table, kc, np.abs(vc.astype(np.int16)), ks, vs, scale)
     scores = scale * np.abs(q).max() * 128 * q.shape[2] * ks.max()
     bound = attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
-    if int(np.diff(cu_q).max()) * (q.shape[1] // kc.shape[1]) > 32:
+    if (max_q or int(np.diff(cu_q).max())) * (q.shape[1] // kc.shape[1]) > 32:
         return exact, bound + 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread
     return exact, bound + 2 * scores / 65024 * spread + 16 * 2.0**-24 * 1280 * vs.max()

@@ -59,7 +59,7 @@ def test_append_refusals(args, code):
     (dict(Y=None), NULL), (dict(ldy=8), SHAPE), (dict(cu_q=None), NULL), (dict(lens=None), NULL), (dict(lens=P + 1), ALIGN), (dict(max_q=0), SHAPE),
     (dict(max_len=0), SHAPE), (dict(max_len=-5), SHAPE), (dict(max_q=1 << 27), RANGE), (dict(k_scale=P + 4), ALIGN), (dict(pages=-1), SHAPE),
     (dict(page_size=16), SHAPE), (dict(table_width=1 << 30), RANGE), (dict(workspace=None), NULL), (dict(workspace=P + 8), ALIGN), (dict(workspace_bytes=15), WORKSPACE),
-    (dict(batch=65535, max_q=100000), RANGE)])
+    (dict(batch=65535, max_q=100000, tokens=(1 << 31) - 1), RANGE)])
 def test_cache_attention_refusals(args, code):
     assert cache(**args) == code
 
@@ -67,7 +67,7 @@ def test_cache_attention_refusals(args, code):
 @pytest.mark.parametrize("args,code", [
     (dict(x_dtype=fq.FQ_F32), DTYPE), (dict(scale=0.0), RANGE), (dict(scale=float("inf")), RANGE), (dict(K=None), NULL), (dict(V=P + 2), ALIGN), (dict(ldk=1 << 23), RANGE),
     (dict(ldv=100), SHAPE), (dict(Y=None), NULL), (dict(ldy=513), SHAPE), (dict(cu_q=None), NULL), (dict(cu_k=P + 3), ALIGN), (dict(max_q=0), SHAPE),
-    (dict(tokens_k=-1), SHAPE), (dict(batch=65535, max_q=2**31 - 1), RANGE)])
+    (dict(tokens_k=-1), SHAPE), (dict(batch=65535, max_q=2**31 - 1, tokens_q=2**31 - 1), RANGE)])
 def test_prompt_attention_refusals(args, code):
     assert prompt(**args) == code
 

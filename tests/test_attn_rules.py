@@ -1,6 +1,7 @@
 """What the attention kernels make of device-resident offsets, lengths and page tables (csrc/fq_attn_rules.h), compiled with the host
 compiler and walked on the CPU: every address they form comes from these."""
 import ctypes
+import random
 import os
 import shutil
 import subprocess
@@ -34,16 +35,19 @@ extern "C" int keys(int len, int max_len, int capacity) { return cached_keys(len
 extern "C" int visible(int keys, int n, int i) { return visible_keys(keys, n, i); }
 extern "C" int share(int keys, int splits, int round) { return share_keys(keys, splits, round); }
 extern "C" int used(int keys, int share) { return shares_used(keys, share); }
-extern "C" void plan(int batch, int max_q, int max_len, int heads_q, int heads_kv, int* out)
+extern "C" void plan(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv, long long* out)
 {
-    const CachePlan p = cache_plan(batch, max_q, max_len, heads_q, heads_kv);
-    out[0] = p.tiles; out[1] = p.round; out[2] = p.splits; out[3] = p.blocks; out[4] = cache_holds(p, batch, max_q, heads_kv);
+    const CachePlan p = cache_plan(batch, tokens, max_q, max_len, heads_q, heads_kv);
+    out[0] = p.tiles; out[1] = p.round; out[2] = p.splits; out[3] = cache_holds(p, heads_kv); out[4] = p.places;
 }
-extern "C" void place(unsigned id, unsigned items, unsigned pairs, unsigned* out)
+extern "C" void unit(unsigned id, unsigned members, unsigned heads_kv, unsigned* out)
 {
-    const PromptPlace p = prompt_place(id, items, pairs);
-    out[0] = p.pair; out[1] = p.item;
+    const TileUnit u = tile_unit(id, members, heads_kv);
+    out[0] = u.place; out[1] = u.head_kv; out[2] = u.member;
 }
+extern "C" long long places(long long tokens, int batch, long long longest, int rows) { return tile_places(tokens, batch, longest, rows); }
+extern "C" long long workgroups(long long places, int members, int heads_kv) { return tile_workgroups(places, members, heads_kv); }
+extern "C" int first(long long row, int rows, int b) { return first_place(row, rows, b); }
 """
 
 
@@ -58,7 +62,10 @@ def rules(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-static-libubsan",
                     "-shared", "-fPIC", "-I", CSRC, "-o", so, src], check=True)
     lib = ctypes.CDLL(so)
-    lib.touched.restype = ctypes.c_longlong
+    lib.touched.restype = lib.places.restype = lib.workgroups.restype = ctypes.c_longlong
+    lib.places.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.c_int]
+    lib.workgroups.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
+    lib.first.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
     return lib
 
 
@@ -134,43 +141,73 @@ def test_shares_cover_all_keys_in_whole_steps(rules, waves):
 
 
 def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
-    out = (ctypes.c_int * 5)()
+    out = (ctypes.c_longlong * 5)()
     for batch in (1, 4, 64, 65535):
         for max_q in (1, 5, 512, 65472):
             for max_len in (1, 256, 257, 8192, 2**30):
                 for hq, hkv in ((1, 1), (64, 8), (64, 64), (16384, 1)):
                     if max_q * hq >= 2**30:
                         continue
-                    rules.plan(batch, max_q, max_len, hq, hkv, out)
-                    tiles, rnd, splits, blocks, holds = out
-                    assert blocks == -(-max_q * (hq // hkv) // (16 * tiles))
+                    tokens = min(batch * max_q, HI)
+                    rules.plan(batch, tokens, max_q, max_len, hq, hkv, out)
+                    tiles, rnd, splits, holds, places = out
                     columns = max_q * (hq // hkv)
-                    wgs = batch * hkv * -(-columns // (16 * tiles))
-                    assert tiles in (1, 2, 8) and (tiles == 8 or columns <= 16 * tiles) and rnd == (1 if tiles == 8 else 8 if wgs <= 256 else 4)
+                    assert tiles in (1, 2, 8) and (tiles == 8 or columns <= 16 * tiles)
+                    if tiles == 8:
+                        assert places == rules.places(tokens * (hq // hkv), batch, columns, 128) and places > 0
+                    wgs = hkv * (places if tiles == 8 else batch)
+                    assert rnd == (1 if tiles == 8 else 8 if wgs <= 256 else 4)
                     assert 1 <= splits <= 256 and (splits - 1) * 64 * rnd < max_len
                     assert splits == 1 or wgs * splits <= (512 if tiles == 8 else 256)
-                    assert holds == (blocks * splits * (batch * hkv if tiles == 8 else 1) * 512 < 2**32) and (splits == 1 or max_q <= 65535)
+                    along_x = -(-wgs // 8) * 8 * splits if tiles == 8 else splits
+                    assert holds == (along_x * 512 < 2**32)
+                    assert splits == 1 or min(max_q, tokens) <= 65535      # the join has the query tokens along y
 
 
-@pytest.mark.parametrize("items,pairs", [(1, 1), (1, 7), (3, 8), (5, 9), (16, 23), (2, 64), (7, 1), (64, 3)])
-def test_prompt_places_are_each_taken_once_and_pairs_stay_on_an_xcd(rules, items, pairs):
-    out = (ctypes.c_uint * 2)()
-    seen, xcds = set(), {}
-    for i in range(items * pairs):
-        rules.place(i, items, pairs, out)
-        assert out[0] < pairs and out[1] < items
-        seen.add((out[0], out[1]))
-        xcds.setdefault(out[0], set()).add(i % 8)
-    assert len(seen) == items * pairs
-    assert all(len(xcds[p]) == 1 for p in range(pairs // 8 * 8))
+@pytest.mark.parametrize("rows", [16, 128])
+@pytest.mark.parametrize("batch", [1, 2, 7, 64, 65, 300, 5000])
+def test_every_tile_of_every_sequence_has_a_place(rules, batch, rows):
+    r = random.Random(1000 * batch + rows)
+    for longest in (1, rows - 1, rows, rows + 1, 10 * rows + 3):
+        for lens in ([longest] * batch, [r.randrange(longest + 1) for _ in range(batch)], [longest] + [0] * (batch - 1), [0] * (batch - 1) + [longest]):
+            tiles, tokens = [-(-n // rows) for n in lens], sum(lens)
+            places = rules.places(tokens, batch, longest, rows)
+            assert sum(tiles) <= places <= tokens // rows + batch
+            if batch <= 64:
+                assert places <= batch * -(-longest // rows)
+                continue
+            row = 0
+            for b, n in enumerate(lens):      # a sequence's tiles end before the next one's first place
+                behind = rules.first(row + n, rows, b + 1)
+                assert rules.first(row, rows, b) + tiles[b] <= behind <= places
+                row += n
 
 
-def test_prompt_places_of_a_launch_of_2_to_the_31_workgroups(rules):
-    out = (ctypes.c_uint * 2)()
-    for items, pairs in ((2**15, 65535), (2**31 - 1, 1), (1, 2**31 - 1), (2**24, 127)):
-        for i in (0, 7, items * pairs // 2, items * pairs - 1):
-            rules.place(i, items, pairs, out)
-            assert out[0] < pairs and out[1] < items
+@pytest.mark.parametrize("places,members,heads_kv", [(1, 1, 1), (1, 7, 1), (3, 8, 5), (5, 9, 8), (16, 2, 12), (2, 64, 40), (7, 1, 3), (64, 8, 8)])
+def test_units_are_each_taken_once_and_a_heads_members_stay_on_an_xcd(rules, places, members, heads_kv):
+    out, seen, xcds, taken = (ctypes.c_uint * 3)(), set(), {}, [0] * 8
+    for i in range(rules.workgroups(places, members, heads_kv)):
+        rules.unit(i, members, heads_kv, out)
+        place, head, member = out
+        assert head < heads_kv and member < members
+        if place < places:
+            seen.add((place, head, member))
+            xcds.setdefault((place, head), set()).add(i % 8)
+            xcds.setdefault(head, set()).add(i % 8)
+            taken[i % 8] += 1
+    assert len(seen) == places * members * heads_kv == sum(taken)
+    assert all(len(x) == 1 for k, x in xcds.items() if isinstance(k, tuple) or heads_kv % 8 == 0)
+    assert max(taken) - min(taken) <= members
+
+
+def test_units_of_a_launch_of_2_to_the_31_workgroups(rules):
+    out = (ctypes.c_uint * 3)()
+    for places, members, heads_kv in ((2**15, 65535, 1), (2**31 - 8, 1, 1), (1, 1, 2**31 - 8), (2**24, 127, 1), (2**10, 2**8, 2**12)):
+        n = rules.workgroups(places, members, heads_kv)
+        assert places * members * heads_kv <= n < 2**31 + 2**20
+        for i in (0, 7, n // 2, n - 1):
+            rules.unit(i, members, heads_kv, out)
+            assert out[1] < heads_kv and out[2] < members and out[0] * heads_kv + out[1] <= -(-places * heads_kv // 8) * 8
 
 
 @pytest.mark.parametrize("page", [64, 128])

@@ -107,7 +107,7 @@ def test_append_token_by_token_grows_the_scales():
 
 
 # ------------------------------------------------------------------------------------------------
-def _cache_both(rng, x, dim, page, heads_q, heads_kv, lens, queries, scale=None, max_len=None, spare_rows=0, bad=(), stream=None, q_scale=1.0):
+def _cache_both(rng, x, dim, page, heads_q, heads_kv, lens, queries, scale=None, max_len=None, spare_rows=0, bad=(), stream=None, q_scale=1.0, max_q=None):
     scale = dim ** -0.5 if scale is None else scale
     tokens = int(sum(queries)) + spare_rows
     q, qn = U.packed(rng, tokens, heads_q, dim, x, pad=32, scale=q_scale)
@@ -118,14 +118,14 @@ def _cache_both(rng, x, dim, page, heads_q, heads_kv, lens, queries, scale=None,
     used = table[(table >= 0) & (table < pages)]
     idle = np.setdiff1d(np.arange(pages), used)
     ks[idle], vs[idle] = np.nan, np.inf
-    cu, max_len = U.offsets(queries), max_len or max(1, max(lens))
+    cu, max_len, max_q = U.offsets(queries), max_len or max(1, max(lens)), max_q or max(queries)
     y = torch.full((tokens, heads_q, dim), 7.0, dtype=q.dtype, device=U.DEV)
-    ws = torch.full((fq.fq_attn_cache_workspace_bytes(len(lens), tokens, max(queries), max_len, heads_q, heads_kv, dim),), 0xFF, dtype=torch.uint8, device=U.DEV)
+    ws = torch.full((fq.fq_attn_cache_workspace_bytes(len(lens), tokens, max_q, max_len, heads_q, heads_kv, dim),), 0xFF, dtype=torch.uint8, device=U.DEV)
     print(f"[cache] {x} dim={dim} page={page} heads={heads_q}/{heads_kv} lens={lens} queries={queries} ws={ws.numel()}", flush=True)
-    fq.fq_attn_cache(q, U.i32(cu), U.i32(lens), max(queries), max_len, *U.to_dev(kc, vc, ks, vs), U.i32(table), scale, y, ws)
+    fq.fq_attn_cache(q, U.i32(cu), U.i32(lens), max_q, max_len, *U.to_dev(kc, vc, ks, vs), U.i32(table), scale, y, ws)
     torch.cuda.synchronize()
     ks[idle], vs[idle] = 0.0, 0.0
-    exact, bound = U.cache_case(qn, cu, lens, table, kc, vc, ks, vs, scale, x)
+    exact, bound = U.cache_case(qn, cu, lens, table, kc, vc, ks, vs, scale, x, max_q)
     n = int(sum(queries))
     U.check(y[:n], exact[:n], bound[:n], "cache")
     assert (y[n:] == 7.0).all()
@@ -175,6 +175,23 @@ def test_cache_attention_of_many_uneven_sequences(batch, heads):
     _cache_both(rng, "bf16", 64, 64, heads, heads, lens, [1] * batch, max_len=1024)
 
 
+@pytest.mark.parametrize("batch,heads", [(3, (8, 1)), (40, (4, 2)), (64, (12, 3)), (65, (8, 8)), (150, (5, 1))])
+def test_cache_attention_of_pieces_beside_single_tokens(batch, heads):
+    """Some sequences with many new tokens, most with one, some with none: up to 64 go by their length, more as they come."""
+    rng = np.random.default_rng(batch)
+    lens = [int(n) for n in rng.integers(0, 150, batch)]
+    queries = [min(1, n) for n in lens]
+    lens[batch // 2], queries[batch // 2] = 400, 300
+    lens[-1], queries[-1] = 130, 67
+    _cache_both(rng, "bf16", 64, 64, *heads, lens, queries, spare_rows=2)
+
+
+def test_cache_attention_with_a_bound_of_queries_far_above_them():
+    rng = np.random.default_rng(31)
+    _cache_both(rng, "f16", 64, 64, 4, 2, [1500, 80], [1, 1], spare_rows=200, max_q=100000)      # in shares, too
+    _cache_both(rng, "f16", 64, 64, 4, 2, [80] * 70, [1] * 70, max_q=100000)
+
+
 @pytest.mark.parametrize("spread", [1.0, 12.0, 30.0])
 def test_cache_attention_of_many_columns_over_pages_of_very_different_scales(spread):
     """Values' scales up to a factor e^60 apart between neighbouring pages, and pages of zeros."""
@@ -203,7 +220,7 @@ def test_cache_attention_of_large_and_small_queries(x, q_scale, scale):
 
 
 # ------------------------------------------------------------------------------------------------
-def _prompt_both(rng, x, dim, heads_q, heads_kv, queries, keys, causal, scale=None, pad=16, spare=3, q_scale=1.0):
+def _prompt_both(rng, x, dim, heads_q, heads_kv, queries, keys, causal, scale=None, pad=16, spare=3, q_scale=1.0, max_q=None):
     scale = dim ** -0.5 if scale is None else scale
     q, qn = U.packed(rng, int(sum(queries)) + spare, heads_q, dim, x, pad=pad, scale=q_scale)
     k, kn = U.packed(rng, int(sum(keys)) + spare, heads_kv, dim, x, pad=2 * pad)
@@ -212,7 +229,7 @@ def _prompt_both(rng, x, dim, heads_q, heads_kv, queries, keys, causal, scale=No
     k[cu_k[-1]:], v[cu_k[-1]:] = float("nan"), float("inf")       # behind the last sequence
     y = torch.full((q.shape[0], heads_q, dim), 7.0, dtype=q.dtype, device=U.DEV)
     print(f"[prompt] {x} dim={dim} heads={heads_q}/{heads_kv} queries={queries} keys={keys} causal={causal}", flush=True)
-    fq.fq_attn_prompt(q, k, v, U.i32(cu_q), U.i32(cu_k), max(queries), scale, y, causal=causal)
+    fq.fq_attn_prompt(q, k, v, U.i32(cu_q), U.i32(cu_k), max_q or max(max(queries), 1), scale, y, causal=causal)
     torch.cuda.synchronize()
     n, m = cu_q[-1], cu_k[-1]
     exact, bound = U.prompt_case(qn[:n], kn[:m], vn[:m], cu_q, cu_k, scale, causal, x)
@@ -242,6 +259,26 @@ def test_prompt_attention_of_many_sequences(batch):
     lens[batch // 3] = 150
     _prompt_both(rng, "bf16", 64, 3, 1, lens, lens, True)
     _prompt_both(rng, "f16", 64, 1, 1, [n // 2 for n in lens], lens, False)
+
+
+@pytest.mark.parametrize("batch,heads", [(5, (12, 12)), (20, (3, 1)), (70, (2, 2))])
+def test_prompt_attention_of_one_long_sequence_among_short_ones(batch, heads):
+    rng = np.random.default_rng(batch)
+    lens = [int(n) for n in rng.integers(0, 20, batch)]
+    lens[1], lens[batch - 2] = 700, 128
+    _prompt_both(rng, "bf16", 64, *heads, lens, lens, True, spare=300)
+    _prompt_both(rng, "bf16", 64, *heads, lens, [n + 9 for n in lens], True, max_q=1 << 30)
+    _prompt_both(rng, "bf16", 64, *heads, [n // 2 for n in lens], lens, False)
+
+
+@pytest.mark.parametrize("batch", [3, 100])
+def test_prompt_attention_of_a_batch_without_queries(batch):
+    rng = np.random.default_rng(3)
+    q, k = U.packed(rng, 300, 2, 64, "bf16")[0], U.packed(rng, 3 * batch, 1, 64, "bf16")[0]
+    y = torch.full_like(q, 7.0)
+    fq.fq_attn_prompt(q, k, k, U.i32([0] * (batch + 1)), U.i32([3 * b for b in range(batch + 1)]), 100, 0.1, y)
+    torch.cuda.synchronize()
+    assert (y == 7.0).all()
 
 
 @pytest.mark.parametrize("heads", [(1, 1), (7, 1), (5, 5), (16, 8)])
