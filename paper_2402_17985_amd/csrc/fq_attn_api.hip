@@ -98,7 +98,7 @@ int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int t
         if (!aligned16(rope_cos) || !aligned16(rope_sin)) return fail(FQ_ERR_ALIGN, "rope_cos or rope_sin is not 16-byte aligned");
         if (rope_rows <= 0) return fail(FQ_ERR_SHAPE, "rope_rows = %d must be positive", rope_rows);
     }
-    const long long places = batch * pages_touched(max_new, page_size) * ((Q_out ? 3 : 2) * heads_kv);
+    const long long places = append_pages(batch, tokens, max_new, page_size).places * ((Q_out ? 3 : 2) * heads_kv);
     if (!launch_holds(places, append_plan(max_new, page_size, head_dim).threads))
         return fail(FQ_ERR_RANGE, "%d sequences of up to %d new tokens are more than one launch holds", batch, max_new);
     if (tokens == 0) return FQ_OK;

@@ -46,6 +46,21 @@ FQ_BOTH Fill page_fill(Rows r, int past, int j, int page, int capacity)
 // Pages that `tokens` tokens can touch, wherever the first one lies in its page.
 inline long long pages_touched(int tokens, int page) { return ((long long)tokens + page - 2) / page + 1; }
 
+// The pages that an append's workgroups look at.  As many for each sequence as max_new tokens can touch; or, where that is twice what all tokens' rows
+// can need, place by place: sequence b's pages begin at place cu_new[b] / page + 2 b (n tokens touch n / page + 2 pages at most, rounded down).
+// us, so many for each / place by place: 64 sequences, one with 4096 new tokens and 63 with one, 40 heads, 411 / 84; one with 512, 64 heads over 8, 21 / 18;
+// 30 of 10 to 1000 tokens (1.7 times what they need), 32 heads over 8, 114 / 118.
+struct AppendPages {
+    long long places;
+    int each;      // of a sequence, or 0: place by place
+};
+inline AppendPages append_pages(int batch, int tokens, int max_new, int page)
+{
+    const long long each = pages_touched(max_new, page), by_rows = tokens / page + 2LL * batch;
+    return 2 * by_rows < batch * each ? AppendPages{by_rows, 0} : AppendPages{batch * each, (int)each};
+}
+FQ_BOTH int first_page_place(int row, int page, int b) { return row / page + 2 * b; }
+
 // An append's workgroup takes what one call adds to a page of one head: 8 elements a thread where 512 threads are enough for the most new
 // tokens (64 sequences, one token each, 64 heads over 8: 5.2 us with 64 threads, 7.2 with 256), else up to 32 and four threads a token of the page.
 struct AppendPlan {

@@ -21,7 +21,7 @@ struct Append {
     const float *cosine, *sine;
     int8_t *k_cache, *v_cache;
     float *k_scale, *v_scale;
-    int tokens, max_new, heads_kv, group, half, interleaved, capacity, pages, page, width, parts, slots;      // parts: key heads times two (keys, values) or three (queries too)
+    int tokens, max_new, heads_kv, group, half, interleaved, capacity, pages, page, width, parts, batch, each;      // parts: key heads times two (keys, values) or three (queries too)
 };
 
 template <int DT> __device__ __forceinline__ void load8(const typename Stored<DT>::type* base, uint32_t at, float* out)
@@ -125,7 +125,9 @@ __global__ __launch_bounds__(4 * MAX_PAGE, TURN == TURN_HALVES ? (DT == FQ_F32 ?
     __shared__ __attribute__((aligned(16))) uint8_t staged[MAX_PAGE * LDS_ROW];
     // the heads of the same tokens one after the other: together they read and write whole rows
     const unsigned at_page = blockIdx.x / a.parts, part = blockIdx.x - at_page * a.parts;
-    const int b = at_page / a.slots, j = at_page - b * a.slots, kind = part / a.heads_kv, h = part - kind * a.heads_kv;
+    const auto first_of = [&](int b) { return first_page_place(min(max(a.cu_new[b], 0), a.tokens), a.page, b); };
+    const int b = a.each ? at_page / a.each : sequence_at(at_page, a.batch, first_of), j = a.each ? (int)at_page - b * a.each : (int)at_page - first_of(b);
+    const int kind = part / a.heads_kv, h = part - kind * a.heads_kv;
     const int tid = threadIdx.x, threads = blockDim.x;
     const Fill f = page_fill(packed_rows(a.cu_new[b], a.cu_new[b + 1], a.tokens, a.max_new), a.past[b], j, a.page, a.capacity);
     const int m = f.slot1 - f.slot0;
@@ -256,9 +258,8 @@ template <int DT, int D, bool FEW> void launch_turn(const Append& a, unsigned gr
     else kv_append_kernel<DT, D, TURN_ANY, FEW><<<grid, threads, 0, stream>>>(a);
 }
 
-template <int DT, int D> int launch(const Append& a, int batch, hipStream_t stream)
+template <int DT, int D> int launch(const Append& a, unsigned grid, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)((long long)batch * a.slots * a.parts);
     const AppendPlan plan = append_plan(a.max_new, a.page, D);
     if (plan.few) launch_turn<DT, D, true>(a, grid, plan.threads, stream);
     else launch_turn<DT, D, false>(a, grid, plan.threads, stream);
@@ -266,13 +267,13 @@ template <int DT, int D> int launch(const Append& a, int batch, hipStream_t stre
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache append launch failed: %s", hipGetErrorString(e));
 }
 
-template <int DT> int launch_dim(const Append& a, int head_dim, int batch, hipStream_t stream)
+template <int DT> int launch_dim(const Append& a, int head_dim, unsigned grid, hipStream_t stream)
 {
     switch (head_dim) {
-    case 64: return launch<DT, 64>(a, batch, stream);
-    case 80: return launch<DT, 80>(a, batch, stream);
-    case 96: return launch<DT, 96>(a, batch, stream);
-    default: return launch<DT, 128>(a, batch, stream);
+    case 64: return launch<DT, 64>(a, grid, stream);
+    case 80: return launch<DT, 80>(a, grid, stream);
+    case 96: return launch<DT, 96>(a, grid, stream);
+    default: return launch<DT, 128>(a, grid, stream);
     }
 }
 
@@ -286,13 +287,15 @@ int launch_kv_append(const void* Q, const void* K, const void* V, int x_dtype, i
 {
     int capacity = table_width * page_size;
     if (rope_dim > 0) capacity = std::min(capacity, rope_rows);
+    const AppendPages places = append_pages(batch, tokens, max_new, page_size);
     const Append a{Q, K, V, Q_out, K_out, ldq, ldk, ldv, ldqo, ldko, cu_new, past, page_table, rope_cos, rope_sin, k_cache, v_cache,
                    k_scale, v_scale, tokens, max_new, heads_kv, heads_q / heads_kv, rope_dim / 2, interleaved, capacity, pages, page_size,
-                   table_width, (Q_out ? 3 : 2) * heads_kv, (int)pages_touched(max_new, page_size)};
+                   table_width, (Q_out ? 3 : 2) * heads_kv, batch, places.each};
+    const unsigned grid = (unsigned)(places.places * a.parts);
     switch (x_dtype) {
-    case FQ_F32: return launch_dim<FQ_F32>(a, head_dim, batch, stream);
-    case FQ_F16: return launch_dim<FQ_F16>(a, head_dim, batch, stream);
-    default: return launch_dim<FQ_BF16>(a, head_dim, batch, stream);
+    case FQ_F32: return launch_dim<FQ_F32>(a, head_dim, grid, stream);
+    case FQ_F16: return launch_dim<FQ_F16>(a, head_dim, grid, stream);
+    default: return launch_dim<FQ_BF16>(a, head_dim, grid, stream);
     }
 }
 

@@ -49,7 +49,7 @@ def test_shared_refusals(call, args, code):
     (dict(rope_cos=None), NULL), (dict(rope_sin=P + 8), ALIGN), (dict(rope_rows=0), SHAPE), (dict(k_cache=None), NULL), (dict(v_cache=P + 8), ALIGN),
     (dict(k_scale=None), NULL), (dict(v_scale=P + 4), ALIGN), (dict(pages=0), SHAPE), (dict(page_size=32), SHAPE), (dict(page_size=96), SHAPE),
     (dict(page_size=256), SHAPE), (dict(page_table=None), NULL), (dict(table_width=0), SHAPE), (dict(table_width=(1 << 24) + 1), RANGE),
-    (dict(batch=65535, max_new=2**31 - 1), RANGE)])
+    (dict(batch=65535, max_new=2**31 - 1, tokens=2**31 - 1), RANGE)])
 def test_append_refusals(args, code):
     assert append(**args) == code
 

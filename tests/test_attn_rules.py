@@ -45,6 +45,12 @@ extern "C" void unit(unsigned id, unsigned members, unsigned heads_kv, unsigned*
     const TileUnit u = tile_unit(id, members, heads_kv);
     out[0] = u.place; out[1] = u.head_kv; out[2] = u.member;
 }
+extern "C" void pages(int batch, int tokens, int max_new, int page, long long* out)
+{
+    const AppendPages p = append_pages(batch, tokens, max_new, page);
+    out[0] = p.places; out[1] = p.each;
+}
+extern "C" int first_page(int row, int page, int b) { return first_page_place(row, page, b); }
 extern "C" long long places(long long tokens, int batch, long long longest, int rows) { return tile_places(tokens, batch, longest, rows); }
 extern "C" long long workgroups(long long places, int members, int heads_kv) { return tile_workgroups(places, members, heads_kv); }
 extern "C" int first(long long row, int rows, int b) { return first_place(row, rows, b); }
@@ -181,6 +187,26 @@ def test_every_tile_of_every_sequence_has_a_place(rules, batch, rows):
                 behind = rules.first(row + n, rows, b + 1)
                 assert rules.first(row, rows, b) + tiles[b] <= behind <= places
                 row += n
+
+
+@pytest.mark.parametrize("page", [64, 128])
+@pytest.mark.parametrize("batch", [1, 2, 30, 64, 65, 3000])
+def test_every_page_of_every_append_has_a_place(rules, batch, page):
+    r, out, forms = random.Random(batch + page), (ctypes.c_longlong * 2)(), set()
+    for longest in (1, 2, page, page + 1, page + 2, 20 * page + 5):
+        for new in ([longest] * batch, [r.randrange(longest + 1) for _ in range(batch)], [longest] + [1] * (batch - 1), [1] * (batch - 1) + [longest]):
+            rules.pages(batch, sum(new), max(new + [1]), page, out)
+            places, each = out
+            forms.add(each > 0)
+            if each:
+                assert places == batch * each and each == rules.touched(max(new + [1]), page)
+                continue
+            row = 0
+            for b, n in enumerate(new):
+                touched = rules.touched(n, page) if n else 0
+                assert rules.first_page(row, page, b) + touched <= rules.first_page(row + n, page, b + 1) <= places
+                row += n
+    assert forms == ({True} if batch == 1 else {True, False})
 
 
 @pytest.mark.parametrize("places,members,heads_kv", [(1, 1, 1), (1, 7, 1), (3, 8, 5), (5, 9, 8), (16, 2, 12), (2, 64, 40), (7, 1, 3), (64, 8, 8)])

@@ -76,6 +76,15 @@ def test_append_in_place_spare_rows_and_long_groups():
     _append_both(rng, "f16", 128, 128, 64, 1, [127, 1], [2, 250], 128, True, spare_rows=130)
 
 
+@pytest.mark.parametrize("batch,page", [(20, 64), (64, 128), (65, 64), (200, 64)])
+def test_append_of_a_long_prompt_beside_single_tokens(batch, page):
+    rng = np.random.default_rng(batch)
+    past, new = [int(n) for n in rng.integers(0, 150, batch)], [int(n) for n in rng.integers(0, 3, batch)]
+    new[batch // 2], new[-1] = 8 * page + 30, page + 1
+    _append_both(rng, "bf16", 64, page, 2, 1, past, new, 64, False, spare_rows=3)
+    _append_both(rng, "f16", 64, page, 2, 2, [0] * batch, new[::-1], 0, False)
+
+
 @pytest.mark.parametrize("scale", [0.0, 1e-39, 1e-20, 1e4])
 def test_append_of_tiny_huge_and_zero_values(scale):
     _append_both(np.random.default_rng(2), "f32", 64, 64, 2, 2, [0, 10, 64], [70, 3, 1], 64, False, scale=scale)
