@@ -396,7 +396,8 @@ int fq_gemm_select(int variant);
  * Packed arrays: Q [tokens, heads_q, head_dim], K, V [tokens, heads_kv, head_dim]; heads dense, token stride ldq / ldk / ldv
  *   elements (views into the rows of a fused projection), a multiple of 16 bytes; heads_q a multiple of heads_kv:
  *   query head i reads key head i / (heads_q / heads_kv).  head_dim 64, 80, 96 or 128.  Sequence b's rows are
- *   cu[b] .. cu[b + 1] - 1 (cu int32 [batch + 1], device, ascending from 0); rows behind the last sequence are left as they were.
+ *   cu[b] .. cu[b + 1] - 1 (cu int32 [batch + 1], device, from 0 and never falling, else rows may be left out); rows behind the last
+ *   sequence are left as they were.
  * Cache: pages of page_size (64 or 128) tokens, 8-bit codes with one scale for each page and head,
  *   k_cache [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size] (transposed within a page:
  *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv], finite and not negative; an element is code * scale.
@@ -425,8 +426,8 @@ int fq_gemm_select(int variant);
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
  *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider, probabilities enter the second
  *   product as fp16; with up to 32 columns (query tokens times heads of a group) queries enter the first as integers of 1 / 32512 of their
- *   head's largest magnitude.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they,
- *   not the lengths on the device, set the launch, so a captured call may be replayed with other lengths within them.
+ *   head's largest magnitude.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they
+ *   and the number of rows, not the values on the device, set the launch, so a captured call may be replayed with other sequences within them.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
  *   Calls that overlap (different streams) need a workspace each; calls and graphs that follow one another may share one.
  *   Y may be Q itself (same address and stride), else it must not overlap the inputs.

@@ -13,12 +13,12 @@
 // No operand passes through LDS: which key of the page stands in which row of the first product is free, and with key
 // 16 (r / 4) + 4 t + r % 4 in row r of tile t a lane's scores are those of 16 consecutive keys, the very ones whose values it
 // reads as 16 consecutive bytes of a dimension (the cache holds values transposed for that) in the second product.
-// Each wave has a step of keys and values under way while it works on the one before, 16 KiB for heads of 128; eight waves a CU, in one workgroup
-// where there are few (its own waves share the keys of one sequence and head, their parts meet in LDS), in two otherwise.
-// Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 189 us, 5.7 TB/s (a large sum reads 6.0); two of 131072 tokens 95 us and
-// 5 for the join of 16 shares, 5.6 TB/s; one of 1001 tokens, 32 heads, 11.7 us: 2.5 to the first scores, then 3 for each round of 512 keys (128
-// KiB through one CU), 0.8 until the waves have met.  Two steps under way instead of one, or the first step's loads before the queries', took up to
-// 1 us more on short sequences, as longer code has to come in first, and no less on long ones.
+// Each wave has a step of keys and values under way while it works on the one before, 16 KiB for heads of 128.  The waves of a workgroup share the keys
+// of one sequence and head, their parts meet in LDS; few workgroups share them once more, and a second kernel joins the shares.
+// Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 181 to 190 us, 5.7 to 5.9 TB/s (a large sum reads 6.0); two of 131072 tokens 97 us, 5.5 TB/s,
+// 5 us of it the join of 16 shares; one of 1001 tokens, 32 heads, 8.9 us, a chain of latencies: 2.5 to the first scores, 3 for 256 keys through one CU, the
+// second launch.  Two steps under way instead of one, or the first step's loads before the queries', took up to 1 us more on short sequences, as
+// longer code has to come in first, and no less on long ones.
 #include "fq_attn_cache.h"
 
 namespace fq {
@@ -433,9 +433,8 @@ template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, un
     if (tiles * 16 == WIDE_COLUMNS) {
         const int rc = launch_attn_cache_wide(a, DT, D, batch, wide_grid, stream);
         if (rc) return rc;
-    } else if (tiles == 1 && a.round == 8) attn_cache_kernel<DT, D, 1, 8><<<grid, 512, 0, stream>>>(a);
+    } else if (tiles == 1 && a.round == 2) attn_cache_kernel<DT, D, 1, 2><<<grid, 128, 0, stream>>>(a);
     else if (tiles == 1) attn_cache_kernel<DT, D, 1, 4><<<grid, 256, 0, stream>>>(a);
-    else if (a.round == 8) attn_cache_kernel<DT, D, 2, 8><<<grid, 512, 0, stream>>>(a);
     else attn_cache_kernel<DT, D, 2, 4><<<grid, 256, 0, stream>>>(a);
     if (a.splits > JOIN_FEW) attn_cache_join_many_kernel<DT, D><<<dim3((unsigned)a.heads_q, (unsigned)std::min(a.max_q, a.tokens), (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
     else if (a.splits > 4) join<DT, D, JOIN_FEW>(a, batch, stream);

@@ -221,7 +221,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         }
         float m = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
-        for (int e = 1; e < 16; ++e) m = fmaxf(m, fmaxf(s[0][e], s[1][e]));
+        for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
         m = __builtin_fmaf(over_halves_max(m), f, -shift);
         if (__ballot(top == -INFINITY || m - top > SLACK)) {
             const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - now);

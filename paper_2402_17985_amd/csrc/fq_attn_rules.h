@@ -131,11 +131,17 @@ inline CachePlan cache_plan(int batch, int tokens, int max_q, int max_len, int h
     const bool wide = tiles > 2;
     const long long places = wide ? tile_places((long long)tokens * (heads_q / heads_kv), batch, columns, WIDE_COLUMNS) : 1;
     const long long wgs = std::max((wide ? places : batch) * heads_kv, 1LL);
-    const int round = wide ? 1 : wgs <= CACHE_CUS ? 8 : 4;
+    // Four waves; two where a CU has one workgroup, of one tile of columns, and the longest share is long: fewer streams a CU then
+    // read the cache faster.  us, two / four, 64 heads over 8: two sequences of 131072 tokens 97.5 / 99.8, 8 of 16384 44.5 / 48.0, 32 of 4096 41.5 / 44.1; but one of
+    // 16384 (shares of 512) 13.4 / 12.7, 20 of up to 1200 13.8 / 11.1, two column tiles of 8 x 32768 106 / 102.  (Eight: 1001 tokens 11.7 / 8.7, 8192 13.2 / 10.1.)
+    const bool few = wgs <= CACHE_CUS;
+    const int round = wide ? 1 : tiles == 1 && few && max_len / (CACHE_CUS / wgs) >= 2048 ? 2 : 4;
     const long long rounds = ((long long)max_len + CACHE_STEP * round - 1) / (CACHE_STEP * round);
     const long long splits = std::min({wide ? rounds / 4 : rounds, (wide ? 2 * CACHE_CUS : CACHE_CUS) / wgs, (long long)MAX_SPLITS});
-    // ordering them costs each workgroup about 0.4 us, too much for short ones
-    const int order = wide || batch == 1 || batch > 64 || wgs <= CACHE_CUS || max_len < 1024 ? CACHE_AS_GIVEN : wgs <= 2 * CACHE_CUS ? CACHE_FOLDED : CACHE_LONGEST_FIRST;
+    // One workgroup a CU where the keys are split (two: 8 x 2000 tokens 14.2 us, one 11.6; 24 x 1500 21.1, 16.1), two of many columns (512 behind 7680: one
+    // 225 us, two 158, four 186), and no split into two rounds or fewer, whose join costs more (300 tokens 8.4 us, 6.9; 500 8.6, 7.2).
+    // Ordering the sequences costs each workgroup about 0.3 us, too much for short ones.
+    const int order = wide || batch == 1 || batch > 64 || few || max_len < 1024 ? CACHE_AS_GIVEN : wgs <= 2 * CACHE_CUS ? CACHE_FOLDED : CACHE_LONGEST_FIRST;
     return CachePlan{tiles, round, rounds > 2 && splits > 1 ? (int)splits : 1, order, places};
 }
 

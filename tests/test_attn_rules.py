@@ -136,7 +136,7 @@ def test_keys_and_visible_keys(rules):
                 assert rules.visible(keys, n, i) == max(0, keys - n + i + 1)
 
 
-@pytest.mark.parametrize("waves", [1, 4, 8])
+@pytest.mark.parametrize("waves", [1, 2, 4])
 def test_shares_cover_all_keys_in_whole_steps(rules, waves):
     for splits in (1, 2, 3, 7, 64, 256):
         for keys in (0, 1, 255, 256, 257, 1000, 4096, 131072, 2**30 - 1, 2**30):
@@ -162,7 +162,7 @@ def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
                     if tiles == 8:
                         assert places == rules.places(tokens * (hq // hkv), batch, columns, 128) and places > 0
                     wgs = hkv * (places if tiles == 8 else batch)
-                    assert rnd == (1 if tiles == 8 else 8 if wgs <= 256 else 4)
+                    assert rnd == (1 if tiles == 8 else 2 if tiles == 1 and wgs <= 256 and max_len // (256 // wgs) >= 2048 else 4)
                     assert 1 <= splits <= 256 and (splits - 1) * 64 * rnd < max_len
                     assert splits == 1 or wgs * splits <= (512 if tiles == 8 else 256)
                     along_x = -(-wgs // 8) * 8 * splits if tiles == 8 else splits

@@ -175,6 +175,13 @@ def test_cache_attention_split_over_the_keys(x, dim, page, heads, lens, queries)
     _cache_both(rng, x, dim, page, *heads, lens, queries, max_len=60000)     # a bound far above the lengths
 
 
+@pytest.mark.parametrize("x,dim,page,heads,lens", [
+    ("bf16", 128, 64, (8, 1), [5000]), ("f16", 64, 128, (16, 2), [900, 0, 2100, 1, 130]), ("bf16", 96, 64, (5, 5), [200] * 33), ("f16", 80, 128, (9, 3), [400, 64, 65])])
+def test_cache_attention_in_long_shares(x, dim, page, heads, lens):
+    """A bound of lengths that makes the shares long: workgroups of two waves."""
+    _cache_both(np.random.default_rng(sum(lens)), x, dim, page, *heads, lens, [1] * len(lens), max_len=1 << 20, spare_rows=1)
+
+
 @pytest.mark.parametrize("batch,heads", [(64, 5), (33, 12), (9, 64), (64, 16)])
 def test_cache_attention_of_many_uneven_sequences(batch, heads):
     """Enough work for an order by length: longest first, or folded (at most two workgroups per CU)."""
