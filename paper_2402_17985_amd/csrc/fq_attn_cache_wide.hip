@@ -8,9 +8,10 @@
 //   its values' scale goes into P, relative to that of the tiles accumulated so far, as an addend of the exponent; where the two are
 //     more than a factor 64 apart the accumulators change to the new one first, so that fp16 holds every P.  (Not to one 2^60 times smaller:
 //     what the accumulators hold then outweighs the tile, or is below 2^-25 of its own values, fp16's smallest P.)
-// Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 163 us and 14 for the join, 0.8 PFLOP/s; the
-// matrix pipe busy for 45 %.  Per tile and wave 430 vector instructions, 90 of them to widen and store its part of the codes, against 32 products:
-// with two waves a SIMD the vector instructions bound it.  By 64 columns straight from registers, as the kernel for few columns works, 268 us.
+// Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 160 us and 8.5 for the join, 0.8 PFLOP/s; the
+// matrix pipe is busy for 45 % of the cycles, the vector pipe for 55 %: 240 vector instructions a tile and wave beside 32 products, a third of them to widen and
+// store its part of the codes, and the two waves of a SIMD seldom overlap.  By 64 columns straight from registers, as the kernel for few columns works,
+// 268 us.  From 17 columns on instead of 33: 64 sequences of 4096, 4 tokens each 121 us, so 105; 16 of 1000, 5 tokens 21.9 us, so 15.5.
 #include "fq_attn_cache.h"
 
 namespace fq {
@@ -141,26 +142,33 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     };
     // A row of keys holds 16-byte pieces of the head's elements; a row of values the 64 keys of a dimension, of each 16 first 0..3, 8..11, then
     // 4..7, 12..15: what a lane of either half needs for a product lies together.  A thread writes two neighbouring pieces.
-    const auto put_keys = [&](int stage, const v4u (&reg)[PIECES]) {
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid, r = i / (D / 16), e = i - r * (D / 16);
-            if (!EVEN && i >= CACHE_STEP * D / 16) continue;
-            uint8_t* row = lds + stage * KTILE + r * ROW;
-            *reinterpret_cast<v8h*>(row + pair_place(C, r, e, 0) * 16) = widen8(reg[p][0], reg[p][1]);
-            *reinterpret_cast<v8h*>(row + pair_place(C, r, e, 1) * 16) = widen8(reg[p][2], reg[p][3]);
-        }
+    const auto key_put = [&](int i, int j) { return i / (D / 16) * ROW + pair_place(C, i / (D / 16), i % (D / 16), j) * 16; };
+    const auto value_put = [&](int i, int j) { return 2 * KTILE + i / 4 * VROW + pair_place(8, i / 4, i % 4, j) * 16; };
+    const int key_puts[2] = {key_put(tid, 0), key_put(tid, 1)}, value_puts[2] = {value_put(tid, 0), value_put(tid, 1)};
+    const auto put_keys = [&](int stage, const v4u (&reg)[PIECES], int p, int j) {
+        const int i = p * WIDE_THREADS + tid;
+        if (!EVEN && i >= CACHE_STEP * D / 16) return;
+        // whole rows, a multiple of 32, from one of a thread's pieces to the next: in the same places
+        const int at = EVEN ? key_puts[j] + p * (16 * WIDE_THREADS / D) * ROW : key_put(i, j);
+        *reinterpret_cast<v8h*>(lds + stage * KTILE + at) = widen8(reg[p][2 * j], reg[p][2 * j + 1]);
     };
-    const auto put_values = [&](int stage, const v4u (&reg)[PIECES]) {
-        const _Float16 off = (_Float16)WIDEN_BIAS;
+    const auto put_values = [&](int stage, const v4u (&reg)[PIECES], int p, int j) {
+        if (!EVEN && p * WIDE_THREADS + tid >= 4 * D) return;
+        *reinterpret_cast<v8h*>(lds + stage * VTILE + value_puts[j] + p * (WIDE_THREADS / 4) * VROW) = widen8(reg[p][j], reg[p][j + 2]) - (_Float16)WIDEN_BIAS;
+    };
+    const auto put_all_keys = [&](int stage, const v4u (&reg)[PIECES]) {
 #pragma unroll
-        for (int p = 0; p < PIECES; ++p) {
-            const int i = p * WIDE_THREADS + tid, d = i / 4, e = i % 4;
-            if (!EVEN && i >= 4 * D) continue;
-            uint8_t* row = lds + 2 * KTILE + stage * VTILE + d * VROW;
-            *reinterpret_cast<v8h*>(row + pair_place(8, d, e, 0) * 16) = widen8(reg[p][0], reg[p][2]) - off;
-            *reinterpret_cast<v8h*>(row + pair_place(8, d, e, 1) * 16) = widen8(reg[p][1], reg[p][3]) - off;
-        }
+        for (int p = 0; p < 2 * PIECES; ++p) put_keys(stage, reg, p / 2, p % 2);
+    };
+    const auto put_all_values = [&](int stage, const v4u (&reg)[PIECES]) {
+#pragma unroll
+        for (int p = 0; p < 2 * PIECES; ++p) put_values(stage, reg, p / 2, p % 2);
+    };
+    // Piece n of those that a thread puts in a step: keys for stage `odd`, values for the other.
+    constexpr int PUTS = 4 * PIECES;
+    const auto put = [&](int odd, int n) {
+        if (n < PUTS / 2) put_keys(odd, kreg[odd], n / 2, n % 2);
+        else put_values(1 - odd, vreg[1 - odd], (n - PUTS / 2) / 2, n % 2);
     };
 
     v16f o[VT], s[2];
@@ -179,7 +187,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     for (int n = 0; n < 4; ++n) value_at[n] = 2 * KTILE + col * VROW + pair_place(8, col, n, half) * 16;
 
     // O^T += V^T P of a tile (PV), then S^T of the next (QK); first operands come from LDS AHEAD - 1 products early, the order is kept
-    const auto products = [&](auto with_pv, auto with_qk, auto odd) {      // odd: whether the values' tile has an odd number
+    const auto products = [&](auto with_pv, auto with_qk, auto odd, auto between) {      // odd: whether the values' tile has an odd number
         constexpr int VSTAGE = decltype(odd)::value, KSTAGE = 1 - VSTAGE;
         constexpr int PV = decltype(with_pv)::value ? 4 * VT : 0, N = PV + (decltype(with_qk)::value ? 2 * KS : 0), AHEAD = 4;
         v8h ring[AHEAD];
@@ -202,9 +210,11 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
                     for (int k = 0; k < 16; ++k) s[t][k] = 0.0f;
                 s[t] = M::mul(ring[n % AHEAD], q[e], s[t]);
             }
+            between(n);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    const auto nothing = [](int) {};
     const std::true_type yes;
     const std::false_type no;
     const auto softmax = [&](int i, const Place& at) {
@@ -260,27 +270,34 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         load_keys(now, kreg[0]);
         load_values(now, vreg[0]);
         load_keys(line[0], kreg[1]);
-        put_keys(0, kreg[0]);
+        put_all_keys(0, kreg[0]);
+        put_all_values(0, vreg[0]);
+        put_all_keys(1, kreg[1]);
+        // in the order of the steps' loads, so that a step waits for no later one
+        __builtin_amdgcn_sched_barrier(0);
         load_keys(line[1], kreg[0]);
-        put_values(0, vreg[0]);
+        __builtin_amdgcn_sched_barrier(0);
         load_values(line[0], vreg[1]);
-        load_values(line[1], vreg[0]);
-        put_keys(1, kreg[1]);
+        __builtin_amdgcn_sched_barrier(0);
         load_keys(line[2], kreg[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        load_values(line[1], vreg[0]);
+        __builtin_amdgcn_sched_barrier(0);
         Place fourth = place(4, page_of(4));
         int page_then = page_of(5);
         __syncthreads();
         if (own > 0) {
-            products(no, yes, yes);
+            products(no, yes, yes, nothing);
             softmax(0, now);
         }
         __syncthreads();
         int i = 0;
         const auto begin_step = [&](auto odd) {
             constexpr int O = decltype(odd)::value;
-            put_keys(O, kreg[O]);
-            put_values(1 - O, vreg[1 - O]);
+#pragma unroll
+            for (int n = 0; n < PUTS; ++n) put(O, n);
             load_keys(fourth, kreg[O]);
+            __builtin_amdgcn_sched_barrier(0);
             load_values(line[2], vreg[1 - O]);
         };
         const auto end_step = [&] {
@@ -293,10 +310,15 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
             __syncthreads();
         };
         const auto step = [&](auto odd) {
-            begin_step(odd);
+            constexpr int O = decltype(odd)::value, APART = (4 * VT + 2 * KS) / PUTS;
             __builtin_amdgcn_s_setprio(1);
-            products(yes, yes, odd);
+            products(yes, yes, odd, [&](int n) {
+                if (n % APART == APART - 1 && n / APART < PUTS) put(O, n / APART);
+            });
             __builtin_amdgcn_s_setprio(0);
+            load_keys(fourth, kreg[O]);
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(line[2], vreg[1 - O]);
             softmax(i + 1, line[0]);
             end_step();
         };
@@ -308,10 +330,10 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         if (own > 0) {
             if (i % 2) {
                 begin_step(yes);
-                products(yes, no, yes);
+                products(yes, no, yes, nothing);
             } else {
                 begin_step(no);
-                products(yes, no, no);
+                products(yes, no, no, nothing);
             }
             end_step();
         }

@@ -10,10 +10,11 @@
 // P is rounded to the input's type (the values' type has to match; its rounding is what the output's is), the row sums are taken before that in
 // 32 bits.
 // Two workgroups a CU (four for heads of 64), independent of each other: one's softmax runs beside the other's products.  Eight waves in one workgroup
-// that take turns by barriers gave the same busy cycles (61 % of them the matrix pipe) and lost 15 % on prompts of 256.
-// Measured: 8192 tokens, 64 heads of 128 over 8, causal, bf16: 0.97 to 1.05 ms, 1.05 to 1.13 PFLOP/s (a library product of 8192^3: 1.6); the pipe is
-// busy for 66 % of the cycles at 1.4 GHz, the clock that the power limit leaves: variants of 4.1e8 to 5.4e8 busy cycles all took 1.04 to 1.18 ms.  8 x 256
-// tokens, 32 heads: 16 us for 67 MB, 4.2 TB/s; of a workgroup's 11 us there 5 are the way to the first tile.
+// that take turns by barriers gave the same busy cycles (61 % of them the matrix pipe) and lost 12 % on prompts of 256.
+// Measured: 8192 tokens, 64 heads of 128 over 8, causal, bf16: 0.95 to 1.05 ms, 1.05 to 1.15 PFLOP/s (a library product of 8192^3: 1.6); the pipe is busy for
+// 68 % of the cycles at 1.4 to 1.6 GHz, the clock that the power limit leaves: variants of 4.1e8 to 5.4e8 busy CU cycles all took 1.04 to 1.18 ms.  Eight
+// prompts of 438 to 2048 tokens, 40 heads: 225 us, 0.7 PFLOP/s, 43 % of the cycles: of a workgroup's 27 us 6 are the way to the first tile and the end, 3 or 4 more
+// pass between two workgroups.  8 x 256 tokens, 32 heads: 16 us for 67 MB, 4.2 TB/s; of a workgroup's 11 us there 5 are the way to the first tile.
 #include "fq_attn_common.h"
 
 namespace fq {
