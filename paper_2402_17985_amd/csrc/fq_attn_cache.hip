@@ -52,7 +52,8 @@ __device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
     return __builtin_ctzll(__ballot(lane < batch && longer == nth));
 }
 
-// NT tiles of 16 columns, which all of a sequence and key head's have room in.  Grid: x the shares of the keys, y the key heads, z the sequences.
+// NT tiles of 16 columns.  Grid: x the shares of the keys, y the key heads of one block of columns after the other (with 8 key heads the blocks of one are on
+// one XCD), z the sequences.
 template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(const CacheAttn a)
 {
     constexpr int ROUND = CACHE_STEP * WAVES;
@@ -61,15 +62,16 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     __shared__ float gathered[WAVES][16][ROW];
     __shared__ float tops[WAVES][16 * NT], sums[WAVES][16 * NT];
 
-    const int split = blockIdx.x, h = blockIdx.y;
+    const int split = blockIdx.x, tile = blockIdx.y / a.heads_kv, h = blockIdx.y - tile * a.heads_kv;
     const int b = a.order != CACHE_AS_GIVEN ? by_length(a, blockIdx.z, gridDim.z) : (int)blockIdx.z;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64, col = lane % 16, g = lane / 16;
     const Rows rows = packed_rows(a.cu_q[b], a.cu_q[b + 1], a.tokens, a.max_q);
-    const int columns = rows.count * a.group;
-    if (columns == 0) return;
+    const int columns = rows.count * a.group, c0 = 16 * NT * tile;
+    if (c0 >= columns) return;
     const int keys = cached_keys(a.lens[b], a.max_len, a.capacity), share = share_keys(keys, a.splits, WAVES);
     if (split > 0 && split * (long long)share >= keys) return;
-    const int most = visible_keys(keys, rows.count, rows.count - 1), least = visible_keys(keys, rows.count, 0);
+    const int last = min(c0 + 16 * NT, columns) - 1;
+    const int most = visible_keys(keys, rows.count, last / a.group), least = visible_keys(keys, rows.count, c0 / a.group);
     const int from = split * share, to = min((int)min(from + (long long)share, (long long)most), most);
 
     // the queries, as the second operand: lane (col, g) holds elements 64 j + 16 g + 0..15 of its column's head, as integers of up to 127 * 256
@@ -79,7 +81,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     int limit[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int c = 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
+        const int c = c0 + 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
         const T* p = static_cast<const T*>(a.Q) + (rows.first + t) * (size_t)a.ldq + (size_t)(h * a.group + cc - t * a.group) * D + 16 * g;
         limit[n] = visible_keys(keys, rows.count, t);
         typedef T v8 __attribute__((ext_vector_type(8)));
@@ -279,7 +281,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f*>(&gathered[wave][col][16 * t + 4 * g]) = o[n][t] * mine;
         __syncthreads();
         for (int i = tid; i < 16 * (D / 4); i += 64 * WAVES) {
-            const int cl = i / (D / 4), d = (i - cl * (D / 4)) * 4, c = 16 * n + cl;
+            const int cl = i / (D / 4), d = (i - cl * (D / 4)) * 4, c = c0 + 16 * n + cl;
             if (c >= columns) continue;
             float best = tops[0][16 * n + cl], l = 0.0f;
 #pragma unroll
@@ -427,9 +429,9 @@ template <int DT, int D, int MOST> void join(const CacheAttn& a, int batch, hipS
     attn_cache_join_kernel<DT, D, MOST><<<dim3((unsigned)((a.heads_q + heads - 1) / heads), (unsigned)std::min(a.max_q, a.tokens), (unsigned)batch), JOIN_THREADS, 0, stream>>>(a);
 }
 
-template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, unsigned wide_grid, hipStream_t stream)
+template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, int blocks, unsigned wide_grid, hipStream_t stream)
 {
-    const dim3 grid((unsigned)a.splits, (unsigned)a.heads_kv, (unsigned)batch);
+    const dim3 grid((unsigned)a.splits, (unsigned)(a.heads_kv * blocks), (unsigned)batch);
     if (tiles * 16 == WIDE_COLUMNS) {
         const int rc = launch_attn_cache_wide(a, DT, D, batch, wide_grid, stream);
         if (rc) return rc;
@@ -444,13 +446,13 @@ template <int DT, int D> int launch(const CacheAttn& a, int tiles, int batch, un
     return e == hipSuccess ? FQ_OK : fail(FQ_ERR_HIP, "cache attention launch failed: %s", hipGetErrorString(e));
 }
 
-template <int DT> int launch_dim(const CacheAttn& a, int tiles, int head_dim, int batch, unsigned wide_grid, hipStream_t stream)
+template <int DT> int launch_dim(const CacheAttn& a, int tiles, int head_dim, int batch, int blocks, unsigned wide_grid, hipStream_t stream)
 {
     switch (head_dim) {
-    case 64: return launch<DT, 64>(a, tiles, batch, wide_grid, stream);
-    case 80: return launch<DT, 80>(a, tiles, batch, wide_grid, stream);
-    case 96: return launch<DT, 96>(a, tiles, batch, wide_grid, stream);
-    default: return launch<DT, 128>(a, tiles, batch, wide_grid, stream);
+    case 64: return launch<DT, 64>(a, tiles, batch, blocks, wide_grid, stream);
+    case 80: return launch<DT, 80>(a, tiles, batch, blocks, wide_grid, stream);
+    case 96: return launch<DT, 96>(a, tiles, batch, blocks, wide_grid, stream);
+    default: return launch<DT, 128>(a, tiles, batch, blocks, wide_grid, stream);
     }
 }
 
@@ -468,9 +470,10 @@ int launch_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int h
     const CacheAttn a{Q, Y, ldq, ldy, cu_q, lens, page_table, k_cache, v_cache, k_scale, v_scale, part, stat, scale, tokens, max_q, max_len,
                       heads_q, heads_kv, heads_q / heads_kv, table_width * page_size, pages, page_size,
                       page_size == 128 ? 7 : 6, table_width, splits, plan.round, plan.order};
+    const int blocks = plan.tiles > 2 ? 1 : (int)plan.places;
     const unsigned wide_grid = (unsigned)tile_workgroups(plan.places, splits, heads_kv);
-    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, wide_grid, stream)
-                             : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, wide_grid, stream);
+    return x_dtype == FQ_F16 ? launch_dim<FQ_F16>(a, plan.tiles, head_dim, batch, blocks, wide_grid, stream)
+                             : launch_dim<FQ_BF16>(a, plan.tiles, head_dim, batch, blocks, wide_grid, stream);
 }
 
 }  // namespace fq

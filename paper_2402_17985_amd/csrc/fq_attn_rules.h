@@ -116,21 +116,25 @@ FQ_BOTH TileUnit tile_unit(unsigned id, unsigned members, unsigned heads_kv)
 inline long long tile_workgroups(long long places, int members, int heads_kv) { return (places * heads_kv + 7) / 8 * 8 * members; }
 
 // How fq_attn_cache deals out its work.  A workgroup takes a tile of columns (query token, head of the group; 16 * tiles of them) of one
-// sequence and key head, and of its keys all or one of `splits` shares, `round` steps at a time: its waves take the steps of a round in turn, or (many
-// columns) each step together.
+// sequence and key head, and of its keys all or one of `splits` shares, `round` steps at a time: its waves take the steps of a round in turn, or (128
+// columns, the kernel for many) each step together.
 constexpr int MAX_SPLITS = 256, CACHE_CUS = 256, WIDE_COLUMNS = 128;
 enum CacheOrder { CACHE_AS_GIVEN, CACHE_LONGEST_FIRST, CACHE_FOLDED };
 struct CachePlan {
     int tiles, round, splits, order;      // order of the sequences
-    long long places;                     // many columns: for the tiles of all sequences, else 1
+    long long places;                     // tiles of columns: of all sequences with many columns, else of one
 };
 inline CachePlan cache_plan(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv)
 {
-    const long long columns = (long long)max_q * (heads_q / heads_kv);
-    const int tiles = columns <= 16 ? 1 : columns <= 32 ? 2 : WIDE_COLUMNS / 16;
-    const bool wide = tiles > 2;
-    const long long places = wide ? tile_places((long long)tokens * (heads_q / heads_kv), batch, columns, WIDE_COLUMNS) : 1;
-    const long long wgs = std::max((wide ? places : batch) * heads_kv, 1LL);
+    // Many columns go by tiles of 128 where there is much to compute, else by as many of 32 as they need, which are spread over more of the device.
+    // us, tiles of 128 / of 32, 64 heads over 8 if not said otherwise: 64 columns, a sequence of 1000 14.5 / 12.1, 32 of 2048 46.4 / 35.9, three of 40000 72 / 60, but 64
+    // of 1024 41 / 44; 128 columns, 8192 27.5 / 19.1, three of 40000 91 / 123, 8 of 8192 58 / 55, 64 of 500 32 / 52; 1024 columns, 4096 39 / 31; 512 tokens of 5 heads to a key
+    // head before 128 keys, 100 sequences, 63 / 123.
+    const long long pairs = (long long)batch * heads_kv, columns = (long long)max_q * (heads_q / heads_kv), by32 = (columns + 31) / 32;
+    const bool wide = columns > 32 && (pairs * by32 > 3 * CACHE_CUS || (columns > 64 && columns * pairs > (1LL << 25) / max_len));
+    const int tiles = columns <= 16 ? 1 : wide ? WIDE_COLUMNS / 16 : 2;
+    const long long places = wide ? tile_places((long long)tokens * (heads_q / heads_kv), batch, columns, WIDE_COLUMNS) : by32;
+    const long long wgs = std::max(wide ? places * heads_kv : pairs * places, 1LL);
     // Four waves; two where a CU has one workgroup, of one tile of columns, and the longest share is long: fewer streams a CU then
     // read the cache faster.  us, two / four, 64 heads over 8: two sequences of 131072 tokens 97.5 / 99.8, 8 of 16384 44.5 / 48.0, 32 of 4096 41.5 / 44.1; but one of
     // 16384 (shares of 512) 13.4 / 12.7, 20 of up to 1200 13.8 / 11.1, two column tiles of 8 x 32768 106 / 102.  (Eight: 1001 tokens 11.7 / 8.7, 8192 13.2 / 10.1.)

@@ -81,10 +81,12 @@ def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, max_q=None):
     head's largest magnitude (half a step is 1 / 65024 of it), which moves a score by `scores` / 65024 at most and a probability and the
     sum that divides it by as much each; and a step's product is a sum of 64 p (1152 + v) less 1152 times the sum of p, 16 roundings (two
     products, four lanes' partial sums) of up to 1280 times the sum of p, in codes.
-    For more columns: the scores' 32-bit sums are of codes plus 1152, up to 1280 where `scores` counts 128."""
+    From 33 columns on either kernel may serve, the one for few columns or the one for many, in which the scores' 32-bit sums are of codes plus 1152, up to 1280
+    where `scores` counts 128: the larger of the two bounds."""
     exact, spread = A.cache(q, cu_q, lens, table, kc, vc, ks, vs, scale), A.cache(q, cu_q, lens, table, kc, np.abs(vc.astype(np.int16)), ks, vs, scale)
     scores = scale * np.abs(q).max() * 128 * q.shape[2] * ks.max()
     bound = attention_bound(exact, spread, scores, int(max(lens)), q.shape[2], 128 * vs.max(), x, HALF_STEP["f16"])
+    few = 2 * scores / 65024 * spread + 16 * 2.0**-24 * 1280 * vs.max()
     if (max_q or int(np.diff(cu_q).max())) * (q.shape[1] // kc.shape[1]) > 32:
-        return exact, bound + 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread
-    return exact, bound + 2 * scores / 65024 * spread + 16 * 2.0**-24 * 1280 * vs.max()
+        return exact, bound + np.maximum(few, 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread)
+    return exact, bound + few

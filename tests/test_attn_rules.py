@@ -158,10 +158,11 @@ def test_plans_are_bounded_and_do_not_split_where_there_is_work_enough(rules):
                     rules.plan(batch, tokens, max_q, max_len, hq, hkv, out)
                     tiles, rnd, splits, holds, places = out
                     columns = max_q * (hq // hkv)
-                    assert tiles in (1, 2, 8) and (tiles == 8 or columns <= 16 * tiles)
-                    if tiles == 8:
-                        assert places == rules.places(tokens * (hq // hkv), batch, columns, 128) and places > 0
-                    wgs = hkv * (places if tiles == 8 else batch)
+                    by32 = -(-columns // 32)
+                    many = columns > 32 and (batch * hkv * by32 > 768 or (columns > 64 and columns * batch * hkv > 2**25 // max_len))
+                    assert tiles == (1 if columns <= 16 else 8 if many else 2)
+                    assert places == (rules.places(tokens * (hq // hkv), batch, columns, 128) if many else by32) > 0
+                    wgs = hkv * places * (1 if many else batch)
                     assert rnd == (1 if tiles == 8 else 2 if tiles == 1 and wgs <= 256 and max_len // (256 // wgs) >= 2048 else 4)
                     assert 1 <= splits <= 256 and (splits - 1) * 64 * rnd < max_len
                     assert splits == 1 or wgs * splits <= (512 if tiles == 8 else 256)

@@ -161,6 +161,19 @@ def test_cache_attention_of_single_tokens(x, dim, page, heads):
     ("bf16", 80, 128, (4, 1), [500], [70]), ("f16", 64, 64, (2, 1), [260, 65], [150, 66])])
 def test_cache_attention_of_several_tokens(x, dim, page, heads, lens, queries):
     _cache_both(np.random.default_rng(sum(lens)), x, dim, page, *heads, lens, queries, spare_rows=3)
+    _cache_both(np.random.default_rng(sum(lens)), x, dim, page, *heads, lens, queries, max_len=1 << 20)     # tiles of 128 from 65 columns on
+
+
+@pytest.mark.parametrize("x,dim,page", [("bf16", 64, 128), ("f16", 80, 64), ("bf16", 96, 64), ("f16", 96, 128), ("bf16", 128, 64), ("f16", 128, 128), ("bf16", 80, 128)])
+@pytest.mark.parametrize("batch,heads,most,shared", [(50, (16, 8), 32, False), (49, (8, 8), 40, False), (13, (24, 8), 139, "some"), (20, (24, 8), 139, False)])
+def test_cache_attention_of_many_columns_in_many_workgroups(x, dim, page, batch, heads, most, shared):
+    """Tiles of 128 columns, mostly with keys that are not shared out: 64 columns, 40, and several tiles."""
+    rng = np.random.default_rng(batch + dim)
+    lens = [int(n) for n in rng.integers(0, 180, batch)]
+    queries = [int(rng.integers(0, min(n, most) + 1)) for n in lens]
+    lens[3], queries[3] = max(190, most), most
+    assert shared or fq.fq_attn_cache_workspace_bytes(batch, sum(queries), most, 5000, *heads, dim) == 16
+    _cache_both(rng, x, dim, page, *heads, lens, queries, max_len=5000)
 
 
 @pytest.mark.parametrize("x,dim,page,heads,lens,queries", [
@@ -200,6 +213,7 @@ def test_cache_attention_of_pieces_beside_single_tokens(batch, heads):
     lens[batch // 2], queries[batch // 2] = 400, 300
     lens[-1], queries[-1] = 130, 67
     _cache_both(rng, "bf16", 64, 64, *heads, lens, queries, spare_rows=2)
+    _cache_both(rng, "f16", 64, 64, *heads, lens, queries, max_len=1 << 20)
 
 
 def test_cache_attention_with_a_bound_of_queries_far_above_them():
@@ -219,6 +233,7 @@ def test_cache_attention_of_many_columns_over_pages_of_very_different_scales(spr
         return k, v, ks, vs
     try:
         U.filled_cache = filled
+        _cache_both(rng, "bf16", 64, 64, 4, 2, [1000, 300], [40, 20], max_len=1 << 20)
         _cache_both(rng, "bf16", 64, 64, 4, 2, [1000, 300], [40, 20])
         _cache_both(rng, "f16", 64, 64, 4, 2, [1000, 300], [1, 2])
     finally:
@@ -227,6 +242,7 @@ def test_cache_attention_of_many_columns_over_pages_of_very_different_scales(spr
 
 def test_cache_attention_leaves_out_pages_that_do_not_exist():
     _cache_both(np.random.default_rng(5), "f16", 128, 64, 4, 2, [200, 64, 400], [50, 20, 21], bad=((0, 1, -1), (1, 0, 0), (2, 6, 1 << 20), (2, 0, -(1 << 31))))
+    _cache_both(np.random.default_rng(5), "f16", 128, 64, 4, 2, [200, 64, 400], [50, 20, 21], bad=((0, 1, -1), (1, 0, 0), (2, 6, 1 << 20), (2, 0, -(1 << 31))), max_len=1 << 20)
     _cache_both(np.random.default_rng(5), "bf16", 64, 64, 4, 2, [200, 64, 400], [1, 1, 2], bad=((0, 1, -1), (1, 0, 0), (2, 6, 1 << 20), (2, 0, -(1 << 31))))
 
 
