@@ -424,10 +424,11 @@ int fq_gemm_select(int variant);
  *
  * fq_attn_cache — Y[i] = softmax(scale * Q[i] K^T) V over the cache: with n query tokens of sequence b and lens[b] tokens in the
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
- *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider, probabilities enter the second
- *   product as fp16; with up to 32 columns (query tokens times heads of a group) queries enter the first as integers of 1 / 32512 of their
- *   head's largest magnitude.  max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they
- *   and the number of rows, not the values on the device, set the launch, so a captured call may be replayed with other sequences within them.
+ *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider.  Up to 32 columns (query tokens times
+ *   heads of a group), and beyond where the sizes leave little to compute, queries enter the first product as integers of 1 / 32512 of their head's
+ *   largest magnitude and probabilities the second as fp16 (F16: as the sum of two); else both as fp16.
+ *   max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they and the number of rows, not the
+ *   values on the device, set the launch, so a captured call may be replayed with other sequences within them.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
  *   Calls that overlap (different streams) need a workspace each; calls and graphs that follow one another may share one.
  *   Y may be Q itself (same address and stride), else it must not overlap the inputs.

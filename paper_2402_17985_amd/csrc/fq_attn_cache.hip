@@ -7,8 +7,10 @@
 //                 two limbs, so that each product is done twice; the sums are exact.  (Codes widened to fp16 take five instructions
 //                 for four of them; a step of 64 keys is 300 vector instructions beside 32 products as it is.)
 //   softmax       running maximum and sum per column.  The product leaves a column's 64 scores in four lanes, 16 each.
-//   O^T += V^T P  16 dimensions x 16 columns, 32 keys deep, P rounded to fp16: half a step is 2^-11 of each, what an fp16 output is
-//                 rounded by too.  The sum that divides is that of the rounded ones.  A step's keys lie in one page, whose scale multiplies
+//   O^T += V^T P  16 dimensions x 16 columns, 32 keys deep, P in fp16: half a step is 2^-11 of each, little beside the 2^-8 that a bf16 output is
+//                 rounded by.  For an fp16 output it would be as much as that one's own rounding (error against 64 bits 1.4 times that of
+//                 exact probabilities, 1.03 so), so that P is the sum of two there: another product, 0.5 to 4 % of the time of single tokens.
+//                 The sum that divides is that of the rounded ones.  A step's keys lie in one page, whose scale multiplies
 //                 its product in 32 bits.
 // No operand passes through LDS: which key of the page stands in which row of the first product is free, and with key
 // 16 (r / 4) + 4 t + r % 4 in row r of tile t a lane's scores are those of 16 consecutive keys, the very ones whose values it
@@ -57,6 +59,7 @@ __device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
 template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void attn_cache_kernel(const CacheAttn a)
 {
     constexpr int ROUND = CACHE_STEP * WAVES;
+    constexpr int LIMBS = DT == FQ_F16 ? 2 : 1;      // of a probability
     typedef typename Stored<DT>::type T;
     constexpr int KC = (D + 63) / 64, VT = D / 16, ROW = D + 4;   // 64-byte pieces of a key, 16-dimension tiles, LDS row
     __shared__ float gathered[WAVES][16][ROW];
@@ -200,7 +203,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         load_keys(next);
         __builtin_amdgcn_sched_barrier(0);
 
-        v8h p[NT][2];
+        v8h p[NT][LIMBS][2];
         float step_sum[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -234,11 +237,16 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; i += 2) {
-                    const v2h e = {(_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i], f, -base)),
-                                   (_Float16)__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i + 1], f, -base))};
-                    add = __builtin_amdgcn_fdot2(e, ones, add, false);      // of the rounded ones: they weigh the values
-                    p[n][t / 2][4 * (t % 2) + i] = e[0];
-                    p[n][t / 2][4 * (t % 2) + i + 1] = e[1];
+                    float w[2] = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i], f, -base)), __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][t][i + 1], f, -base))};
+#pragma unroll
+                    for (int l = 0; l < LIMBS; ++l) {
+                        const v2h e = {(_Float16)w[0], (_Float16)w[1]};
+                        add = __builtin_amdgcn_fdot2(e, ones, add, false);      // of the rounded ones: they weigh the values
+                        p[n][l][t / 2][4 * (t % 2) + i] = e[0];
+                        p[n][l][t / 2][4 * (t % 2) + i + 1] = e[1];
+                        w[0] -= (float)e[0];
+                        w[1] -= (float)e[1];
+                    }
                 }
             step_sum[n] = over_groups_sum(add);
             sum[n] += step_sum[n];
@@ -250,8 +258,12 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const float start = -WIDEN_BIAS * step_sum[n];
-                v4f r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][0], v4f{start, start, start, start}, 0, 0, 0);
-                r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[n][1], r, 0, 0, 0);
+                v4f r = {start, start, start, start};
+#pragma unroll
+                for (int l = 0; l < LIMBS; ++l) {
+                    r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[n][l][0], r, 0, 0, 0);
+                    r = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[n][l][1], r, 0, 0, 0);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[n][t][i] = __builtin_fmaf(r[i], vs, o[n][t][i]);
             }

@@ -10,8 +10,8 @@
 //     what the accumulators hold then outweighs the tile, or is below 2^-25 of its own values, fp16's smallest P.)
 // Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 157 us and 8.4 for the join, 0.85 PFLOP/s at
 // 1.7 GHz; the matrix pipe is busy for 47 % of the cycles, the vector pipe for 57 %: 240 vector instructions a tile and wave beside 32 products, a third of them to
-// widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us.  From 17 columns on instead
-// of 33: 64 sequences of 4096, 4 tokens each, 121 us, so 105; 16 of 1000, 5 tokens, 21.9 us, so 15.5.
+// widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
+// same: cache_plan).
 #include "fq_attn_cache.h"
 
 namespace fq {

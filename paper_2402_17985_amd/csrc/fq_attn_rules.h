@@ -127,9 +127,9 @@ struct CachePlan {
 inline CachePlan cache_plan(int batch, int tokens, int max_q, int max_len, int heads_q, int heads_kv)
 {
     // Many columns go by tiles of 128 where there is much to compute, else by as many of 32 as they need, which are spread over more of the device.
-    // us, tiles of 128 / of 32, 64 heads over 8 if not said otherwise: 64 columns, a sequence of 1000 14.5 / 12.1, 32 of 2048 46.4 / 35.9, three of 40000 72 / 60, but 64
-    // of 1024 41 / 44; 128 columns, 8192 27.5 / 19.1, three of 40000 91 / 123, 8 of 8192 58 / 55, 64 of 500 32 / 52; 1024 columns, 4096 39 / 31; 512 tokens of 5 heads to a key
-    // head before 128 keys, 100 sequences, 63 / 123.
+    // us, tiles of 128 / of 32, 64 heads over 8: 32 columns, 64 sequences of 4096 121 / 105; 64 columns, one of 1000 14.5 / 12.1, 32 of 2048 46.4 / 35.9, three of
+    // 40000 72 / 60, but 64 of 1024 41 / 44; 128 columns, one of 8192 27.5 / 19.1, 8 of 8192 58 / 55, three of 40000 91 / 123, 64 of 500 32 / 52; 320 columns, 100 of
+    // 128 63 / 123; 1024 columns, one of 4096 39 / 31.
     const long long pairs = (long long)batch * heads_kv, columns = (long long)max_q * (heads_q / heads_kv), by32 = (columns + 31) / 32;
     const bool wide = columns > 32 && (pairs * by32 > 3 * CACHE_CUS || (columns > 64 && columns * pairs > (1LL << 25) / max_len));
     const int tiles = columns <= 16 ? 1 : wide ? WIDE_COLUMNS / 16 : 2;
