@@ -127,6 +127,48 @@ def test_captured_cache_attention_follows_lengths_and_cache(lens, queries):
         assert torch.equal(eager, y)
 
 
+@pytest.mark.parametrize("batch", [12, 70])
+def test_captured_calls_follow_how_the_rows_are_dealt_out(batch):
+    """An append, a prompt's attention and attention of pieces, captured once and replayed with the rows dealt out otherwise among the sequences."""
+    rng = np.random.default_rng(batch)
+    rows, hq, hkv, dim, page, longest, scale = 700, 4, 2, 64, 64, 520, 0.11
+    (q, qn), (k, kn), (v, vn) = (U.packed(rng, rows, h, dim, "bf16") for h in (hq, hkv, hkv))
+    table, pages = U.page_tables(rng, [-(-longest // page)] * batch)
+    start = U.filled_cache(rng, pages, hkv, page, dim)
+    dev, tab, cu, none, ln = U.to_dev(*start), U.i32(table), U.i32([0] * (batch + 1)), U.i32([0] * batch), U.i32([0] * batch)
+    k_out, y, z = torch.empty_like(k), torch.empty_like(q), torch.empty_like(q)
+    ws = torch.empty(fq.fq_attn_cache_workspace_bytes(batch, rows, longest, longest, hq, hkv, dim), dtype=torch.uint8, device=U.DEV)
+
+    def calls():
+        fq.fq_kv_append(None, k, v, cu, none, longest, *dev, tab, K_out=k_out)
+        fq.fq_attn_prompt(q, k_out, v, cu, cu, longest, scale, y)
+        fq.fq_attn_cache(q, cu, ln, longest, longest, *dev, tab, scale, z, ws)
+    calls()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    deals = [[rows // batch] * batch, [longest] + [2] * (batch - 1), [1] * (batch - 1) + [longest], [0, 300] + [0] * (batch - 3) + [400]]
+    for turn, lens in enumerate(deals):
+        at = U.offsets(lens)
+        n = at[-1]
+        assert n <= rows
+        cu.copy_(U.i32(at)), ln.copy_(U.i32(lens))
+        for have, value in zip(dev, U.to_dev(*start)):
+            have.copy_(value)
+        ws.fill_(0xFF), y.fill_(5.0), z.fill_(5.0)
+        g.replay()
+        torch.cuda.synchronize()
+        want = [a.copy() for a in start]
+        A.append(qn, kn, vn, at, [0] * batch, table, *want, None, None, False)
+        for got, w in zip(dev, want):
+            assert np.array_equal(got.cpu().numpy(), w), turn
+        U.check(y[:n], *U.prompt_case(qn[:n], kn[:n], vn[:n], at, at, scale, True, "bf16"), f"prompt {turn}")
+        exact, bound = U.cache_case(qn, at, lens, table, *want, scale, "bf16", longest)
+        U.check(z[:n], exact[:n], bound[:n], f"pieces {turn}")
+        assert (y[n:] == 5.0).all() and (z[n:] == 5.0).all()
+
+
 def test_captured_decoding_steps_share_cache_and_workspace():
     """A graph of a decoding step (append, then attention) and one of another batch's, both on one workspace, replayed in turn."""
     rng = np.random.default_rng(2)
