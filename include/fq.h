@@ -400,7 +400,8 @@ int fq_gemm_select(int variant);
  *   sequence are left as they were.
  * Cache: pages of page_size (64 or 128) tokens, 8-bit codes with one scale for each page and head,
  *   k_cache [pages, heads_kv, page_size, head_dim], v_cache [pages, heads_kv, head_dim, page_size] (transposed within a page:
- *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv], finite and not negative; an element is code * scale.
+ *   tokens are the reduction of P V), k_scale, v_scale fp32 [pages, heads_kv], finite and not negative (values' scales below 2^-126 may
+ *   count as 0); an element is code * scale.
  *   page_table int32 [batch, table_width], device: token t of sequence b lies in page page_table[b, t / page_size], slot
  *   t % page_size.  table_width * page_size <= 2^30.  Nothing has to be cleared before use: a page's first token starts it anew.
  * Values on the device cannot be checked when the call is made; the kernels use them within bounds: offsets are clamped to

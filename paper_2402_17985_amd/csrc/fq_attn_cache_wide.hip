@@ -5,9 +5,9 @@
 // tiles of 64 keys, S^T = K Q^T and O^T += V^T P with P as it lies in the scores' registers.  A tile lies in one page:
 //   its keys' scale goes into the factor of the scores; the keys stay 1152 too large each (see widen8), which adds 1152 times the sum of
 //     the query's elements to every score of a column and is taken off where the maximum is;
-//   its values' scale goes into P, relative to that of the tiles accumulated so far, as an addend of the exponent; where the two are
-//     more than a factor 64 apart the accumulators change to the new one first, so that fp16 holds every P.  (Not to one 2^60 times smaller:
-//     what the accumulators hold then outweighs the tile, or is below 2^-25 of its own values, fp16's smallest P.)
+//   its values' scale goes into P as an addend of the exponent.  So P's unit, which the accumulators count in, is the largest product of a weight and
+//     a scale so far, kept apart from the largest weight, which the sum counts in: whatever the scales, P is at most 1 (or the 2^8 that a unit may lag
+//     behind), neither is ever changed to something smaller, and what fp16 cannot hold of a P is little beside the largest one's products.
 // Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 157 us and 8.4 for the join, 0.85 PFLOP/s at
 // 1.7 GHz; the matrix pipe is busy for 47 % of the cycles, the vector pipe for 57 %: 240 vector instructions a tile and wave beside 32 products, a third of them to
 // widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
@@ -18,6 +18,7 @@ namespace fq {
 namespace {
 
 constexpr int WIDE_WAVES = WIDE_COLUMNS / 32, WIDE_THREADS = 64 * WIDE_WAVES;
+constexpr float LOWEST = -0x1p100f;      // below every score, and finite: differences of two are numbers
 
 // Where piece 2 e + half of row r lies among its row's C: both the eight lanes that write neighbouring pairs' first (or second) pieces and the
 // 16 rows that are read at a time, the same piece of each, then meet all banks.  (Widths of 10 and 12 pieces are only turned for the reads.)
@@ -176,8 +177,8 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     for (int t = 0; t < VT; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
-    float top = -INFINITY, sum = 0.0f;                   // of the scaled scores; over this lane's keys
-    float unit = 0.0f, per_unit = 0.0f;                  // values' scale that o counts in
+    float top = LOWEST, sum = 0.0f;                      // of the scaled scores; over this lane's keys
+    float unit = LOWEST;                                 // log2 of what o counts in: weights times values' scales
     v8h p[4];                                            // 16 keys each
 
     uint32_t key_at[KS], value_at[4];
@@ -233,24 +234,18 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 #pragma unroll
         for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
         m = __builtin_fmaf(over_halves_max(m), f, -shift);
-        if (__ballot(top == -INFINITY || m - top > SLACK)) {
-            const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top - now);
+        const float log_scale = fmaxf(__builtin_amdgcn_logf(at.v_scale), -200.0f);      // below 2^-126: 0, which counts as 2^-200
+        if (__ballot(m > top + SLACK || m + log_scale > unit + SLACK)) {
+            const float now = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= keep;
+            const float now_unit = fmaxf(m + log_scale, unit), keep_o = __builtin_amdgcn_exp2f(unit - now_unit);
+            unit = now_unit;
 #pragma unroll
-            for (int t = 0; t < VT; ++t) o[t] *= keep;
+            for (int t = 0; t < VT; ++t) o[t] *= keep_o;
         }
-        if (at.v_scale > 64.0f * unit || (at.v_scale < unit * 0x1p-6f && at.v_scale >= unit * 0x1p-60f && at.v_scale > 0.0f)) {
-            asm volatile("");
-            const float change = unit / at.v_scale;
-            unit = at.v_scale;
-            per_unit = 1.0f / unit;
-#pragma unroll
-            for (int t = 0; t < VT; ++t) o[t] *= change;
-        }
-        // far below the unit (or 0): probabilities too small for fp16, whose sum still counts
-        const float part = fmaxf(at.v_scale * per_unit, 0x1p-60f);
-        const float off = (top == -INFINITY ? 0.0f : top) + shift - __builtin_amdgcn_logf(part);
+        // the weight that has P = 1; far above the tile's largest (whose P are too small for fp16) 2^60 times that one, so that the sum still counts them
+        const float one = fminf(unit - log_scale, fmaxf(m, LOWEST) + 60.0f), off = one + shift;
         float add = 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -260,7 +255,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
                 add += w;
                 p[2 * t + e / 8][e % 8] = (_Float16)w;
             }
-        sum = __builtin_fmaf(add, __builtin_amdgcn_rcpf(part), sum);
+        sum = __builtin_fmaf(add, __builtin_amdgcn_exp2f(one - top), sum);
     };
 
     // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), more is asked for (keys of i + 4, values of i + 3), PV of
@@ -346,6 +341,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
     sum = over_halves_sum(sum);
     if (c >= columns) return;
+    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - top));      // twice, as the whole may be beyond fp32 where a product with it is not
     const size_t row = rows.first + (size_t)token;
     if (a.splits > 1) {
         const size_t at = (row * a.heads_q + head) * a.splits + split;
@@ -358,10 +354,10 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (32 * t + 8 * e < D) *reinterpret_cast<v4f*>(a.part + at * D + 32 * t + 8 * e + 4 * half) =
-                    v4f{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]} * unit;
+                    v4f{o[t][4 * e], o[t][4 * e + 1], o[t][4 * e + 2], o[t][4 * e + 3]} * half_unit * half_unit;
         return;
     }
-    const float inv = sum > 0.0f ? unit / sum : 0.0f;
+    const float inv = sum > 0.0f ? half_unit / sum : 0.0f;
     typedef T v4 __attribute__((ext_vector_type(4)));
     T* yp = static_cast<T*>(a.Y) + row * (size_t)a.ldy + (size_t)head * D + 4 * half;
 #pragma unroll
@@ -371,7 +367,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
             if (32 * t + 8 * e >= D) continue;
             v4 y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = (T)(o[t][4 * e + i] * inv);
+            for (int i = 0; i < 4; ++i) y[i] = (T)(o[t][4 * e + i] * inv * half_unit);
             *reinterpret_cast<v4*>(yp + 32 * t + 8 * e) = y;
         }
 }

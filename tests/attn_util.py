@@ -90,3 +90,64 @@ def cache_case(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, max_q=None):
     if (max_q or int(np.diff(cu_q).max())) * (q.shape[1] // kc.shape[1]) > 32:
         return exact, bound + np.maximum(few, 2 * (q.shape[2] + 16) * 2.0**-24 * 9 * scores * spread)
     return exact, bound + few
+
+
+# ------------------------------------------------------------------------------------------------
+# bounds row by row and key by key
+# ------------------------------------------------------------------------------------------------
+def _softmax(s):
+    w = np.exp(s - s.max(-1, keepdims=True))
+    return w / w.sum(-1, keepdims=True)
+
+
+def _off(p, y, v, delta, half_p, floor):
+    """What weights that are off by `delta` (and by a rounding of half_p each that their sum may or may not see) and the products lose: p [n, keys],
+    y [n, dim], v [keys, dim], delta [n, keys] or [n, 1]; floor [n, keys]: what a weight may lose whatever its size."""
+    keys = p.shape[1]
+    sums = (keys / 64 + 80) * 2.0**-24              # a step's 64 products and sums, then one sum a step
+    return (p * (delta + half_p + sums) + floor) @ np.abs(v) + ((p * (delta + half_p + sums)).sum(1, keepdims=True)) * np.abs(y)
+
+
+def cache_rows(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, columns):
+    """Exact results and how far they may be off, for sequences with queries.  columns "few": the kernel for up to 32 columns, whose queries are integers of
+    1 / 32512 of their largest, whose second product has 1152 too much in it (16 roundings a step) and whose weights below 2^-33 of a step's largest vanish;
+    "many": scores of codes plus 1152, logarithms of the values' scales, and weights times scales that vanish below 2^-36 of their largest."""
+    page, pages, dim = kc.shape[2], kc.shape[0], q.shape[2]
+    g = q.shape[1] // kc.shape[1]
+    exact, bound = np.zeros(q.shape), np.zeros(q.shape)
+    for b in range(len(lens)):
+        n, keys = int(cu_q[b + 1] - cu_q[b]), int(lens[b])
+        if not n or not keys:
+            continue
+        at = table[b, :-(-keys // page)]
+        assert ((at >= 0) & (at < pages)).all()
+        for h in range(kc.shape[1]):
+            codes = kc[at, h].reshape(-1, dim)[:keys].astype(np.float64)
+            k_scale, v_scale = (np.repeat(s[at, h].astype(np.float64), page)[:keys] for s in (ks, vs))
+            v = vc[at, h].transpose(0, 2, 1).reshape(-1, dim)[:keys].astype(np.float64) * v_scale[:, None]
+            hidden = np.arange(keys)[None, :] > keys - n + np.arange(n)[:, None]
+            for head in range(h * g, (h + 1) * g):
+                rows = slice(int(cu_q[b]), int(cu_q[b + 1]))
+                qh = q[rows, head].astype(np.float64)
+                s = np.where(hidden, -np.inf, scale * (qh @ codes.T) * k_scale)
+                seen = ~hidden.all(1)
+                p = np.zeros_like(s)
+                p[seen] = _softmax(s[seen])
+                y = p @ v
+                aq, top = np.abs(qh), np.abs(qh).max(1, keepdims=True)
+                size = scale * (aq @ (np.abs(codes) + (1152 if columns == "many" else 0)).T) * k_scale
+                by_q = scale * top * (np.abs(codes).sum(1) * k_scale)
+                fp32 = 2 * (dim + 16) * 2.0**-24 * np.where(hidden, 0.0, size).max(1, keepdims=True) + 2.0**-21
+                if columns == "few":
+                    delta = fp32 + by_q / 65024
+                    floor = np.repeat(np.maximum.reduceat(p, np.arange(0, keys, 64), axis=1), 64, axis=1)[:, :keys] * 2.0**-33
+                    more = 16 * 2.0**-24 * 1280 * (p @ v_scale)[:, None]
+                    half_p = 2.0**-22 if x == "f16" else 2.0**-11
+                else:
+                    logs = np.abs(np.log2(v_scale[v_scale > 0])).max() if (v_scale > 0).any() else 0.0
+                    delta = fp32 + (by_q * 2.0**-25 if x == "bf16" else 0.0) + 2.0**-22 * (logs + 16)
+                    floor = (p * v_scale).max(1, keepdims=True) * 2.0**-36 / np.where(v_scale > 0, v_scale, np.inf)
+                    more, half_p = 0.0, 2.0**-11
+                off = _off(p, y, v, delta, half_p, np.where(hidden, 0.0, floor)) + more
+                exact[rows, head], bound[rows, head] = y, HALF_STEP[x] * (np.abs(y) + off) + off + 2.0**-24 * (x == "f16") + 1e-36
+    return exact, bound

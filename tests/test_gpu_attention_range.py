@@ -1,0 +1,74 @@
+"""Attention where weights and values' scales are far apart: pages whose scales fall or rise by large factors."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_17985_amd as fq
+from tests import attn_util as U
+
+pytestmark = pytest.mark.gpu
+
+
+def _attend(q, cu, lens, table, arrays, scale, max_q, max_len, one_share=True):
+    size = fq.fq_attn_cache_workspace_bytes(len(lens), q.shape[0], max_q, max_len, q.shape[1], arrays[0].shape[1], q.shape[2])
+    assert (size == 16) == one_share
+    y, ws = torch.full_like(q, 7.0), torch.full((size,), 0xFF, dtype=torch.uint8, device=U.DEV)
+    fq.fq_attn_cache(q, U.i32(cu), U.i32(lens), max_q, max_len, *U.to_dev(*arrays), U.i32(table), scale, y, ws)
+    torch.cuda.synchronize()
+    return y
+
+
+def _queries(rng, tokens, heads, dim, x):
+    """Rows of nearly equal elements, about 1."""
+    q = torch.from_numpy((1.0 + 0.01 * rng.standard_normal((tokens, heads, 1)) + 0.002 * rng.standard_normal((tokens, heads, dim))).astype(np.float32)).to(U.TYPES[x])
+    return q.to(U.DEV), q.float().numpy()
+
+
+# ------------------------------------------------------------------------------------------------
+def _ladder(rng, dim, page, lens, heads, v_scales, gap):
+    """A cache in which every sequence's page i has values' scales v_scales[i % n] and scores that rise by `gap` nats from page to page."""
+    table, pages = U.page_tables(rng, [-(-n // page) for n in lens])
+    kc, vc, ks, vs = U.filled_cache(rng, pages, heads, page, dim)
+    vc[:] = rng.integers(20, 100, vc.shape)
+    for b, n in enumerate(lens):
+        for i in range(-(-n // page)):
+            kc[table[b, i]] = (25 if gap >= 0 else -25) * (i % 5 - 2) + rng.integers(-2, 3, kc[0].shape)
+            vs[table[b, i]] = v_scales[i % len(v_scales)]
+    ks[:] = (abs(gap) if gap else 1.0) / (25 * dim)
+    return table, (kc, vc, ks, vs)
+
+
+LADDERS = {"down": [2.0**(-59 * i) for i in range(3)], "up": [2.0**(59 * i - 118) for i in range(3)], "down by halves of it": [2.0**(-30 * i) for i in range(5)],
+           "zeros between": [1.0, 0.0, 2.0**-59, 0.0, 2.0**-118], "from zero": [0.0, 2.0**-100, 2.0**-40, 2.0**-126, 1.0], "up and down": [2.0**-60, 2.0**60, 2.0**-60, 1.0, 2.0**-59],
+           "wide": [2.0**100, 2.0**-20, 2.0**41, 2.0**-79, 2.0**-126]}
+
+
+@pytest.mark.parametrize("gap", [0.0, 41.0, -41.0])
+@pytest.mark.parametrize("ladder", list(LADDERS))
+@pytest.mark.parametrize("columns", ["many", "few"])
+def test_pages_whose_scales_fall_and_rise_step_by_step(columns, ladder, gap):
+    rng = np.random.default_rng(len(ladder))
+    dim, page, heads, most = 64, 64, (16, 8), 32 if columns == "many" else 2
+    batch = 50
+    lens = [int(n) for n in rng.integers(32, 320, batch)]
+    lens[:3] = [320, 192, 257]
+    queries = [most if b < 4 else 0 for b in range(batch)]
+    table, arrays = _ladder(rng, dim, page, lens, heads[1], LADDERS[ladder], gap)
+    q, qn = _queries(rng, sum(queries), heads[0], dim, "bf16")
+    print(f"[ladder] {columns} {ladder} gap={gap}", flush=True)
+    y = _attend(q, U.offsets(queries), lens, table, arrays, 1.0, most, 5000)
+    exact, bound = U.cache_rows(qn, U.offsets(queries), lens, table, *arrays, 1.0, "bf16", columns)
+    U.check(y, exact, bound, "ladder")
+
+
+def test_scales_that_fall_across_shares():
+    """The same with keys that are shared out: parts of very different units meet."""
+    rng = np.random.default_rng(12)
+    lens, queries = [1600, 900], [64, 33]
+    for name in LADDERS:
+        table, arrays = _ladder(rng, 64, 64, lens, 2, LADDERS[name], 20.0)
+        q, qn = _queries(rng, sum(queries), 4, 64, "bf16")
+        print(f"[ladder in shares] {name}", flush=True)
+        y = _attend(q, U.offsets(queries), lens, table, arrays, 1.0, 64, 1 << 20, one_share=False)
+        exact, bound = U.cache_rows(qn, U.offsets(queries), lens, table, *arrays, 1.0, "bf16", "many")
+        U.check(y, exact, bound, "ladder in shares")
