@@ -219,14 +219,16 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
             for (int t = 0; t < VT; ++t) o[t] *= keep;
         }
         const float off = top == -INFINITY ? 0.0f : top * a.factor;
+        float add = 0.0f;      // of the tile by itself: weights that the whole sum has no bit for count together
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], a.factor, -off));
-                sum += w;
+                add += w;
                 p[2 * t + e / 8][e % 8] = (T)w;
             }
+        sum += add;
     };
     // Step i: copies of the next tiles, PV of tile i, QK and softmax of tile i + 1.  A stage's keys are copied over when QK has read them,
     // a step before its values.  While one workgroup's wave on a SIMD is at the softmax the other's uses the matrix pipe; the priority of the

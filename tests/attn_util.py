@@ -151,3 +151,27 @@ def cache_rows(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, columns):
                 off = _off(p, y, v, delta, half_p, np.where(hidden, 0.0, floor)) + more
                 exact[rows, head], bound[rows, head] = y, HALF_STEP[x] * (np.abs(y) + off) + off + 2.0**-24 * (x == "f16") + 1e-36
     return exact, bound
+
+
+def prompt_rows(q, k, v, cu_q, cu_k, scale, causal, x):
+    """The same for the prompt's attention: weights rounded to the type; of fp16 those below 2^-36 of the largest vanish."""
+    dim, g = q.shape[2], q.shape[1] // k.shape[1]
+    exact, bound = np.zeros(q.shape), np.zeros(q.shape)
+    for b in range(len(cu_q) - 1):
+        rows, keys = slice(int(cu_q[b]), int(cu_q[b + 1])), slice(int(cu_k[b]), int(cu_k[b + 1]))
+        n, m = rows.stop - rows.start, keys.stop - keys.start
+        if not n or not m:
+            continue
+        hidden = causal & (np.arange(m)[None, :] > m - n + np.arange(n)[:, None])
+        for head in range(q.shape[1]):
+            qh, kh, vh = q[rows, head].astype(np.float64), k[keys, head // g].astype(np.float64), v[keys, head // g].astype(np.float64)
+            s = np.where(hidden, -np.inf, scale * (qh @ kh.T))
+            seen = ~hidden.all(1)
+            p = np.zeros_like(s)
+            p[seen] = _softmax(s[seen])
+            y = p @ vh
+            size = np.where(hidden, 0.0, scale * (np.abs(qh) @ np.abs(kh).T)).max(1, keepdims=True)
+            floor = np.where(hidden, 0.0, p.max(1, keepdims=True) * 2.0**-36 * (x == "f16"))
+            off = _off(p, y, vh, 2 * (dim + 16) * 2.0**-24 * size + 2.0**-21, HALF_STEP[x], floor)
+            exact[rows, head], bound[rows, head] = y, HALF_STEP[x] * (np.abs(y) + off) + off + 2.0**-24 * (x == "f16") + 1e-36
+    return exact, bound

@@ -1,4 +1,4 @@
-"""Attention where weights and values' scales are far apart: pages whose scales fall or rise by large factors."""
+"""Attention where weights and values' scales are far apart: long prompts under a dominating token, pages whose scales fall or rise by large factors."""
 import numpy as np
 import pytest
 import torch
@@ -72,3 +72,23 @@ def test_scales_that_fall_across_shares():
         y = _attend(q, U.offsets(queries), lens, table, arrays, 1.0, 64, 1 << 20, one_share=False)
         exact, bound = U.cache_rows(qn, U.offsets(queries), lens, table, *arrays, 1.0, "bf16", "many")
         U.check(y, exact, bound, "ladder in shares")
+
+
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [17.0, 17.7])
+def test_long_prompts_whose_weights_lie_in_one_token_and_all_others(x, gap):
+    """The dominating key's values are 1, all others 0: the sum that divides has to hold what 2^19 weights of e^-gap add up to."""
+    rng = np.random.default_rng(int(10 * gap))
+    dim, keys, n = 64, 1 << 19, 5
+    q, qn = _queries(rng, n, 2, dim, x)
+    k = (rng.integers(-20, 21, (keys, 1, dim)) / 100.0).astype(np.float32)
+    v = np.zeros((keys, 1, dim), np.float32)
+    k[0], v[0] = 1.0, 1.0
+    k, v = (torch.from_numpy(a).to(U.TYPES[x]) for a in (k, v))
+    y, cu_q, cu_k = torch.full_like(q, 7.0), [0, n], [0, keys]
+    print(f"[prompt sum] {x} gap={gap}", flush=True)
+    fq.fq_attn_prompt(q, k.to(U.DEV), v.to(U.DEV), U.i32(cu_q), U.i32(cu_k), n, gap / dim, y)
+    torch.cuda.synchronize()
+    exact, bound = U.prompt_rows(qn, k.float().numpy(), v.float().numpy(), cu_q, cu_k, gap / dim, True, x)
+    U.check(y, exact, bound, "prompt sum")
