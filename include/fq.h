@@ -427,7 +427,8 @@ int fq_gemm_select(int variant);
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
  *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider.  Up to 32 columns (query tokens times
  *   heads of a group), and beyond where the sizes leave little to compute, queries enter the first product as integers of 1 / 32512 of their head's
- *   largest magnitude and probabilities the second as fp16 (F16: as the sum of two); else both as fp16.
+ *   largest magnitude and probabilities the second as fp16 (F16: as the sum of two); else both as fp16.  So a probability counts as 0 where it is below
+ *   2^-32 of the largest and 2^-24 of that among its own 64 keys, or (both as fp16), times its values' scale, below 2^-36 of the largest such product.
  *   max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they and the number of rows, not the
  *   values on the device, set the launch, so a captured call may be replayed with other sequences within them.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
@@ -435,7 +436,7 @@ int fq_gemm_select(int variant);
  *   Y may be Q itself (same address and stride), else it must not overlap the inputs.
  *
  * fq_attn_prompt — the same over packed K and V: query i of n sees keys 0 .. m - n + i of the sequence's m (causal != 0), or all
- *   of them; a query that sees none gets 0.  Probabilities enter the second product in x_dtype.  Y as above.  Reads nothing of
+ *   of them; a query that sees none gets 0.  Probabilities enter the second product in x_dtype.  (F16: 0 below 2^-36 of the largest.)  Y as above.  Reads nothing of
  *   a sequence's neighbours; K and V of one sequence must be finite throughout.
  * ------------------------------------------------------------------------------------------- */
 int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim,

@@ -6,8 +6,8 @@
 //   its keys' scale goes into the factor of the scores; the keys stay 1152 too large each (see widen8), which adds 1152 times the sum of
 //     the query's elements to every score of a column and is taken off where the maximum is;
 //   its values' scale goes into P as an addend of the exponent.  So P's unit, which the accumulators count in, is the largest product of a weight and
-//     a scale so far, kept apart from the largest weight, which the sum counts in: whatever the scales, P is at most 1 (or the 2^8 that a unit may lag
-//     behind), neither is ever changed to something smaller, and what fp16 cannot hold of a P is little beside the largest one's products.
+//     a scale so far, kept apart from the largest weight, which the sum counts in: whatever the scales, neither is ever changed to something
+//     smaller, and what fp16 cannot hold of a P (HALF_SHIFT) is little beside the largest one's products.
 // Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 157 us and 8.4 for the join, 0.85 PFLOP/s at
 // 1.7 GHz; the matrix pipe is busy for 47 % of the cycles, the vector pipe for 57 %: 240 vector instructions a tile and wave beside 32 products, a third of them to
 // widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
@@ -235,7 +235,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
         m = __builtin_fmaf(over_halves_max(m), f, -shift);
         const float log_scale = fmaxf(__builtin_amdgcn_logf(at.v_scale), -200.0f);      // below 2^-126: 0, which counts as 2^-200
-        if (__ballot(m > top + SLACK || m + log_scale > unit + SLACK)) {
+        if (__ballot(m > top + HALF_SLACK || m + log_scale > unit + HALF_SLACK)) {
             const float now = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(top - now);
             top = now;
             sum *= keep;
@@ -245,7 +245,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
             for (int t = 0; t < VT; ++t) o[t] *= keep_o;
         }
         // the weight that has P = 1; far above the tile's largest (whose P are too small for fp16) 2^60 times that one, so that the sum still counts them
-        const float one = fminf(unit - log_scale, fmaxf(m, LOWEST) + 60.0f), off = one + shift;
+        const float one = fminf(unit - log_scale, fmaxf(m, LOWEST) + 60.0f) - HALF_SHIFT, off = one + shift;
         float add = 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -341,7 +341,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
     sum = over_halves_sum(sum);
     if (c >= columns) return;
-    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - top));      // twice, as the whole may be beyond fp32 where a product with it is not
+    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - HALF_SHIFT - top));      // twice, as the whole may be beyond fp32 where a product with it is not
     const size_t row = rows.first + (size_t)token;
     if (a.splits > 1) {
         const size_t at = (row * a.heads_q + head) * a.splits + split;

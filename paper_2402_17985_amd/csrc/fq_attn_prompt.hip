@@ -195,6 +195,7 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
     const std::true_type yes;
     const std::false_type no;
     // its probabilities
+    constexpr float LAG = DT == FQ_F16 ? HALF_SLACK : SLACK, SHIFT = DT == FQ_F16 ? HALF_SHIFT : 0.0f;      // bf16 holds all that fp32 does
     const auto softmax = [&](int i) {
         const int k0 = i * PROMPT_KEYS;
         // register e of tile t: key 32 t + 8 (e / 4) + 4 half + e % 4
@@ -211,14 +212,14 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
 #pragma unroll
         for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
         m = over_halves_max(m);
-        if (__ballot(top == -INFINITY || (m - top) * a.factor > SLACK)) {
+        if (__ballot(top == -INFINITY || (m - top) * a.factor > LAG)) {
             const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - now) * a.factor);
             top = now;
             sum *= keep;
 #pragma unroll
             for (int t = 0; t < VT; ++t) o[t] *= keep;
         }
-        const float off = top == -INFINITY ? 0.0f : top * a.factor;
+        const float off = (top == -INFINITY ? 0.0f : top * a.factor) - SHIFT;
         float add = 0.0f;      // of the tile by itself: weights that the whole sum has no bit for count together
 #pragma unroll
         for (int t = 0; t < 2; ++t)

@@ -110,7 +110,7 @@ def _off(p, y, v, delta, half_p, floor):
 
 def cache_rows(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, columns):
     """Exact results and how far they may be off, for sequences with queries.  columns "few": the kernel for up to 32 columns, whose queries are integers of
-    1 / 32512 of their largest, whose second product has 1152 too much in it (16 roundings a step) and whose weights below 2^-33 of a step's largest vanish;
+    1 / 32512 of their largest, whose second product has 1152 too much in it (16 roundings a step) and whose weights below 2^-24 of a step's largest vanish;
     "many": scores of codes plus 1152, logarithms of the values' scales, and weights times scales that vanish below 2^-36 of their largest."""
     page, pages, dim = kc.shape[2], kc.shape[0], q.shape[2]
     g = q.shape[1] // kc.shape[1]
@@ -140,7 +140,7 @@ def cache_rows(q, cu_q, lens, table, kc, vc, ks, vs, scale, x, columns):
                 fp32 = 2 * (dim + 16) * 2.0**-24 * np.where(hidden, 0.0, size).max(1, keepdims=True) + 2.0**-21
                 if columns == "few":
                     delta = fp32 + by_q / 65024
-                    floor = np.repeat(np.maximum.reduceat(p, np.arange(0, keys, 64), axis=1), 64, axis=1)[:, :keys] * 2.0**-33
+                    floor = np.repeat(np.maximum.reduceat(p, np.arange(0, keys, 64), axis=1), 64, axis=1)[:, :keys] * 2.0**-24
                     more = 16 * 2.0**-24 * 1280 * (p @ v_scale)[:, None]
                     half_p = 2.0**-22 if x == "f16" else 2.0**-11
                 else:

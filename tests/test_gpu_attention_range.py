@@ -1,4 +1,4 @@
-"""Attention where weights and values' scales are far apart: long prompts under a dominating token, pages whose scales fall or rise by large factors."""
+"""Attention where weights and values' scales are far apart: long caches and prompts under a dominating token, pages whose scales fall or rise by large factors."""
 import numpy as np
 import pytest
 import torch
@@ -92,3 +92,48 @@ def test_long_prompts_whose_weights_lie_in_one_token_and_all_others(x, gap):
     torch.cuda.synchronize()
     exact, bound = U.prompt_rows(qn, k.float().numpy(), v.float().numpy(), cu_q, cu_k, gap / dim, True, x)
     U.check(y, exact, bound, "prompt sum")
+
+
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("columns", ["few", "many"])
+@pytest.mark.parametrize("gap,spread", [(17.0, 20), (17.7, 20), (17.7, 0)])
+def test_long_caches_under_a_dominating_token(x, columns, gap, spread):
+    """One key holds nearly all the weight and its values are zero: the result is what the many others add up to, each of e^-gap."""
+    rng = np.random.default_rng(int(10 * gap) + spread)
+    dim, page, heads, batch, most = 64, 64, (8, 1), 300, 1 if columns == "few" else 16
+    lens = [131072, 70001] + [0] * (batch - 2)
+    queries = [most, most] + [0] * (batch - 2)
+    kc, vc, ks, vs = U.filled_cache(rng, 8, 1, page, dim)
+    kc[:] = rng.integers(-spread, spread + 1, kc.shape)
+    vc[:] = rng.integers(20, 61, vc.shape)
+    kc[0, 0, 0], vc[0, 0, :, 0] = 100, 0
+    ks[:], vs[:] = gap / (100 * dim), 1.0 / 64
+    table = np.full((batch, 2048), -1, np.int32)
+    for b in range(2):
+        table[b, 0], table[b, 1:] = 0, rng.integers(1, 8, 2047)
+    q, qn = _queries(rng, sum(queries), heads[0], dim, x)
+    print(f"[sink] {x} {columns} gap={gap} spread={spread}", flush=True)
+    y = _attend(q, U.offsets(queries), lens, table, (kc, vc, ks, vs), 1.0, most, 131072)
+    exact, bound = U.cache_rows(qn, U.offsets(queries), lens, table, kc, vc, ks, vs, 1.0, x, columns)
+    assert (bound < 0.1 * np.abs(exact)).all()
+    U.check(y, exact, bound, "sink")
+
+
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("gap", [17.0, 17.7])
+def test_long_prompts_under_a_dominating_token(x, gap):
+    rng = np.random.default_rng(int(10 * gap))
+    dim, keys, n = 64, 131072, 5
+    q, qn = _queries(rng, n, 2, dim, x)
+    k = (rng.integers(-20, 21, (keys, 1, dim)) / 100.0).astype(np.float32)
+    v = rng.integers(20, 61, (keys, 1, dim)).astype(np.float32) / np.float32(64.0)
+    k[0], v[0] = 1.0, 0.0
+    k, v = (torch.from_numpy(a.astype(np.float32)).to(U.TYPES[x]) for a in (k, v))
+    y, cu_q, cu_k = torch.full_like(q, 7.0), [0, n], [0, keys]
+    print(f"[prompt sink] {x} gap={gap}", flush=True)
+    fq.fq_attn_prompt(q, k.to(U.DEV), v.to(U.DEV), U.i32(cu_q), U.i32(cu_k), n, gap / dim, y)
+    torch.cuda.synchronize()
+    exact, bound = U.prompt_rows(qn, k.float().numpy(), v.float().numpy(), cu_q, cu_k, gap / dim, True, x)
+    assert (bound < 0.1 * np.abs(exact)).all()
+    U.check(y, exact, bound, "prompt sink")
