@@ -86,6 +86,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     v4i high[NT][KC], low[NT][KC];
     float factor[NT];
     int limit[NT];
+    bool spoiled[NT];      // a query that is not finite, with keys to see
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int c = c0 + 16 * n + col, cc = min(c, columns - 1), t = cc / a.group;
@@ -107,9 +108,11 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         uint16_t most_bits = most8[0];
 #pragma unroll
         for (int e = 1; e < 8; ++e) most_bits = max(most_bits, most8[e]);
-        float top = (float)__builtin_bit_cast(T, most_bits);
+        // no number counts as infinite: maxima would drop it
+        float top = (float)__builtin_bit_cast(T, min(most_bits, (uint16_t)(DT == FQ_F16 ? 0x7c00 : 0x7f80)));
         // the power of two first: the largest magnitude to [1, 2) (or what there is below), so that no size of query over- or underflows
         top = over_groups_max(top);
+        spoiled[n] = top == INFINITY && limit[n] > 0;
         const uint32_t power = min(max(__float_as_uint(top) >> 23, 1u), 253u);
         const float down = __uint_as_float((254u - power) << 23), up = __uint_as_float(power << 23);
         top *= down;
@@ -227,8 +230,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, s[n][t][i]);
             m = over_groups_max(m) * f;
-            if (__ballot(m > top[n] + SLACK)) {
-                const float now_top = fmaxf(m, top[n]), keep = now_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - now_top);
+            if (__ballot(m > top[n] + SLACK)) {      // only where it is so: a column's result does not depend on its neighbours
+                const float now_top = m > top[n] + SLACK ? m : top[n], keep = now_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - now_top);
                 top[n] = now_top;
                 sum[n] *= keep;
 #pragma unroll
@@ -241,7 +244,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             unit[n] = 1.0f;
             if (__ballot(m < base + STEP_SHIFT - SLACK)) {
                 asm volatile("");      // a branch
-                const float below = fminf(fmaxf(m, -0x1p100f) - base - STEP_SHIFT, 0.0f);
+                const float below = m < base + STEP_SHIFT - SLACK ? fmaxf(m, -0x1p100f) - base - STEP_SHIFT : 0.0f;
                 unit[n] = __builtin_amdgcn_exp2f(below);
                 base += below;
             }
@@ -302,7 +305,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
         float m = tops[0][16 * n + col];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][16 * n + col]);
-        const float mine = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - m);
+        // a spoiled query's integers mean nothing, and its result is to show that: no product with this is finite
+        const float mine = spoiled[n] ? INFINITY : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - m);
 #pragma unroll
         for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f*>(&gathered[wave][col][16 * t + 4 * g]) = o[n][t] * mine;
         __syncthreads();

@@ -1,4 +1,5 @@
-"""Attention where weights and values' scales are far apart: long caches and prompts under a dominating token, pages whose scales fall or rise by large factors."""
+"""Attention where weights and values' scales are far apart: long caches and prompts under a dominating token, pages whose scales fall or rise by large factors,
+queries that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -137,3 +138,39 @@ def test_long_prompts_under_a_dominating_token(x, gap):
     exact, bound = U.prompt_rows(qn, k.float().numpy(), v.float().numpy(), cu_q, cu_k, gap / dim, True, x)
     assert (bound < 0.1 * np.abs(exact)).all()
     U.check(y, exact, bound, "prompt sink")
+
+
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("queries,max_len", [([1, 1, 1, 1], 700), ([4, 2, 3, 0], 700), ([40, 33, 5, 0], 1 << 20), ([1, 1, 1, 1], 60000)])
+def test_queries_that_are_not_finite_show_and_stay_alone(x, bad, queries, max_len):
+    """A query with an element that is not finite gives no finite result (a plausible one would hide it), and leaves all other rows and heads as they
+    are; where it sees no key the result is 0 as ever."""
+    rng = np.random.default_rng(sum(queries))
+    lens, heads, dim = [600, 130, 200, 0], (8, 2), 128
+    table, pages = U.page_tables(rng, [-(-n // 64) for n in lens])
+    arrays, cu = U.filled_cache(rng, pages, heads[1], 64, dim), U.offsets(queries)
+    q, _ = U.packed(rng, sum(queries), heads[0], dim, x)
+    size = fq.fq_attn_cache_workspace_bytes(4, q.shape[0], max(queries), max_len, *heads, dim)
+    dev, ws, tab, cud, ln = U.to_dev(*arrays), torch.empty(size, dtype=torch.uint8, device=U.DEV), U.i32(table), U.i32(cu), U.i32(lens)
+
+    def call(rows):
+        y = torch.full(q.shape, 7.0, dtype=q.dtype, device=U.DEV)
+        fq.fq_attn_cache(rows, cud, ln, max(queries), max_len, *dev, tab, 0.09, y, ws)
+        torch.cuda.synchronize()
+        return y
+    print(f"[not finite] {x} {bad} queries={queries} max_len={max_len}", flush=True)
+    want, spoiled = call(q), q.clone()
+    at = [(0, 3, 5), (int(cu[1]), 0, 127), (int(cu[2]), 7, 64)] + ([(int(cu[3]), 1, 0)] if queries[3] else [])
+    for row, head, d in at:
+        spoiled[row, head, d] = bad
+    got = call(spoiled)
+    for row, head, _ in at[:3]:
+        assert not torch.isfinite(got[row, head]).any(), (row, head)
+    if queries[3]:
+        assert (got[int(cu[3])] == 0).all()
+    same = torch.ones(q.shape[:2], dtype=torch.bool, device=U.DEV)
+    for row, head, _ in at:
+        same[row, head] = False
+    assert torch.equal(got[same], want[same])
