@@ -1,10 +1,14 @@
-"""Buffer bookkeeping for the paged 8-bit key / value cache of one attention layer: owns the pages, their scales, the page table
-and the workspace that the C ABI wants, hands out pages, and forwards to the fq_* calls.  No arithmetic."""
+"""Buffer bookkeeping for the paged 8-bit key / value cache of one attention layer: owns the pages, their scales and the page table, hands out
+pages, and forwards to the fq_* calls.  No arithmetic."""
 from . import binding as B
 
 
 class FqKvCache:
-    """`pages` pages of `page_size` tokens, shared by up to `batch` sequences of at most `max_len` tokens each."""
+    """`pages` pages of `page_size` tokens, shared by up to `batch` sequences of at most `max_len` tokens each.
+
+    Calls go to the current stream.  attend() may run on several streams at once; reserve(), release() and append() change the table and the pages, and the
+    caller orders them with what else uses the cache.  append() and attend() copy their counts from the host, which waits for the stream: inside a captured
+    graph use the fq_* calls with counts on the device."""
 
     def __init__(self, pages: int, batch: int, max_len: int, heads_kv: int, head_dim: int, page_size: int = 64, rope_cos=None, rope_sin=None,
                  interleaved: bool = False, device="cuda:0"):
@@ -22,7 +26,6 @@ class FqKvCache:
         self.held = [[] for _ in range(batch)]      # page numbers of each sequence
         self.lengths = [0] * batch
         self._free = list(range(pages - 1, -1, -1))
-        self._ws = None
 
     def _i32(self, values):
         return self.torch.tensor(values, dtype=self.torch.int32, device=self.device)
@@ -74,8 +77,8 @@ class FqKvCache:
             Y = self.torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         max_q, max_len = max(1, max(queries)), max(1, max(self.lengths))
         size = B.fq_attn_cache_workspace_bytes(self.batch, Q.shape[0], max_q, max_len, Q.shape[1], self.k_cache.shape[1], Q.shape[2])
-        if self._ws is None or self._ws.numel() < size:
-            self._ws = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        # of this call: torch's allocator gives it to no other stream before the kernels are through
+        workspace = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
         B.fq_attn_cache(Q, self._i32(self._offsets(queries)), self._i32(self.lengths), max_q, max_len, self.k_cache, self.v_cache, self.k_scale,
-                        self.v_scale, self.page_table, scale, Y, self._ws)
+                        self.v_scale, self.page_table, scale, Y, workspace)
         return Y
