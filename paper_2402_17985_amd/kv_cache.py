@@ -37,6 +37,12 @@ class FqKvCache:
             at.append(at[-1] + n)
         return at
 
+    def _check_counts(self, name, counts, rows_of, rows):
+        if min(counts, default=0) < 0:
+            raise ValueError(f"{name} has a negative count")
+        if len(counts) != self.batch or sum(counts) != rows:
+            raise ValueError(f"{name} must say for each sequence how many of {rows_of}'s rows are its own")
+
     def reserve(self, b: int, tokens: int) -> None:
         """Pages for the first `tokens` tokens of sequence b; raises if it may not grow so long, or no page is free (nothing changes then)."""
         if tokens > self.max_len:
@@ -56,8 +62,7 @@ class FqKvCache:
 
     def append(self, Q, K, V, new, Q_out=None, K_out=None) -> None:
         """Append new[b] tokens to every sequence b (0: none): the rows of K, V (and Q) in order.  See fq_kv_append."""
-        if len(new) != self.batch or sum(new) != K.shape[0]:
-            raise ValueError("new must say for each sequence how many of K's rows are its own")
+        self._check_counts("new", new, "K", K.shape[0])
         grown = [n + m for n, m in zip(self.lengths, new)]
         wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held))
         if wanted > len(self._free) or max(grown) > self.max_len:
@@ -71,8 +76,7 @@ class FqKvCache:
 
     def attend(self, Q, queries, scale: float, Y=None):
         """Attention of the last queries[b] tokens of every sequence over all that the cache holds of it.  See fq_attn_cache."""
-        if len(queries) != self.batch or sum(queries) != Q.shape[0]:
-            raise ValueError("queries must say for each sequence how many of Q's rows are its own")
+        self._check_counts("queries", queries, "Q", Q.shape[0])
         if Y is None:
             Y = self.torch.empty(Q.shape, dtype=Q.dtype, device=Q.device)
         max_q, max_len = max(1, max(queries)), max(1, max(self.lengths))

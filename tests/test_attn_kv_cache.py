@@ -33,3 +33,27 @@ def test_attentions_under_way_at_once_have_workspaces_of_their_own(calls):
     assert len(spaces) == 3 and all(s.numel() > 16 for s in spaces)
     ends = sorted((s.data_ptr(), s.data_ptr() + s.numel()) for s in spaces)
     assert all(a[1] <= b[0] for a, b in zip(ends, ends[1:]))
+
+
+@pytest.mark.parametrize("new", [[3, -1], [-2, 4], [-1, -1]])
+def test_counts_below_zero_are_refused(calls, new):
+    """They would make offsets that fall, which the kernels cut, and lengths that the pages do not hold."""
+    c = _cache()
+    c.append(None, _rows(130), _rows(130), [70, 60])
+    before = (list(c.lengths), [list(h) for h in c.held])
+    with pytest.raises(ValueError, match="negative"):
+        c.append(None, _rows(max(0, sum(new))), _rows(max(0, sum(new))), new)
+    with pytest.raises(ValueError, match="negative"):
+        c.attend(_rows(max(0, sum(new))), new, 0.125)
+    assert (c.lengths, c.held) == before and len(calls) == 1
+
+
+def test_calls_get_offsets_lengths_and_bounds(calls):
+    c = _cache()
+    c.append(None, _rows(130), _rows(130), [70, 60])
+    c.append(None, _rows(1), _rows(1), [0, 1])
+    c.attend(_rows(3), [2, 1], 0.125)
+    (_, a, _), (_, b, _), (_, d, _) = calls
+    assert [t.tolist() for t in a[3:5]] == [[0, 70, 130], [0, 0]] and a[5] == 70
+    assert [t.tolist() for t in b[3:5]] == [[0, 0, 1], [70, 60]] and b[5] == 1
+    assert [t.tolist() for t in d[1:3]] == [[0, 2, 3], [70, 61]] and d[3:5] == (2, 70)
