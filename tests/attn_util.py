@@ -175,3 +175,17 @@ def prompt_rows(q, k, v, cu_q, cu_k, scale, causal, x):
             off = _off(p, y, vh, 2 * (dim + 16) * 2.0**-24 * size + 2.0**-21, HALF_STEP[x], floor)
             exact[rows, head], bound[rows, head] = y, HALF_STEP[x] * (np.abs(y) + off) + off + 2.0**-24 * (x == "f16") + 1e-36
     return exact, bound
+
+
+def error_ratio(got, exact, x):
+    """Root mean square of a result's errors, in units of what rounding the exact result to the type x alone gives."""
+    exact = torch.as_tensor(exact, dtype=torch.float64)
+    rounded = exact.to(TYPES[x]).double()
+    return float(((torch.as_tensor(got).double().cpu() - exact).square().mean() / (rounded - exact).square().mean()).sqrt())
+
+
+def ordinary_cache(rng, pages, heads, page, dim):
+    """Codes and scales as keys and values of about normal distribution give them."""
+    k, v = (np.clip(np.rint(rng.standard_normal(s) * 32.0), -127, 127).astype(np.int8) for s in ((pages, heads, page, dim), (pages, heads, dim, page)))
+    ks, vs = (np.exp(rng.standard_normal((pages, heads)) * 0.2).astype(np.float32) / np.float32(32.0) for _ in range(2))
+    return k, v, ks, vs
