@@ -425,7 +425,7 @@ int fq_gemm_select(int variant);
  *
  * fq_attn_cache — Y[i] = softmax(scale * Q[i] K^T) V over the cache: with n query tokens of sequence b and lens[b] tokens in the
  *   cache (the queries' own included), query i sees tokens 0 .. lens[b] - n + i.  A query that sees none gets 0.
- *   scale > 0.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider.  Up to 32 columns (query tokens times
+ *   scale > 0, at most 2.35e38.  F16 / BF16 in and out; scores, maxima, sums and the output accumulate in fp32 or wider.  Up to 32 columns (query tokens times
  *   heads of a group), and beyond where the sizes leave little to compute, queries enter the first product as integers of 1 / 32512 of their head's
  *   largest magnitude and probabilities the second as fp16 (F16: as the sum of two); else both as fp16.  So a probability counts as 0 where it is below
  *   2^-32 of the largest and 2^-24 of that among its own 64 keys, or (both as fp16), times its values' scale, below 2^-36 of the largest such product.

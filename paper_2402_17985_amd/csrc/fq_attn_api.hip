@@ -60,7 +60,8 @@ int check_batch(int batch, const char* what, int most)
 int check_attention(int x_dtype, float scale)
 {
     if (x_dtype != FQ_F16 && x_dtype != FQ_BF16) return fail(FQ_ERR_DTYPE, "dtype %d is not F16 or BF16", x_dtype);
-    if (!(scale > 0.0f) || std::isinf(scale)) return fail(FQ_ERR_RANGE, "scale = %g must be positive and finite", (double)scale);
+    // the kernels count in powers of two: scale * log2(e) must be finite as well
+    if (!(scale > 0.0f) || std::isinf(scale * 1.44269504f)) return fail(FQ_ERR_RANGE, "scale = %g must be positive and at most 2.35e38", (double)scale);
     return FQ_OK;
 }
 
