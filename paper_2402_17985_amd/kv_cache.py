@@ -8,7 +8,8 @@ class FqKvCache:
 
     Calls go to the current stream.  attend() may run on several streams at once; reserve(), release() and append() change the table and the pages, and the
     caller orders them with what else uses the cache.  append() and attend() copy their counts from the host, which waits for the stream: inside a captured
-    graph use the fq_* calls with counts on the device."""
+    graph use the fq_* calls with counts on the device.  A sequence's last tokens (rejected drafts) are dropped by setting lengths[b] to what stays: the next
+    ones take their places; its pages stay with it."""
 
     def __init__(self, pages: int, batch: int, max_len: int, heads_kv: int, head_dim: int, page_size: int = 64, rope_cos=None, rope_sin=None,
                  interleaved: bool = False, device="cuda:0"):
