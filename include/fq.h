@@ -429,8 +429,9 @@ int fq_gemm_select(int variant);
  *   heads of a group), and beyond where the sizes leave little to compute, queries enter the first product as integers of 1 / 32512 of their head's
  *   largest magnitude and probabilities the second as fp16 (F16: as the sum of two); else both as fp16.  So a probability counts as 0 where it is below
  *   2^-32 of the largest and 2^-24 of that among its own 64 keys, or (both as fp16), times its values' scale, below 2^-36 of the largest such product.
- *   max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out); they and the number of rows, not the
- *   values on the device, set the launch, so a captured call may be replayed with other sequences within them.
+ *   max_q and max_len bound the sequences' query tokens and lengths (what goes beyond is left out, as if it were not there); they and the number of
+ *   rows, not the values on the device, set the launch, so a captured call may be replayed with other sequences within them.  They choose the form for all
+ *   sequences of a call, too: single tokens beside a long piece of a prompt take its form, roundings and (long caches) up to a third more time than two calls.
  *   workspace  fq_attn_cache_workspace_bytes(...) bytes for the same sizes, 16-byte aligned; no part of it has to hold a value on entry.
  *   Calls that overlap (different streams) need a workspace each; calls and graphs that follow one another may share one.
  *   Y may be Q itself (same address and stride), else it must not overlap the inputs.

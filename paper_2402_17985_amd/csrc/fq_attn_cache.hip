@@ -19,8 +19,8 @@
 // reads as 16 consecutive bytes of a dimension (the cache holds values transposed for that) in the second product.
 // Each wave has a step of keys and values under way while it works on the one before, 16 KiB for heads of 128.  The waves of a workgroup share the keys
 // of one sequence and head, their parts meet in LDS; few workgroups share them once more, and a second kernel joins the shares.
-// Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 181 to 190 us, 5.7 to 5.9 TB/s (a large sum reads 6.0); two of 131072 tokens 97 us, 5.5 TB/s,
-// 5 us of it the join of 16 shares; one of 1001 tokens, 32 heads, 8.9 us, a chain of latencies: 2.5 to the first scores, 3 for 256 keys through one CU, the
+// Measured, reads of the cache: 64 sequences of 8192 tokens, 64 heads over 8, 181 to 190 us, 5.7 to 5.9 TB/s (a large sum reads 6.0); two of 131072 tokens 93 to 97 us, 5.5 to 5.8 TB/s,
+// 5 us of it the join of 16 shares; one of 1001 tokens, 32 heads, 8.5 us, a chain of latencies: 2.5 to the first scores, 3 for 256 keys through one CU, the
 // second launch.  Two steps under way instead of one, or the first step's loads before the queries', took up to 1 us more on short sequences, as
 // longer code has to come in first, and no less on long ones.
 #include "fq_attn_cache.h"

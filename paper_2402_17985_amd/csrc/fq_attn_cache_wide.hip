@@ -8,9 +8,9 @@
 //   its values' scale goes into P as an addend of the exponent.  So P's unit, which the accumulators count in, is the largest product of a weight and
 //     a scale so far, kept apart from the largest weight, which the sum counts in: whatever the scales, neither is ever changed to something
 //     smaller, and what fp16 cannot hold of a P (HALF_SHIFT) is little beside the largest one's products.
-// Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 157 us and 8.4 for the join, 0.85 PFLOP/s at
-// 1.7 GHz; the matrix pipe is busy for 47 % of the cycles, the vector pipe for 57 %: 240 vector instructions a tile and wave beside 32 products, a third of them to
-// widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
+// Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 153 to 163 us for the call, 0.85 PFLOP/s at 1.7 GHz
+// (under the profiler, with launches further apart, 157 and 8.4 for the join); the matrix pipe is busy for 48 % of the cycles, the vector pipe for 58 %: 240 vector
+// instructions a tile and wave beside 32 products, a third of them to widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
 // same: cache_plan).
 #include "fq_attn_cache.h"
 
