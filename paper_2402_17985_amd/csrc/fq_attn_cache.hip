@@ -229,7 +229,8 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, s[n][t][i]);
-            m = over_groups_max(m) * f;
+            const float largest = over_groups_max(m);
+            m = largest * f;
             if (__ballot(m > top[n] + SLACK)) {      // only where it is so: a column's result does not depend on its neighbours
                 const float now_top = m > top[n] + SLACK ? m : top[n], keep = now_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - now_top);
                 top[n] = now_top;
@@ -240,13 +241,19 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             // P's 1 is 2^7 (at most 2^15 with the slack).  Far below the running maximum it is the step's own largest weight that becomes 2^7, and the
             // product is turned to the running unit in 32 bits.  (In every step: 2 x 131072 tokens 98 us instead of 93, as a wave waits for its own
             // chain of instructions there.)
-            float base = (top[n] == -INFINITY ? 0.0f : top[n]) - STEP_SHIFT;
+            const float best = top[n] == -INFINITY ? 0.0f : top[n];
+            const bool apart = m < best - SLACK || fabsf(m) > FAR;
+            float base = best - STEP_SHIFT;
             unit[n] = 1.0f;
-            if (__ballot(m < base + STEP_SHIFT - SLACK)) {
+            if (__builtin_expect(__ballot(apart) != 0, false)) {
                 asm volatile("");      // a branch
-                const float below = m < base + STEP_SHIFT - SLACK ? fmaxf(m, -0x1p100f) - base - STEP_SHIFT : 0.0f;
+                const float under = fmaxf(m, -0x1p100f) - best, below = under < -SLACK ? under : 0.0f, less = apart && m != -INFINITY ? largest : 0.0f;
                 unit[n] = __builtin_amdgcn_exp2f(below);
-                base += below;
+                base = apart ? below - under - STEP_SHIFT : base;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][t][i] -= less;
             }
             float add = 0.0f;
             const v2h ones = {(_Float16)1.0f, (_Float16)1.0f};

@@ -178,7 +178,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[t][e] = 0.0f;
     float top = LOWEST, sum = 0.0f;                      // of the scaled scores; over this lane's keys
-    float unit = LOWEST;                                 // log2 of what o counts in: weights times values' scales
+    float unit = LOWEST;                                 // log2 of what o counts in, weights times values' scales, less top
     v8h p[4];                                            // 16 keys each
 
     uint32_t key_at[KS], value_at[4];
@@ -218,7 +218,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
     const auto nothing = [](int) {};
     const std::true_type yes;
     const std::false_type no;
-    const auto softmax = [&](int i, const Place& at) {
+    const auto softmax = [&](int i, const Place& at) __attribute__((always_inline)) {
         const int k0 = from + CACHE_STEP * i;
         const float f = fmaxf(factor * at.k_scale, 0x1p-126f), shift = bias * f;      // f is not 0: that times a masked score would be no number
         if (k0 + CACHE_STEP > least || !at.exists) {
@@ -233,19 +233,32 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         float m = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
-        m = __builtin_fmaf(over_halves_max(m), f, -shift);
+        const float largest = fmaxf(over_halves_max(m), LOWEST);
+        m = fmaxf(__builtin_fmaf(largest, f, -shift), LOWEST);
         const float log_scale = fmaxf(__builtin_amdgcn_logf(at.v_scale), -200.0f);      // below 2^-126: 0, which counts as 2^-200
-        if (__ballot(m > top + HALF_SLACK || m + log_scale > unit + HALF_SLACK)) {
-            const float now = fmaxf(m, top), keep = __builtin_amdgcn_exp2f(top - now);
-            top = now;
-            sum *= keep;
-            const float now_unit = fmaxf(m + log_scale, unit), keep_o = __builtin_amdgcn_exp2f(unit - now_unit);
-            unit = now_unit;
+        float above = m - top;
+        if (__ballot(above > HALF_SLACK || above + log_scale > unit + HALF_SLACK)) {
+            const float rise = fmaxf(above, 0.0f);
+            top = fmaxf(m, top);
+            above -= rise;
+            sum *= __builtin_amdgcn_exp2f(-rise);
+            const float now = fmaxf(above + log_scale, unit - rise), keep = __builtin_amdgcn_exp2f(unit - rise - now);
+            unit = now;
 #pragma unroll
-            for (int t = 0; t < VT; ++t) o[t] *= keep_o;
+            for (int t = 0; t < VT; ++t) o[t] *= keep;
         }
-        // the weight that has P = 1; far above the tile's largest (whose P are too small for fp16) 2^60 times that one, so that the sum still counts them
-        const float one = fminf(unit - log_scale, fmaxf(m, LOWEST) + 60.0f) - HALF_SHIFT, off = one + shift;
+        // from the tile's largest weight to that with P = 1; where its P are too small for fp16, 2^60 at most, so that the sum still counts them
+        const float to_one = fminf(unit - log_scale - above, 60.0f) - HALF_SHIFT;
+        float off = __builtin_fmaf(largest, f, to_one);
+        if (__ballot(fabsf(off) > FAR)) {
+            asm volatile("");
+            const float less = fabsf(off) > FAR ? largest : 0.0f;
+            off = fabsf(off) > FAR ? to_one : off;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] -= less;
+        }
         float add = 0.0f;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -255,7 +268,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
                 add += w;
                 p[2 * t + e / 8][e % 8] = (_Float16)w;
             }
-        sum = __builtin_fmaf(add, __builtin_amdgcn_exp2f(one - top), sum);
+        sum = __builtin_fmaf(add, __builtin_amdgcn_exp2f(to_one + above), sum);
     };
 
     // Step i: what has arrived goes into LDS (keys of tile i + 2, values of i + 1), more is asked for (keys of i + 4, values of i + 3), PV of
@@ -341,7 +354,7 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
     sum = over_halves_sum(sum);
     if (c >= columns) return;
-    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - HALF_SHIFT - top));      // twice, as the whole may be beyond fp32 where a product with it is not
+    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - HALF_SHIFT));      // twice, as the whole may be beyond fp32 where a product with it is not
     const size_t row = rows.first + (size_t)token;
     if (a.splits > 1) {
         const size_t at = (row * a.heads_q + head) * a.splits + split;

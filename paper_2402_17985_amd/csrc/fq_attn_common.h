@@ -29,6 +29,9 @@ constexpr float SLACK = 8.0f;   // accumulators are rescaled only when a maximum
 // Where accumulators run over all keys with probabilities in fp16 it is 2^4, and a probability's 1 is 2^11: at most 2^15 then, and what is below 2^-36 of the
 // largest vanishes, little even of 2^17 of them (as 1 and 2^8 everything below 2^-25 did: the whole of 131072 keys 17.7 nats below one).
 constexpr float HALF_SLACK = 4.0f, HALF_SHIFT = 11.0f;
+// Exponents of probabilities are one fused product and sum, s f - off, whose off is rounded as scores of its size are.  Beyond this the largest score is taken off
+// first: half a step of off would make the largest probability too large for fp16 from 2^24 on.
+constexpr float FAR = 0x1p16f;
 constexpr float LOG2E = 1.44269504088896340736f;
 
 template <int DT> struct Mma;

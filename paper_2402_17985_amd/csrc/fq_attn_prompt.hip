@@ -196,7 +196,9 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
     const std::false_type no;
     // its probabilities
     constexpr float LAG = DT == FQ_F16 ? HALF_SLACK : SLACK, SHIFT = DT == FQ_F16 ? HALF_SHIFT : 0.0f;      // bf16 holds all that fp32 does
-    const auto softmax = [&](int i) {
+    float off = -SHIFT;            // what is taken off a scaled score: its maximum, or (far) nothing, as the unscaled one is taken off the score before
+    bool any_far = false;          // in this wave
+    const auto softmax = [&](int i) __attribute__((always_inline)) {
         const int k0 = i * PROMPT_KEYS;
         // register e of tile t: key 32 t + 8 (e / 4) + 4 half + e % 4
         if (k0 + PROMPT_KEYS > least) {
@@ -215,11 +217,21 @@ template <int DT, int D> __global__ __launch_bounds__(PROMPT_THREADS, D == 64 ? 
         if (__ballot(top == -INFINITY || (m - top) * a.factor > LAG)) {
             const float now = fmaxf(m, top), keep = now == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((top - now) * a.factor);
             top = now;
+            const bool far = fabsf(top * a.factor) > FAR && top != -INFINITY;
+            off = (far || top == -INFINITY ? 0.0f : top * a.factor) - SHIFT;
+            any_far = __ballot(far) != 0;
             sum *= keep;
 #pragma unroll
             for (int t = 0; t < VT; ++t) o[t] *= keep;
         }
-        const float off = (top == -INFINITY ? 0.0f : top * a.factor) - SHIFT;
+        if (__builtin_expect(any_far, false)) {
+            asm volatile("");
+            const float less = fabsf(top * a.factor) > FAR && top != -INFINITY ? top : 0.0f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[t][e] -= less;
+        }
         float add = 0.0f;      // of the tile by itself: weights that the whole sum has no bit for count together
 #pragma unroll
         for (int t = 0; t < 2; ++t)
