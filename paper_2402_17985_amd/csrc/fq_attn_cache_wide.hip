@@ -233,8 +233,9 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
         float m = fmaxf(s[0][0], s[1][0]);
 #pragma unroll
         for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, s[0][e]), s[1][e]);
-        const float largest = fmaxf(over_halves_max(m), LOWEST);
-        m = fmaxf(__builtin_fmaf(largest, f, -shift), LOWEST);
+        m = over_halves_max(m);
+        const float largest = fmaxf(m, LOWEST);
+        m = fmaxf(__builtin_fmaf(m, f, -shift), LOWEST);      // infinite where none is visible: LOWEST whatever f
         const float log_scale = fmaxf(__builtin_amdgcn_logf(at.v_scale), -200.0f);      // below 2^-126: 0, which counts as 2^-200
         float above = m - top;
         if (__ballot(above > HALF_SLACK || above + log_scale > unit + HALF_SLACK)) {
@@ -354,7 +355,9 @@ template <int DT, int D> __global__ __launch_bounds__(WIDE_THREADS, 2) void attn
 
     sum = over_halves_sum(sum);
     if (c >= columns) return;
-    const float half_unit = __builtin_amdgcn_exp2f(0.5f * (unit - HALF_SHIFT));      // twice, as the whole may be beyond fp32 where a product with it is not
+    // Twice, as the whole may be beyond fp32 where a product with it is not.  Where the query is not finite (nor its sum then), no product with it is.
+    const bool spoiled = (__float_as_uint(bias) & 0x7f800000u) == 0x7f800000u && mine > 0;
+    const float half_unit = spoiled ? INFINITY : __builtin_amdgcn_exp2f(0.5f * (unit - HALF_SHIFT));
     const size_t row = rows.first + (size_t)token;
     if (a.splits > 1) {
         const size_t at = (row * a.heads_q + head) * a.splits + split;

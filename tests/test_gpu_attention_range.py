@@ -174,3 +174,41 @@ def test_queries_that_are_not_finite_show_and_stay_alone(x, bad, queries, max_le
     for row, head, _ in at:
         same[row, head] = False
     assert torch.equal(got[same], want[same])
+
+
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("columns", ["many", "few", "shares"])
+@pytest.mark.parametrize("nats", [-300.0, -100000.0])
+def test_pages_that_do_not_exist_beside_scores_far_below_zero(x, columns, nats):
+    """A page that is left out has scales of 0; it must not pass for scores of 0."""
+    rng = np.random.default_rng(int(-nats))
+    dim, heads = 64, (8, 2)
+    batch, most = (2, 40) if columns == "shares" else (200, 20 if columns == "many" else 1)
+    lens, queries = [700, 300] + [0] * (batch - 2), [most, min(most, 33)] + [0] * (batch - 2)
+    table, pages = U.page_tables(rng, [-(-n // 64) for n in lens])
+    kc, vc, ks, vs = U.filled_cache(rng, pages, heads[1], 64, dim)
+    kc[:] = rng.integers(-101, -99, kc.shape)
+    ks[:] = -nats / (100 * dim)
+    for b, i in ((0, 0), (0, 5), (0, 10), (1, 4)):
+        table[b, i] = -1
+    cu = U.offsets(queries)
+    q, qn = _queries(rng, sum(queries), heads[0], dim, x)
+    print(f"[missing pages] {x} {columns} {nats}", flush=True)
+    y = _attend(q, cu, lens, table, (kc, vc, ks, vs), 1.0, most, 1 << 20 if columns == "shares" else 700, one_share=columns != "shares")
+    assert torch.isfinite(y).all()
+    for b in range(2):
+        there = np.repeat(table[b, :-(-lens[b] // 64)] >= 0, 64)[:lens[b]]
+        for head in (0, 3, 5):
+            at, h = np.maximum(table[b, :-(-lens[b] // 64)], 0), head // 4
+            k = kc[at, h].reshape(-1, dim)[:lens[b]].astype(np.float64) * ks[0, 0]
+            v = (vc[at, h].transpose(0, 2, 1) * vs[at, h][:, None, None].astype(np.float64)).reshape(-1, dim)[:lens[b]]
+            for i in range(queries[b]):
+                row = int(cu[b]) + i
+                seen = there & (np.arange(lens[b]) <= lens[b] - queries[b] + i)
+                s = k[seen] @ qn[row, head].astype(np.float64)
+                assert s.max() < nats / 2
+                got, size = y[row, head].float().cpu().numpy(), np.abs(v[seen]).max(0)
+                if nats == -300.0:      # a score's sums and the fused exponent are off by 2^-15 of it at most (1152 is nine times the codes): 1 % of a weight
+                    w = np.exp(s - s.max())
+                    assert (np.abs(got - w @ v[seen] / w.sum()) <= 0.03 * (w @ np.abs(v[seen]) / w.sum()) + U.HALF_STEP[x] * size).all()
+                assert np.abs(got).max() > 0 and (np.abs(got) <= 1.01 * size).all()
