@@ -39,5 +39,8 @@ __device__ __forceinline__ v8h widen8(uint32_t lo, uint32_t hi)
 }
 constexpr float WIDEN_BIAS = 1152.0f;
 
+// The maximum of no scores: below every score, and finite, so that differences of maxima are numbers.
+constexpr float LOWEST = -0x1p100f;
+
 }  // namespace
 }  // namespace fq

@@ -138,7 +138,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
     float top[NT], sum[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        top[n] = -INFINITY;
+        top[n] = LOWEST;
         sum[n] = 0.0f;
 #pragma unroll
         for (int t = 0; t < VT; ++t) o[n][t] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
@@ -230,10 +230,12 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
 #pragma unroll
                 for (int i = 0; i < 4; ++i) m = fmaxf(m, s[n][t][i]);
             const float largest = over_groups_max(m);
-            m = largest * f;
-            if (__ballot(m > top[n] + SLACK)) {      // only where it is so: a column's result does not depend on its neighbours
-                const float now_top = m > top[n] + SLACK ? m : top[n], keep = now_top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - now_top);
-                top[n] = now_top;
+            m = fmaxf(largest * f, LOWEST);
+            float above = m - top[n];      // of large scores a single step can be more than the slack
+            if (__ballot(above > SLACK)) {      // only where it is so: a column's result does not depend on its neighbours
+                const float rise = above > SLACK ? above : 0.0f, keep = __builtin_amdgcn_exp2f(-rise);
+                top[n] = above > SLACK ? m : top[n];
+                above -= rise;
                 sum[n] *= keep;
 #pragma unroll
                 for (int t = 0; t < VT; ++t) o[n][t] *= keep;
@@ -241,15 +243,14 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             // P's 1 is 2^7 (at most 2^15 with the slack).  Far below the running maximum it is the step's own largest weight that becomes 2^7, and the
             // product is turned to the running unit in 32 bits.  (In every step: 2 x 131072 tokens 98 us instead of 93, as a wave waits for its own
             // chain of instructions there.)
-            const float best = top[n] == -INFINITY ? 0.0f : top[n];
-            const bool apart = m < best - SLACK || fabsf(m) > FAR;
-            float base = best - STEP_SHIFT;
+            const bool apart = above < -SLACK || fabsf(m) > FAR;
+            float base = top[n] - STEP_SHIFT;
             unit[n] = 1.0f;
             if (__builtin_expect(__ballot(apart) != 0, false)) {
                 asm volatile("");      // a branch
-                const float under = fmaxf(m, -0x1p100f) - best, below = under < -SLACK ? under : 0.0f, less = apart && m != -INFINITY ? largest : 0.0f;
+                const float below = above < -SLACK ? above : 0.0f, less = apart ? fmaxf(largest, LOWEST) : 0.0f;
                 unit[n] = __builtin_amdgcn_exp2f(below);
-                base = apart ? below - under - STEP_SHIFT : base;
+                base = apart ? below - above - STEP_SHIFT : base;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -313,7 +314,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][16 * n + col]);
         // a spoiled query's integers mean nothing, and its result is to show that: no product with this is finite
-        const float mine = spoiled[n] ? INFINITY : m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[n] - m);
+        const float mine = spoiled[n] ? INFINITY : __builtin_amdgcn_exp2f(top[n] - m);
 #pragma unroll
         for (int t = 0; t < VT; ++t) *reinterpret_cast<v4f*>(&gathered[wave][col][16 * t + 4 * g]) = o[n][t] * mine;
         __syncthreads();
@@ -326,7 +327,7 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             v4f y = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
-                if (best != -INFINITY) l += sums[w][16 * n + cl] * __builtin_amdgcn_exp2f(tops[w][16 * n + cl] - best);
+                l += sums[w][16 * n + cl] * __builtin_amdgcn_exp2f(tops[w][16 * n + cl] - best);
                 y += *reinterpret_cast<const v4f*>(&gathered[w][cl][d]);
             }
             const int t = c / a.group, head = h * a.group + c - t * a.group;

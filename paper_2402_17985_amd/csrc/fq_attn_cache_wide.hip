@@ -18,7 +18,6 @@ namespace fq {
 namespace {
 
 constexpr int WIDE_WAVES = WIDE_COLUMNS / 32, WIDE_THREADS = 64 * WIDE_WAVES;
-constexpr float LOWEST = -0x1p100f;      // below every score, and finite: differences of two are numbers
 
 // Where piece 2 e + half of row r lies among its row's C: both the eight lanes that write neighbouring pairs' first (or second) pieces and the
 // 16 rows that are read at a time, the same piece of each, then meet all banks.  (Widths of 10 and 12 pieces are only turned for the reads.)

@@ -73,3 +73,29 @@ def test_prompt_attention_of_huge_scores(x, dim, scale):
             clear += _check(y[rows, head], qn[rows, head].astype(np.float64), kn[cu[b]:cu[b + 1], head // 2].astype(np.float64), vn[cu[b]:cu[b + 1], head // 2].astype(np.float64), scale,
                             np.arange(n)[None] > 1 + np.arange(n - 1)[:, None], x, U.HALF_STEP[x], f"{b} {head}")
     assert clear >= 100
+
+
+@pytest.mark.parametrize("x", ["bf16", "f16"])
+@pytest.mark.parametrize("columns", ["few", "many"])
+def test_scores_that_grow_by_single_steps_of_fp32(x, columns):
+    """Pages whose keys' scales are neighbours in fp32: scores of 2^24 to 2^31 that differ by one step, which may be less, as much or more than what the running
+    maximum may lag behind."""
+    rng = np.random.default_rng(3)
+    dim, page, heads, batch, most = 64, 64, (32, 4), 130, 1 if columns == "few" else 5
+    lens, queries = [1500] * 8 + [0] * (batch - 8), [most] * 8 + [0] * (batch - 8)
+    table, pages = U.page_tables(rng, [-(-n // page) for n in lens])
+    kc, vc, ks, vs = U.filled_cache(rng, pages, heads[1], page, dim)
+    kc[:], vs[:] = 100, 1.0
+    one = np.float32(0.01)
+    for b in range(8):
+        for i in range(-(-lens[b] // page)):
+            ks[table[b, i]] = (one.view(np.int32) + i // 4).view(np.float32)
+    q, _ = U.packed(rng, sum(queries), heads[0], dim, x)
+    q = q.abs()
+    y, ws = torch.full_like(q, 7.0), torch.empty(16, dtype=torch.uint8, device=U.DEV)
+    for power in range(24, 32):
+        print(f"[single steps] {x} {columns} 2^{power}", flush=True)
+        fq.fq_attn_cache(q, U.i32(U.offsets(queries)), U.i32(lens), most, 1500, *U.to_dev(kc, vc, ks, vs), U.i32(table), 2.0**power / 70.0, y, ws)
+        torch.cuda.synchronize()
+        n = sum(queries)
+        assert torch.isfinite(y[:n]).all() and (y[:n].abs() <= 129).all()
