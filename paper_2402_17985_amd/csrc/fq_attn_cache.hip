@@ -56,7 +56,7 @@ __device__ __forceinline__ int by_length(const CacheAttn& a, int z, int batch)
     return __builtin_ctzll(__ballot(lane < batch && longer == nth));
 }
 
-constexpr float STEP_SHIFT = 7.0f;      // log2 of what a probability of 1 is in fp16
+constexpr float STEP_SHIFT = 7.0f, STEP_UNIT = 0x1p-7f;      // a probability of 1 is 2^7 in fp16; accumulators and sums count in 1
 
 // NT tiles of 16 columns.  Grid: x the shares of the keys, y the key heads of one block of columns after the other (with 8 key heads the blocks of one are on
 // one XCD), z the sequences.
@@ -245,11 +245,11 @@ template <int DT, int D, int NT, int WAVES> __global__ __launch_bounds__(64 * WA
             // chain of instructions there.)
             const bool apart = above < -SLACK || fabsf(m) > FAR;
             float base = top[n] - STEP_SHIFT;
-            unit[n] = 1.0f;
+            unit[n] = STEP_UNIT;
             if (__builtin_expect(__ballot(apart) != 0, false)) {
                 asm volatile("");      // a branch
                 const float below = above < -SLACK ? above : 0.0f, less = apart ? fmaxf(largest, LOWEST) : 0.0f;
-                unit[n] = __builtin_amdgcn_exp2f(below);
+                unit[n] = __builtin_amdgcn_exp2f(below - STEP_SHIFT);
                 base = apart ? below - above - STEP_SHIFT : base;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)

@@ -62,6 +62,20 @@ def test_pages_whose_scales_fall_and_rise_step_by_step(columns, ladder, gap):
     U.check(y, exact, bound, "ladder")
 
 
+@pytest.mark.parametrize("columns", ["many", "few"])
+def test_values_near_the_largest(columns):
+    """Values of up to 2^115: what the accumulators hold of 320 of them is still a number."""
+    rng = np.random.default_rng(4)
+    most, batch = 32 if columns == "many" else 2, 50
+    lens, queries = [320, 200, 64] + [0] * (batch - 3), [most] * 3 + [0] * (batch - 3)
+    table, arrays = _ladder(rng, 64, 64, lens, 8, [2.0**108, 2.0**107, 2.0**90], 0.0)
+    q, qn = _queries(rng, sum(queries), 16, 64, "bf16")
+    print(f"[near the largest] {columns}", flush=True)
+    y = _attend(q, U.offsets(queries), lens, table, arrays, 1.0, most, 5000)
+    exact, bound = U.cache_rows(qn, U.offsets(queries), lens, table, *arrays, 1.0, "bf16", columns)
+    U.check(y, exact, bound, "near the largest")
+
+
 def test_scales_that_fall_across_shares():
     """The same with keys that are shared out: parts of very different units meet."""
     rng = np.random.default_rng(12)
