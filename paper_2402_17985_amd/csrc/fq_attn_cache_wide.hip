@@ -9,9 +9,9 @@
 //     a scale so far, kept apart from the largest weight, which the sum counts in: whatever the scales, neither is ever changed to something
 //     smaller, and what fp16 cannot hold of a P (HALF_SHIFT) is little beside the largest one's products.
 // Measured: 512 tokens behind 7680, 64 heads of 128 over 8 (256 workgroups of columns, keys in two shares): 153 to 163 us for the call, 0.85 PFLOP/s at 1.7 GHz
-// (under the profiler, with launches further apart, 157 and 8.4 for the join); the matrix pipe is busy for 48 % of the cycles, the vector pipe for 58 %: 240 vector
-// instructions a tile and wave beside 32 products, a third of them to widen and store its part of the codes.  By 64 columns straight from registers, as the kernel for few columns works, 268 us (where that one is faster all the
-// same: cache_plan).
+// (under the profiler, with launches further apart, 157 and 8.4 for the join); the matrix pipe is busy for 48 % of the cycles, the vector pipe for 58 %: 240
+// vector instructions a tile and wave beside 32 products, a third of them to widen and store its part of the codes.  By 64 columns straight from registers, as the
+// kernel for few columns works, 268 us (where that one is faster all the same: cache_plan).
 #include "fq_attn_cache.h"
 
 namespace fq {
