@@ -357,6 +357,57 @@ int fq_linear_fused_a_i8(const void* X, int x_dtype, int M, int K, int ldx, cons
                          void* Y, int y_dtype, int ldy, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * fq_rms_norm_quant — what stands ahead of a quantized layer: the residual's addition, the root-mean-square norm, and the
+ * norm's result as fq_flatten_quant_act would quantize it, without being written and read in between.
+ *
+ *   h[i,j] = round_to_r_dtype(fl32(X[i,j] + R[i,j])), stored in R_out; without R (R = R_out = NULL) h = X
+ *   t_i    = fl32(1 / sqrt(sum_j h[i,j]^2 / K + eps)), formed in float64
+ *   y[i,j] = fl32(fl32(h[i,j] * t_i) * gamma[j])
+ *   Y      = y rounded to y_dtype (NULL: not wanted)
+ *   Xq_out, s_x_out (NULL: not wanted; not both Y and Xq_out): codes and scale of the fp32 y by the map, in the storage of `bits`,
+ *            exactly as fq_flatten_quant_act: static bound *absmax_in, or dynamic (absmax_in == NULL).
+ *
+ * X [M, K], R, R_out [M, K], Y [M, K]: F32 / F16 / BF16 each, 16-byte aligned, row strides of a multiple of 16 bytes (R_out has R's type).
+ *   Elements between K and a stride are neither read nor written.  gamma [K], g_dtype F32 / F16 / BF16, dense.  eps > 0, finite.
+ *   K <= 32768; map, Kpad and bits as for fq_flatten_quant_act (src_idx, rep unused without Xq_out).
+ *   Sums X + R must be finite in r_dtype, and a row's root mean square below 2^126 (t_i is subnormal beyond).
+ * R_out may be R or X itself, Y may be X or R itself (same address, type and stride; Y and R_out apart); else outputs must not overlap
+ *   inputs or each other.
+ * workspace  fq_rms_norm_workspace_bytes(M, K, Kpad) bytes, device, 16-byte aligned; no part of it has to hold a value on entry.  Needed with
+ *   Xq_out and a dynamic scale only (else NULL and 0 will do).  Calls that overlap (different streams) need one each.
+ * ------------------------------------------------------------------------------------------- */
+int fq_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, const void* R, int r_dtype, int ldr, void* R_out, int ldro,
+                      const void* gamma, int g_dtype, float eps, void* Y, int y_dtype, int ldy,
+                      const int32_t* src_idx, const int32_t* rep, int Kpad, int bits, const float* absmax_in,
+                      void* Xq_out, float* s_x_out, void* workspace, size_t workspace_bytes, void* stream);
+size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
+
+/* ---------------------------------------------------------------------------------------------
+ * 4-bit weights with a scale for each row and group of columns, for layers that one scale per tensor does not serve; activations
+ * stay as they are (no flattening).
+ *
+ *   w[n,k] = S[n, k / group] * q[n,k] + B[n, k / group]        q in [-8, 7];  B NULL: no offsets
+ *   Wq  [N, K / 2] bytes, two's-complement nibbles, even column in the low one; rows dense.  K a multiple of 32.
+ *   S, B  [N, ceil(K / group)], dense, s_dtype F32 / F16 / BF16; group 32, 64 or 128; a row's last group may be a short one.
+ *
+ * fq_group_weights_i4 — offline: the weights' codes, scales and offsets.  W [N, K] F32 / F16 / BF16, row stride ldw (a multiple of 16 bytes).
+ *   Over a row's group, without offsets (B_out == NULL):  s = fl32(max|w| / 7);
+ *                       with offsets, lo and hi being its least and largest element:  s = fl32(fl32(hi - lo) / 15);
+ *   s is rounded to s_dtype, at most that type's largest finite value, and 0 where below 2^-126;  b = fl32(lo + fl32(8 s)), rounded
+ *   likewise (between -largest and largest);  q = clamp(rne(fl32(fl32(w - b) * fl32(1 / s))), -8, 7), 0 for s = 0  (b = 0 without offsets).
+ *
+ * fq_linear_group_i4 — Y[i,n] = round_to_y_dtype(sum_k X[i,k] * w[n,k] + bias[n]).
+ *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
+ *   Products of activations and codes are exact (BF16: codes enter as q + 24, whose surplus leaves with the activations' sum); sums, and scales
+ *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights; no limit on M.
+ *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.
+ * ------------------------------------------------------------------------------------------- */
+int fq_group_weights_i4(const void* W, int w_dtype, int N, int K, int ldw, int group, void* Wq_out, void* S_out, void* B_out, int s_dtype,
+                        void* stream);
+int fq_linear_group_i4(const void* X, int x_dtype, int M, int K, int ldx, const void* Wq, const void* S, const void* B, int s_dtype, int group,
+                       int N, const float* bias, void* Y, int y_dtype, int ldy, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * fq_gemm_bf16 — the unquantized baseline the paper compares against (Table 5, "Gemm (FP16)"):
  * Y = X W^T with bf16 operands, fp32 accumulation on the bf16 MFMA, bf16 output.
  * X [M, K], W [N, K] device bf16, dense rows; K a multiple of 8.  Y [M, N] bf16, row stride ldy.
@@ -439,6 +490,10 @@ int fq_gemm_select(int variant);
  * fq_attn_prompt — the same over packed K and V: query i of n sees keys 0 .. m - n + i of the sequence's m (causal != 0), or all
  *   of them; a query that sees none gets 0.  Probabilities enter the second product in x_dtype.  (F16: 0 below 2^-36 of the largest.)  Y as above.  Reads nothing of
  *   a sequence's neighbours; K and V of one sequence must be finite throughout.
+ *
+ * fq_kv_copy_pages — page to[i] becomes a copy of page from[i], i < count: codes and scales, keys and values.  What a server forks, defragments or
+ *   moves sequences with; the page tables are the caller's.  from, to int32 [count], device; a pair with a number outside [0, pages) copies
+ *   nothing.  No page named in `to` may be named a second time, in `to` or in `from` (a pair of equal numbers aside).  count may be 0.
  * ------------------------------------------------------------------------------------------- */
 int fq_kv_append(const void* Q, const void* K, const void* V, int x_dtype, int tokens, int heads_q, int heads_kv, int head_dim,
                  long long ldq, long long ldk, long long ldv, const int32_t* cu_new, const int32_t* past, int batch, int max_new,
@@ -455,6 +510,8 @@ int fq_attn_cache(const void* Q, int x_dtype, int tokens, int heads_q, int heads
 int fq_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype, int tokens_q, int tokens_k, int heads_q, int heads_kv,
                    int head_dim, long long ldq, long long ldk, long long ldv, const int32_t* cu_q, const int32_t* cu_k, int batch, int max_q,
                    int causal, float scale, void* Y, long long ldy, void* stream);
+int fq_kv_copy_pages(int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale, int pages, int heads_kv, int page_size, int head_dim,
+                     const int32_t* from, const int32_t* to, int count, void* stream);
 
 #ifdef __cplusplus
 }

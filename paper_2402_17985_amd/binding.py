@@ -26,7 +26,8 @@ SYMBOLS = ["fq_last_error_string", "fq_version", "fq_flatten_plan", "fq_flatten_
            "fq_flatten_plan_xw", "fq_flatten_weights_split", "fq_flatten_quant_act_peel",
            "fq_gemm_i8_bias", "fq_gemm_i4_bias", "fq_linear_bias", "fq_linear_fused_a_i8", "fq_gemm_i4_e3m2",
            "fq_flatten_quant_act_noalloc", "fq_noalloc_scratch_bytes",
-           "fq_kv_append", "fq_attn_cache_workspace_bytes", "fq_attn_cache", "fq_attn_prompt",
+           "fq_kv_append", "fq_attn_cache_workspace_bytes", "fq_attn_cache", "fq_attn_prompt", "fq_kv_copy_pages",
+           "fq_rms_norm_quant", "fq_rms_norm_workspace_bytes", "fq_group_weights_i4", "fq_linear_group_i4",
            # include/fq_peak.h: measurement hooks
            "fq_peak_mfma", "fq_peak_copy", "fq_peak_gemm_ticks", "fq_peak_wall_clock_khz"]
 FQ_PEAK_I8, FQ_PEAK_BF16, FQ_PEAK_E3M2, FQ_PEAK_I8_NIBBLES = 0, 1, 2, 3
@@ -105,6 +106,13 @@ def lib() -> ctypes.CDLL:
                                 c_int, c_float, vp, c_ll, vp, c_size_t, vp]
     L.fq_attn_prompt.argtypes = [vp, vp, vp, c_int, c_int, c_int, c_int, c_int, c_int, c_ll, c_ll, c_ll, vp, vp, c_int, c_int, c_int, c_float, vp,
                                  c_ll, vp]
+    L.fq_kv_copy_pages.argtypes = [vp, vp, vp, vp, c_int, c_int, c_int, c_int, vp, vp, c_int, vp]
+    L.fq_rms_norm_workspace_bytes.restype = c_size_t
+    L.fq_rms_norm_workspace_bytes.argtypes = [c_int] * 3
+    L.fq_rms_norm_quant.argtypes = [vp, c_int, c_int, c_int, c_int, vp, c_int, c_int, vp, c_int, vp, c_int, c_float, vp, c_int, c_int, vp, vp,
+                                    c_int, c_int, vp, vp, vp, vp, c_size_t, vp]
+    L.fq_group_weights_i4.argtypes = [vp, c_int, c_int, c_int, c_int, c_int, vp, vp, vp, c_int, vp]
+    L.fq_linear_group_i4.argtypes = [vp, c_int, c_int, c_int, c_int, vp, vp, vp, c_int, c_int, c_int, vp, vp, c_int, c_int, vp]
     for name in SYMBOLS:
         getattr(L, name)
     _lib = L
@@ -596,5 +604,120 @@ def fq_attn_prompt(Q, K, V, cu_q, cu_k, max_q: int, scale: float, Y, causal: boo
     rc = (_lib or lib()).fq_attn_prompt(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _dtype_code(Q), tokens_q, tokens_k, heads_q, heads_kv, dim, ldq, ldk, ldv,
                                         _array(cu_q, "cu_q", here, torch.int32, (batch + 1,)), _array(cu_k, "cu_k", here, torch.int32, (batch + 1,)), batch, max_q,
                                         1 if causal else 0, scale, Y.data_ptr(), ldy, _stream_on(stream, here))
+    if rc:
+        _check(rc)
+
+
+def fq_kv_copy_pages(k_cache, v_cache, k_scale, v_scale, src, dst, stream=None) -> None:
+    """Page dst[i] of the paged 8-bit cache becomes a copy of page src[i], codes and scales of keys and values (int32 device tensors).  No page
+    named in dst may be named a second time; a number outside the pool copies nothing."""
+    torch, here = _torch(), _here()
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache is [pages, heads_kv, page_size, head_dim]")
+    pages, heads, size, dim = k_cache.shape
+    count = src.numel()
+    rc = (_lib or lib()).fq_kv_copy_pages(_array(k_cache, "k_cache", here, torch.int8, (pages, heads, size, dim)), _array(v_cache, "v_cache", here, torch.int8, (pages, heads, dim, size)),
+                                          _array(k_scale, "k_scale", here, torch.float32, (pages, heads)), _array(v_scale, "v_scale", here, torch.float32, (pages, heads)),
+                                          pages, heads, size, dim, _array(src, "src", here, torch.int32, (count,)), _array(dst, "dst", here, torch.int32, (count,)), count,
+                                          _stream_on(stream, here))
+    if rc:
+        _check(rc)
+
+
+# ------------------------------------------------------------------------------------------
+# around the products: norm with a quantized output, 4-bit weights with group scales
+# ------------------------------------------------------------------------------------------
+def _matrix(t, name, here, shape=None):
+    """(address, type code, row stride) of a matrix with dense rows on device `here`."""
+    if t.get_device() != here:
+        raise ValueError(f"{name} is on {t.device}: it must be on the current device, cuda:{here}")
+    got = t.shape
+    if len(got) != 2 or (shape is not None and got != shape):
+        raise ValueError(f"{name} must have the shape {tuple(shape) if shape else '[rows, columns]'}; it has {tuple(got)}")
+    rows, cols = got
+    ld, one = t.stride()
+    if cols > 1 and one != 1:
+        raise ValueError(f"{name} must have a contiguous last dimension")
+    if rows == 1:       # a single row's stride means nothing: the next multiple of 16 bytes
+        ld = -(-cols // 8) * 8
+    return t.data_ptr(), _dtype_code(t), ld
+
+
+def fq_rms_norm_workspace_bytes(M: int, K: int, Kpad: int) -> int:
+    return lib().fq_rms_norm_workspace_bytes(M, K, Kpad)
+
+
+def fq_rms_norm_quant(X, gamma, eps: float, R=None, R_out=None, Y=None, src_idx=None, rep=None, bits: int = 8, Xq_out=None, s_x_out=None,
+                      workspace=None, absmax_in=None, stream=None) -> None:
+    """Root-mean-square norm of the rows of X [M, K] (plus R, the sums going to R_out), times gamma [K]: rounded into Y, and flattened and
+    quantized into Xq_out with its scale in s_x_out (either may be None).  absmax_in: the static bound; None: dynamic, which needs a workspace
+    of fq_rms_norm_workspace_bytes(M, K, Kpad) bytes."""
+    torch, here = _torch(), _here()
+    x, x_type, ldx = _matrix(X, "X", here)
+    shape = X.shape
+    M, K = shape
+    r = r_out = y = xq = s_x = src = reps = ws = bound = None
+    r_type = y_type = FQ_F32
+    ldr = ldro = ldy = Kpad = ws_bytes = 0
+    if (R is None) != (R_out is None):
+        raise ValueError("R and R_out go together")
+    if R is not None:
+        r, r_type, ldr = _matrix(R, "R", here, shape)
+        r_out, out_type, ldro = _matrix(R_out, "R_out", here, shape)
+        if out_type != r_type:
+            raise ValueError("R_out must have R's type")
+    g = _array(gamma, "gamma", here, gamma.dtype, (K,))
+    if Y is not None:
+        y, y_type, ldy = _matrix(Y, "Y", here, shape)
+    if Xq_out is not None:
+        if src_idx is None or rep is None or s_x_out is None:
+            raise ValueError("Xq_out needs src_idx, rep and s_x_out")
+        Kpad = src_idx.numel()
+        src, reps = _array(src_idx, "src_idx", here, torch.int32, (Kpad,)), _array(rep, "rep", here, torch.int32, (Kpad,))
+        if Xq_out.get_device() != here or not Xq_out.is_contiguous() or Xq_out.element_size() != 1 or Xq_out.numel() != M * (Kpad if bits == 8 else Kpad // 2 if bits == 4 else 3 * Kpad // 4):
+            raise ValueError(f"Xq_out must be contiguous bytes for {M} rows of {Kpad} slots on the current device, cuda:{here}")
+        xq, s_x = Xq_out.data_ptr(), _array(s_x_out, "s_x_out", here, torch.float32, s_x_out.shape)
+        if absmax_in is not None:
+            bound = _array(absmax_in, "absmax_in", here, torch.float32, absmax_in.shape)
+    if workspace is not None:
+        if workspace.get_device() != here or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous and on the current device, cuda:{here}")
+        ws, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    rc = (_lib or lib()).fq_rms_norm_quant(x, x_type, M, K, ldx, r, r_type, ldr, r_out, ldro, g, _dtype_code(gamma), eps, y, y_type, ldy, src, reps, Kpad, bits,
+                                           bound, xq, s_x, ws, ws_bytes, _stream_on(stream, here))
+    if rc:
+        _check(rc)
+
+
+def _group_arrays(Wq, S, B, group, N, K, here):
+    """Addresses of codes, scales and offsets (or None), and the type of the latter two."""
+    torch = _torch()
+    if group <= 0 or K % 2:
+        raise ValueError(f"groups of {group} columns of {K}")
+    groups = (N, -(-K // group))
+    return (_array(Wq, "Wq", here, torch.uint8, (N, K // 2)), _array(S, "S", here, S.dtype, groups), None if B is None else _array(B, "B", here, S.dtype, groups),
+            _dtype_code(S))
+
+
+def fq_group_weights_i4(W, group: int, Wq_out, S_out, B_out=None, stream=None) -> None:
+    """W [N, K] to 4-bit codes Wq_out uint8 [N, K / 2] with scales S_out [N, ceil(K / group)] and, unless B_out is None, offsets of the same shape and type."""
+    here = _here()
+    w, w_type, ldw = _matrix(W, "W", here)
+    N, K = W.shape
+    rc = (_lib or lib()).fq_group_weights_i4(w, w_type, N, K, ldw, group, *_group_arrays(Wq_out, S_out, B_out, group, N, K, here), _stream_on(stream, here))
+    if rc:
+        _check(rc)
+
+
+def fq_linear_group_i4(X, Wq, S, group: int, Y, B=None, bias=None, stream=None) -> None:
+    """Y [M, N] = X [M, K] times the transpose of the weights that fq_group_weights_i4 made, plus bias (fp32 [N])."""
+    torch, here = _torch(), _here()
+    x, x_type, ldx = _matrix(X, "X", here)
+    M, K = X.shape
+    N = Wq.shape[0]
+    y, y_type, ldy = _matrix(Y, "Y", here, (M, N))
+    codes, scales, offsets, s_type = _group_arrays(Wq, S, B, group, N, K, here)
+    rc = (_lib or lib()).fq_linear_group_i4(x, x_type, M, K, ldx, codes, scales, offsets, s_type, group, N,
+                                            None if bias is None else _array(bias, "bias", here, torch.float32, (N,)), y, y_type, ldy, _stream_on(stream, here))
     if rc:
         _check(rc)

@@ -19,6 +19,8 @@ SOURCES = [("fq_gemm.hip", ["-DFQ_GEMM_MODE=1"], "fq_gemm_i4.o"),
            ("fq_kv_append.hip", [], "fq_kv_append.o"), ("fq_attn_cache.hip", ["-fno-honor-nans"], "fq_attn_cache.o"),
            ("fq_attn_cache_wide.hip", ["-fno-honor-nans"], "fq_attn_cache_wide.o"),
            ("fq_attn_prompt.hip", ["-fno-honor-nans"], "fq_attn_prompt.o"), ("fq_attn_api.hip", [], "fq_attn_api.o"),
+           ("fq_step_api.hip", [], "fq_step_api.o"), ("fq_norm.hip", [], "fq_norm.o"), ("fq_group.hip", [], "fq_group.o"),
+           ("fq_linear_group.hip", [], "fq_linear_group.o"), ("fq_kv_pages.hip", [], "fq_kv_pages.o"),
            ("fq_gemm_select.hip", [], "fq_gemm_select.o"), ("fq_peak.hip", [], "fq_peak.o")]
 # -packed-fp32-ops off: keeps the compiler from forming packed fp32 instructions
 # -ffp-contract=off: every fp32 multiply stays a single correctly rounded operation
@@ -45,6 +47,7 @@ def build(force: bool = True, verbose: bool = False) -> str:
     hdrs = [os.path.join(CSRC, "fq_internal.h"), os.path.join(CSRC, "fq_gemm_common.h"),
             os.path.join(CSRC, "fq_gemm_skinny.h"), os.path.join(CSRC, "fq_quant_common.h"), os.path.join(CSRC, "fq_rules.h"),
             os.path.join(CSRC, "fq_attn_rules.h"), os.path.join(CSRC, "fq_attn_common.h"), os.path.join(CSRC, "fq_attn_cache.h"),
+            os.path.join(CSRC, "fq_checks.h"), os.path.join(CSRC, "fq_rows.h"), os.path.join(CSRC, "fq_linear_group.h"),
             os.path.join(HERE, "..", "include", "fq.h"),
             os.path.join(HERE, "..", "include", "fq_peak.h")]
     srcs = [(os.path.join(CSRC, s), extra, obj) for s, extra, obj in SOURCES]

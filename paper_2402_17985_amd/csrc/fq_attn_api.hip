@@ -13,9 +13,7 @@ int check_heads(int heads_q, int heads_kv, int head_dim)
     if (heads_q <= 0 || heads_kv <= 0 || heads_q % heads_kv != 0)
         return fail(FQ_ERR_SHAPE, "%d query heads over %d key heads: must be positive, the first a multiple of the second", heads_q, heads_kv);
     if (heads_q > 16384) return fail(FQ_ERR_RANGE, "%d query heads: at most 16384", heads_q);
-    for (int d : ATTN_DIMS)
-        if (d == head_dim) return FQ_OK;
-    return fail(FQ_ERR_SHAPE, "head_dim = %d must be 64, 80, 96 or 128", head_dim);
+    return head_dim_ok(head_dim) ? FQ_OK : fail(FQ_ERR_SHAPE, "head_dim = %d must be 64, 80, 96 or 128", head_dim);
 }
 
 // A packed array [tokens, heads, head_dim] with dense heads and `ld` elements from one token to the next.

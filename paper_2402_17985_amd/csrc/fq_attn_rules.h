@@ -17,6 +17,12 @@ namespace fq {
 constexpr int CACHE_STEP = 64;        // keys that a wave of the cache's attention takes at a time; pages are a multiple of it
 constexpr int MAX_PAGE = 128;
 constexpr int ATTN_DIMS[] = {64, 80, 96, 128};
+inline bool head_dim_ok(int head_dim)
+{
+    for (int d : ATTN_DIMS)
+        if (d == head_dim) return true;
+    return false;
+}
 
 // Rows [first, first + count) of a packed array of `rows` rows, from two neighbouring offsets; at most `most` of them.
 struct Rows {
@@ -45,6 +51,10 @@ FQ_BOTH Fill page_fill(Rows r, int past, int j, int page, int capacity)
 }
 // Pages that `tokens` tokens can touch, wherever the first one lies in its page.
 inline long long pages_touched(int tokens, int page) { return ((long long)tokens + page - 2) / page + 1; }
+
+// A workgroup of a page copy takes this much of one page of keys or of values.
+constexpr int COPY_THREADS = 256, COPY_PIECE = 16384;
+inline long long copy_parts(size_t page_bytes) { return (long long)((page_bytes + COPY_PIECE - 1) / COPY_PIECE); }
 
 // The pages that an append's workgroups look at.  As many for each sequence as max_new tokens can touch; or, where that is twice what all tokens' rows
 // can need, place by place: sequence b's pages begin at place cu_new[b] / page + 2 b (n tokens touch n / page + 2 pages at most, rounded down).

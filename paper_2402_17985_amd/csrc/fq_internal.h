@@ -136,4 +136,15 @@ int launch_attn_prompt(const void* Q, const void* K, const void* V, int x_dtype,
                        int head_dim, long long ldq, long long ldk, long long ldv, const int32_t* cu_q, const int32_t* cu_k, int batch, int max_q,
                        int causal, float scale, void* Y, long long ldy, hipStream_t stream);
 
+// ---- around the products and the cache (arguments as in include/fq.h) ----
+size_t rms_norm_workspace(int M);
+int launch_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, const void* R, int r_dtype, int ldr, void* R_out, int ldro,
+                          const void* gamma, int g_dtype, float eps, void* Y, int y_dtype, int ldy, const int32_t* src, const int32_t* rep,
+                          int Kpad, int bits, const float* absmax_in, void* Xq_out, float* s_x_out, void* workspace, hipStream_t stream);
+int launch_group_weights(const void* W, int w_dtype, int N, int K, int ldw, int group, void* Wq, void* S, void* B, int s_dtype, hipStream_t stream);
+int launch_linear_group(const void* X, int x_dtype, int M, int K, int ldx, const void* Wq, const void* S, const void* B, int s_dtype, int group, int N,
+                        const float* bias, void* Y, int y_dtype, int ldy, hipStream_t stream);
+int launch_kv_copy_pages(int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale, int pages, int heads_kv, int page_size, int head_dim,
+                         const int32_t* from, const int32_t* to, int count, hipStream_t stream);
+
 }  // namespace fq

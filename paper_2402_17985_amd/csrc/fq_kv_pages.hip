@@ -1,0 +1,53 @@
+// fq_kv_copy_pages: pages of the paged 8-bit cache copied to other pages, keys, values and both scales.
+//
+// Bytes alone.  A workgroup copies a piece of one page of one of the two arrays, 16 bytes a lane and load, all of a thread's loads
+// ahead of its stores; page numbers come from the device and are checked there.
+#include "fq_attn_rules.h"
+#include "fq_internal.h"
+
+namespace fq {
+namespace {
+
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+constexpr int THREADS = COPY_THREADS, EACH = COPY_PIECE / (16 * COPY_THREADS);
+
+__global__ __launch_bounds__(THREADS) void copy_pages_kernel(int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale, int pages, int heads,
+                                                             size_t page_bytes, const int32_t* from, const int32_t* to, int parts)
+{
+    const unsigned pair = blockIdx.x / (2u * parts), part = blockIdx.x % (2u * parts);
+    const int src = from[pair], dst = to[pair];
+    if ((unsigned)src >= (unsigned)pages || (unsigned)dst >= (unsigned)pages || src == dst) return;
+    const bool values = part >= (unsigned)parts;
+    const unsigned piece = values ? part - parts : part;
+    int8_t* cache = values ? v_cache : k_cache;
+    float* scale = values ? v_scale : k_scale;
+    const v4u* in = reinterpret_cast<const v4u*>(cache + (size_t)src * page_bytes);
+    v4u* out = reinterpret_cast<v4u*>(cache + (size_t)dst * page_bytes);
+    const size_t count = page_bytes / 16, first = (size_t)piece * (COPY_PIECE / 16) + threadIdx.x;
+    v4u v[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (first + i * THREADS < count) v[i] = in[first + i * THREADS];
+    if (piece == 0)
+        for (int h = threadIdx.x; h < heads; h += THREADS) scale[(size_t)dst * heads + h] = scale[(size_t)src * heads + h];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (first + i * THREADS < count) out[first + i * THREADS] = v[i];
+}
+
+}  // namespace
+
+int launch_kv_copy_pages(int8_t* k_cache, int8_t* v_cache, float* k_scale, float* v_scale, int pages, int heads_kv, int page_size, int head_dim,
+                         const int32_t* from, const int32_t* to, int count, hipStream_t stream)
+{
+    const size_t page_bytes = (size_t)heads_kv * page_size * head_dim;
+    const long long parts = copy_parts(page_bytes);
+    copy_pages_kernel<<<(unsigned)(2 * parts * count), THREADS, 0, stream>>>(k_cache, v_cache, k_scale, v_scale, pages, heads_kv, page_bytes, from, to,
+                                                                            (int)parts);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(FQ_ERR_HIP, "page copy launch failed: %s", hipGetErrorString(e));
+    return FQ_OK;
+}
+
+}  // namespace fq

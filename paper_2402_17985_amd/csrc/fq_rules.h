@@ -229,4 +229,7 @@ inline AbsmaxGrid absmax_grid(long long M, long long K, long long ld, int vec, l
     return AbsmaxGrid{(int)bx, (int)((M + rows - 1) / rows), (int)rows};
 }
 
+// Products with group-scaled 4-bit weights: a workgroup of 512 threads for at least 16 columns and 16 rows.
+inline bool group_holds(long long M, long long N) { return launch_holds(((M + 15) / 16) * ((N + 15) / 16), 512); }
+
 }  // namespace fq
