@@ -20,7 +20,8 @@ SOURCES = [("fq_gemm.hip", ["-DFQ_GEMM_MODE=1"], "fq_gemm_i4.o"),
            ("fq_attn_cache_wide.hip", ["-fno-honor-nans"], "fq_attn_cache_wide.o"),
            ("fq_attn_prompt.hip", ["-fno-honor-nans"], "fq_attn_prompt.o"), ("fq_attn_api.hip", [], "fq_attn_api.o"),
            ("fq_step_api.hip", [], "fq_step_api.o"), ("fq_norm.hip", [], "fq_norm.o"), ("fq_group.hip", [], "fq_group.o"),
-           ("fq_linear_group.hip", [], "fq_linear_group.o"), ("fq_kv_pages.hip", [], "fq_kv_pages.o"),
+           ("fq_linear_group.hip", [], "fq_linear_group.o"), ("fq_linear_group_tile.hip", ["-DFQ_GROUP_TYPE=1"], "fq_linear_group_tile_f16.o"),
+           ("fq_linear_group_tile.hip", ["-DFQ_GROUP_TYPE=2"], "fq_linear_group_tile_bf16.o"), ("fq_kv_pages.hip", [], "fq_kv_pages.o"),
            ("fq_gemm_select.hip", [], "fq_gemm_select.o"), ("fq_peak.hip", [], "fq_peak.o")]
 # -packed-fp32-ops off: keeps the compiler from forming packed fp32 instructions
 # -ffp-contract=off: every fp32 multiply stays a single correctly rounded operation
