@@ -30,7 +30,7 @@ struct GroupProduct {
     const float* bias;
     void* Y;
     size_t ldx, ldy;
-    int M, N, K, groups, s_dtype, y_dtype, tiles_n, tiles;
+    int M, N, K, groups, s_dtype, y_dtype, tiles_n, tiles, group_shift;
 
     // The scales (or offsets) of a step's PER groups as they are stored, 16-bit ones two to a word; those of groups behind the row's last are its last one.
     template <int PER> __device__ __forceinline__ StepScales<PER> step_scales(const void* base, size_t row, int group) const
@@ -96,17 +96,6 @@ struct GroupProduct {
 template <int XT> int launch_group_tile(const GroupProduct& a, int group, hipStream_t stream);
 
 namespace {
-
-// Workgroup -> tile.  Ids are dealt round-robin to the 8 XCDs; each gets a contiguous band of tiles, which runs through 8 rows of tiles at a time, so that
-// the tiles under way at once share rows and columns in its L2.
-__device__ __forceinline__ void group_tile(int wg, int tiles_m, int tiles_n, int& tile_m, int& tile_n)
-{
-    const int tiles = tiles_m * tiles_n, q = tiles >> 3, rem = tiles & 7, xcd = wg & 7, idx = wg >> 3;
-    const int at = xcd < rem ? xcd * (q + 1) + idx : rem * (q + 1) + (xcd - rem) * q + idx;
-    const int band = at / (8 * tiles_n), first = band * 8, high = min(tiles_m - first, 8), in_band = at - band * 8 * tiles_n;
-    tile_m = first + in_band % high;
-    tile_n = in_band / high;
-}
 
 // Eight codes (a word of nibbles, two's complement) as eight 16-bit numbers in the columns' order: a byte's two nibbles into the halves of a register.
 // u = q + 8 is q with its highest bit turned.
