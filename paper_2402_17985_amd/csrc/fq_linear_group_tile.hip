@@ -1,8 +1,8 @@
 // fq_linear_group_i4 for more rows than the kernel of single tokens takes: tiles of X shared by the waves of a workgroup through LDS.
 //
 // A wave multiplies 16 MT rows by 16 NT columns; WN waves lie side by side and WK waves take turns along the reduction, a step of 128 columns each, so that few
-// columns of output still give every CU work.  X is copied straight into one of two buffers in LDS while the other is multiplied; weights go from
-// memory into the registers of the one wave that needs them, a step ahead, and are widened there, once for all its rows.
+// columns of output still give every CU work.  Everything is copied straight into a ring of S stages in LDS, S - 1 of them on their way: X for all waves, codes
+// and scales for the one wave that needs them, which widens codes in registers once for all its rows.
 // Codes stay whole numbers up to the end of a group, whose sum takes the scale in fp32: nothing is rounded to 16 bits on the way.
 #include <algorithm>
 #include <atomic>
@@ -13,16 +13,37 @@
 namespace fq {
 namespace {
 
+// s_waitcnt immediate: at most `vm` copies on their way, and no LDS operation
+constexpr int wait_imm(int vm) { return (vm & 0xf) | ((vm >> 4) << 14) | 0x0070; }
+
+// Copies of 2 or 4 bytes a lane into 4 bytes of LDS each, as dma16
+__device__ __forceinline__ void dma2(const uint8_t* uniform_base, uint32_t lane_offset, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %1, %0" : : "s"(uniform_base), "v"(lane_offset), "s"(lds_base) : "memory");
+}
+__device__ __forceinline__ void dma4(const uint8_t* uniform_base, uint32_t lane_offset, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %1, %0" : : "s"(uniform_base), "v"(lane_offset), "s"(lds_base) : "memory");
+}
+
+// Bytes of LDS: a wave's codes and scales of a stage; a stage; the whole
+constexpr int own_bytes(int NT, int PER, bool offset) { return NT * 1024 + (NT * PER / 4) * 256 * (offset ? 2 : 1); }
+constexpr int stage_bytes(int MT, int NT, int WN, int WK, int PER, bool offset) { return 16 * MT * 256 * WK + WN * WK * own_bytes(NT, PER, offset); }
+constexpr int sums_bytes(int MT, int NT, int WN, int WK) { return WK * 16 * MT * (16 * NT * WN + 4) * 4; }
+
 // GROUP = 32 serves groups of any size: every product of 32 columns takes its scale.
-template <int XT, int MT, int NT, int WN, int WK, int GROUP, bool OFFSET>
+template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP, bool OFFSET>
 __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupProduct a)
 {
     typedef GroupMma<XT> M_;
     typedef typename M_::v8 v8;
     constexpr int THREADS = 64 * WN * WK, PER = 128 / GROUP, EACH = 4 / PER;
     constexpr bool TURN = GROUP != 128;                          // product j takes columns 32 j .. 32 j + 31, of one group
-    constexpr int ROWS = 16 * MT, PITCH = 256 * WK, BUFFER = ROWS * PITCH, COPIES = BUFFER / 1024 / (WN * WK);
-    static_assert(BUFFER % (1024 * WN * WK) == 0, "whole copies a wave");
+    constexpr int ROWS = 16 * MT, PITCH = 256 * WK, X_BYTES = ROWS * PITCH, COPIES = X_BYTES / 1024 / (WN * WK);
+    constexpr int SCALES = NT * PER / 4, OWN = own_bytes(NT, PER, OFFSET), STAGE = stage_bytes(MT, NT, WN, WK, PER, OFFSET);
+    constexpr int IN_STAGE = COPIES + NT + SCALES * (OFFSET ? 2 : 1);      // copies of a wave
+    static_assert(X_BYTES % (1024 * WN * WK) == 0 && NT * PER % 4 == 0, "whole copies a wave");
+    static_assert((S - 2) * IN_STAGE < 64, "copies are counted in six bits");
     extern __shared__ __align__(16) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, c = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave % WN, wk = wave / WN;
@@ -30,8 +51,9 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
     tile_of_workgroup(blockIdx.x, a.tiles, a.tiles / a.tiles_n, a.tiles_n, tile_m, tile_n);
     const int m0 = tile_m * ROWS, n0 = (tile_n * WN + wn) * 16 * NT;
     const int steps = (a.K + 127) / 128, stages = (steps + WK - 1) / WK;
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)FQ_LDS_PTR(lds));
 
-    // ---- copies of X: 1 KiB each; piece p of row m of a buffer lies at place p ^ (m % 16), for the banks ----
+    // ---- X: copies of 1 KiB; piece p of row m of a stage lies at place p ^ (m % 16), for the banks ----
     const uint8_t* x_tile = static_cast<const uint8_t*>(a.X) + (size_t)m0 * a.ldx * 2;
     uint32_t x_from[COPIES];
 #pragma unroll
@@ -39,42 +61,47 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
         const int at = (wave * COPIES + i) * 64 + lane, row = at / (16 * WK);
         x_from[i] = (uint32_t)min(row, a.M - 1 - m0) * (uint32_t)(a.ldx * 2) + 16 * (at % (16 * WK) ^ (row & 15));
     }
-    const uint32_t x_lds = __builtin_amdgcn_readfirstlane((uint32_t)(size_t)FQ_LDS_PTR(lds)) + wave * COPIES * 1024;
-    auto copy = [&](int stage) {
+    // ---- codes: lane l copies a piece of column l / 4, pieces turned by column / 4; scales: 64 (column, group of the step) to a copy ----
+    const int n_first = min(n0, a.N - 1), n_last = a.N - 1 - n_first;
+    const uint8_t* w_tile = a.Wq + (size_t)n_first * (a.K / 2);
+    uint32_t w_from[NT], g_from[SCALES];
+    const int piece = (lane & 3) ^ (lane >> 4);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w_from[j] = (uint32_t)min(16 * j + lane / 4, n_last) * (a.K / 2);
+#pragma unroll
+    for (int j = 0; j < SCALES; ++j) g_from[j] = (uint32_t)min((64 * j + lane) / PER, n_last) * a.groups;
+    const int g_size = a.s_dtype == FQ_F32 ? 4 : 2;
+    const uint8_t* s_tile = static_cast<const uint8_t*>(a.S) + (size_t)n_first * a.groups * g_size;
+    const uint8_t* b_tile = static_cast<const uint8_t*>(a.B) + (size_t)n_first * a.groups * g_size;
+    auto copy = [&](int stage, int buffer) {
+        const uint32_t to = lds0 + buffer * STAGE, mine = to + X_BYTES + wave * OWN;
+        const int k = stage * WK + wk;
+        const uint32_t w_at = min(64 * k + 16 * piece, a.K / 2 - 16);      // what lies behind a row's end is read from its end
+#pragma unroll
+        for (int j = 0; j < NT; ++j) dma16(w_tile, w_from[j] + w_at, mine + j * 1024);
+        const uint32_t group = min(GROUP == 32 ? (128 * k + 32 * (lane % 4)) >> a.group_shift : k * PER + lane % PER, a.groups - 1);
+#pragma unroll
+        for (int j = 0; j < SCALES; ++j) {
+            const uint32_t at = mine + NT * 1024 + j * 256;
+            if (g_size == 4) {
+                dma4(s_tile, (g_from[j] + group) * 4, at);
+                if (OFFSET) dma4(b_tile, (g_from[j] + group) * 4, at + SCALES * 256);
+            } else {
+                dma2(s_tile, (g_from[j] + group) * 2, at);
+                if (OFFSET) dma2(b_tile, (g_from[j] + group) * 2, at + SCALES * 256);
+            }
+        }
         const uint8_t* from = x_tile + (size_t)stage * PITCH;
-        const uint32_t to = x_lds + (stage & 1) * BUFFER;
         if ((stage + 1) * WK * 128 <= a.K) {
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) dma16(from, x_from[i], to + i * 1024);
+            for (int i = 0; i < COPIES; ++i) dma16(from, x_from[i], to + (wave * COPIES + i) * 1024);
         } else {                                                 // zeros behind a row's end; the codes there do not matter then
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) {
-                const int at = (wave * COPIES + i) * 64 + lane, piece = at % (16 * WK) ^ (at / (16 * WK) & 15);
-                dma16_addr(stage * WK * 128 + 8 * piece < a.K ? from + x_from[i] : reinterpret_cast<const uint8_t*>(g_zero_chunk), to + i * 1024);
+                const int at = (wave * COPIES + i) * 64 + lane, x_piece = at % (16 * WK) ^ (at / (16 * WK) & 15);
+                dma16_addr(stage * WK * 128 + 8 * x_piece < a.K ? from + x_from[i] : reinterpret_cast<const uint8_t*>(g_zero_chunk),
+                           to + (wave * COPIES + i) * 1024);
             }
-        }
-    };
-    // ---- codes and scales of the wave's columns: lane l has piece l % 4 of the step of column l / 4, and scale l % 4 ----
-    const uint8_t* w_tile = a.Wq + (size_t)min(n0, a.N - 1) * (a.K / 2);
-    uint32_t w_row[NT], g_row[NT];
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int n = max(min(16 * j + lane / 4, a.N - 1 - n0), 0);
-        w_row[j] = (uint32_t)n * (a.K / 2);
-        g_row[j] = (uint32_t)n * a.groups;
-    }
-    const size_t g_tile = (size_t)min(n0, a.N - 1) * a.groups;
-    v4u w_next[NT];
-    uint32_t s_next[NT], b_next[NT];
-    auto load = [&](int stage) {
-        const int k = stage * WK + wk;
-        const uint32_t w_at = min(64 * k + 16 * (lane % 4), a.K / 2 - 16);
-        const uint32_t group = min(GROUP == 32 ? (128 * k + 32 * (lane % 4)) >> a.group_shift : k * PER + lane % 4, a.groups - 1);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            w_next[j] = *reinterpret_cast<const v4u*>(w_tile + (w_row[j] + w_at));
-            s_next[j] = a.one_scale(a.S, g_tile + (g_row[j] + group));
-            if (OFFSET) b_next[j] = a.one_scale(a.B, g_tile + (g_row[j] + group));
         }
     };
 
@@ -83,32 +110,34 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-    load(0);
-    copy(0);
-    for (int stage = 0; stage < stages; ++stage) {
-        // this stage's copies have landed, and the other buffer is read no more
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i)
+        if (i < stages) copy(i, i);
+    for (int stage = 0, buffer = 0; stage < stages; ++stage) {
+        // this stage's copies have landed, and the stage before it is read no more: its place is free
+        if (stage + S - 1 <= stages) __builtin_amdgcn_s_waitcnt(wait_imm((S - 2) * IN_STAGE));
+        else __builtin_amdgcn_s_waitcnt(wait_imm(0));
+        asm volatile("s_barrier" ::: "memory");
+        if (stage + S - 1 < stages) copy(stage + S - 1, buffer == 0 ? S - 1 : buffer - 1);
+        const uint8_t* here = lds + buffer * STAGE;
+        const uint8_t* own = here + X_BYTES + wave * OWN;
+        buffer = buffer + 1 == S ? 0 : buffer + 1;
         v8 wf[NT][4];
         float s[NT][PER], b[NT][PER];
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            v4u codes;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) codes[q] = __shfl(w_next[j][q], 4 * r + c, 64);
+            v4u codes = *reinterpret_cast<const v4u*>(own + j * 1024 + 64 * r + 16 * (c ^ (r >> 2)));
             if (TURN) transpose_quarters(codes);
 #pragma unroll
             for (int q = 0; q < 4; ++q) wf[j][q] = M_::widen(codes[q]);
+            const uint32_t* scales = reinterpret_cast<const uint32_t*>(own + NT * 1024) + (16 * j + r) * PER;
 #pragma unroll
             for (int g = 0; g < PER; ++g) {
-                s[j][g] = a.value(__shfl(s_next[j], 4 * r + g, 64));
-                b[j][g] = OFFSET ? a.value(__shfl(b_next[j], 4 * r + g, 64)) : 0.0f;
+                s[j][g] = a.value(scales[g]);
+                b[j][g] = OFFSET ? a.value(scales[SCALES * 64 + g]) : 0.0f;
             }
         }
-        if (stage + 1 < stages) {
-            load(stage + 1);
-            copy(stage + 1);
-        }
-        const uint8_t* x_at = lds + (stage & 1) * BUFFER + r * PITCH;
+        const uint8_t* x_at = here + r * PITCH;
         auto operands = [&](int i, v8 (&xf)[4]) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) xf[q] = *reinterpret_cast<const v8*>(x_at + 16 * i * PITCH + 16 * ((16 * wk + (TURN ? 4 * q + c : 4 * c + q)) ^ r));
@@ -164,17 +193,13 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
     }
 }
 
-template <int XT, int MT, int NT, int WN, int WK, bool ANY> int launch(GroupProduct a, int group, hipStream_t stream)
+template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP, bool OFFSET> int launch_one(GroupProduct a, hipStream_t stream)
 {
-    void (*kern)(GroupProduct);
-    if constexpr (ANY) kern = a.B ? linear_group_tile_kernel<XT, MT, NT, WN, WK, 32, true> : linear_group_tile_kernel<XT, MT, NT, WN, WK, 32, false>;
-    else
-        kern = a.B ? (group == 32 ? linear_group_tile_kernel<XT, MT, NT, WN, WK, 32, true> : group == 64 ? linear_group_tile_kernel<XT, MT, NT, WN, WK, 64, true> : linear_group_tile_kernel<XT, MT, NT, WN, WK, 128, true>)
-                   : (group == 32 ? linear_group_tile_kernel<XT, MT, NT, WN, WK, 32, false> : group == 64 ? linear_group_tile_kernel<XT, MT, NT, WN, WK, 64, false> : linear_group_tile_kernel<XT, MT, NT, WN, WK, 128, false>);
-    constexpr int SMEM = std::max(2 * 16 * MT * 256 * WK, WK * 16 * MT * (16 * NT * WN + 4) * 4);
-    static std::atomic<unsigned long long> attr_set[6];
-    if (int rc = set_lds_limit(reinterpret_cast<const void*>(kern), SMEM, attr_set[(group == 32 ? 0 : group == 64 ? 1 : 2) + (a.B ? 3 : 0)])) return rc;
-    a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
+    constexpr int SMEM = std::max(S * stage_bytes(MT, NT, WN, WK, 128 / GROUP, OFFSET), sums_bytes(MT, NT, WN, WK));
+    static_assert(SMEM <= 160 * 1024, "LDS of a CU");
+    auto kern = linear_group_tile_kernel<XT, MT, NT, WN, WK, S, GROUP, OFFSET>;
+    static std::atomic<unsigned long long> attr_set;
+    if (int rc = set_lds_limit(reinterpret_cast<const void*>(kern), SMEM, attr_set)) return rc;
     a.tiles_n = (a.N + 16 * NT * WN - 1) / (16 * NT * WN);
     a.tiles = a.tiles_n * ((a.M + 16 * MT - 1) / (16 * MT));
     kern<<<(unsigned)a.tiles, 64 * WN * WK, SMEM, stream>>>(a);
@@ -182,18 +207,29 @@ template <int XT, int MT, int NT, int WN, int WK, bool ANY> int launch(GroupProd
     if (e != hipSuccess) return fail(FQ_ERR_HIP, "group-scaled layer launch failed: %s", hipGetErrorString(e));
     return FQ_OK;
 }
+template <int XT, int MT, int NT, int WN, int WK, int S, bool ANY> int launch(const GroupProduct& a, int group, hipStream_t stream)
+{
+    if constexpr (!ANY) {
+        if (group == 64) return a.B ? launch_one<XT, MT, NT, WN, WK, S, 64, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 64, false>(a, stream);
+        if (group == 128) return a.B ? launch_one<XT, MT, NT, WN, WK, S, 128, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 128, false>(a, stream);
+    }
+    return a.B ? launch_one<XT, MT, NT, WN, WK, S, 32, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 32, false>(a, stream);
+}
 
 }  // namespace
 
-template <int XT> int launch_group_tile(const GroupProduct& a, int group, hipStream_t stream)
+template <int XT> int launch_group_tile(const GroupProduct& product, int group, hipStream_t stream)
 {
+    GroupProduct a = product;
+    a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
     const long long cus = compute_units(), rows64 = (a.M + 63) / 64;
-    if (rows64 * ((a.N + 255) / 256) >= cus) return launch<XT, 4, 4, 4, 1, false>(a, group, stream);
+    if (rows64 * ((a.N + 255) / 256) >= cus) return launch<XT, 4, 4, 4, 1, 2, false>(a, group, stream);
     const bool wide = rows64 * ((a.N + 31) / 32) >= cus;
-    if (a.M <= 16) return wide ? launch<XT, 1, 2, 1, 8, true>(a, group, stream) : launch<XT, 1, 1, 1, 8, true>(a, group, stream);
-    if (a.M <= 32) return wide ? launch<XT, 2, 2, 1, 4, true>(a, group, stream) : launch<XT, 2, 1, 1, 4, true>(a, group, stream);
-    if (a.M <= 48) return wide ? launch<XT, 3, 2, 1, 4, true>(a, group, stream) : launch<XT, 3, 1, 1, 4, true>(a, group, stream);
-    return wide ? launch<XT, 4, 2, 1, 4, true>(a, group, stream) : launch<XT, 4, 1, 1, 4, true>(a, group, stream);
+    if (a.M <= 16) return wide ? launch<XT, 1, 2, 1, 4, 3, true>(a, group, stream) : launch<XT, 1, 1, 1, 4, 3, true>(a, group, stream);
+    if (a.M <= 32) return wide ? launch<XT, 2, 2, 1, 4, 3, true>(a, group, stream) : launch<XT, 2, 1, 1, 4, 3, true>(a, group, stream);
+    if (a.M <= 48) return wide ? launch<XT, 3, 2, 1, 4, 2, true>(a, group, stream) : launch<XT, 3, 1, 1, 4, 2, true>(a, group, stream);
+    if (rows64 * ((a.N + 63) / 64) >= cus) return launch<XT, 4, 2, 2, 2, 2, true>(a, group, stream);
+    return wide ? launch<XT, 4, 2, 1, 4, 2, true>(a, group, stream) : launch<XT, 4, 1, 1, 4, 2, true>(a, group, stream);
 }
 #if FQ_GROUP_TYPE == 1
 template int launch_group_tile<FQ_F16>(const GroupProduct&, int, hipStream_t);
