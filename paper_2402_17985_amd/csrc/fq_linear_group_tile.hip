@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
                         if (OFFSET) acc[i][j][e] = __builtin_fmaf(b[j][g], sum[e], acc[i][j][e]);
                     }
             }
-            __builtin_amdgcn_sched_barrier(0);       // operands of two blocks of rows are enough in registers
+            if (MT * NT > 8) __builtin_amdgcn_sched_barrier(0);      // large tiles: operands of two blocks of rows are enough in registers
         }
     }
     __syncthreads();
@@ -207,29 +207,33 @@ template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP, bool OFFSET>
     if (e != hipSuccess) return fail(FQ_ERR_HIP, "group-scaled layer launch failed: %s", hipGetErrorString(e));
     return FQ_OK;
 }
-template <int XT, int MT, int NT, int WN, int WK, int S, bool ANY> int launch(const GroupProduct& a, int group, hipStream_t stream)
+template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP = 32> int launch(const GroupProduct& a, hipStream_t stream)
 {
-    if constexpr (!ANY) {
-        if (group == 64) return a.B ? launch_one<XT, MT, NT, WN, WK, S, 64, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 64, false>(a, stream);
-        if (group == 128) return a.B ? launch_one<XT, MT, NT, WN, WK, S, 128, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 128, false>(a, stream);
-    }
-    return a.B ? launch_one<XT, MT, NT, WN, WK, S, 32, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, 32, false>(a, stream);
+    return a.B ? launch_one<XT, MT, NT, WN, WK, S, GROUP, true>(a, stream) : launch_one<XT, MT, NT, WN, WK, S, GROUP, false>(a, stream);
 }
 
 }  // namespace
 
+// Tiles by how many there are.  us (bf16, groups of 128), the taken one first:
+//   64 x 256   2048 rows, 11008 x 4096: 229; 64 x 128, waves two by two along both: 331; 64 x 128, waves side by side 351
+//   64 x 128   512 rows, 4096 x 4096: 33; 64 x 256 56; 64 x 32 49.  256 rows, 11008 x 4096, has 172 tiles of 64 x 256: 57, 64 x 128 62
+//   64 x 32    128 rows, 4096 x 4096: 17; 64 x 64 24; 64 x 256 56
+//   48 rows, 4096 x 11008: 30 (16 columns 31, 64 columns 53); 24 rows, 4096 x 11008: 18 (32 columns 25), 11008 x 4096: 21 (16 columns 22)
+//   16 rows, 4096 x 11008: 13 (32 columns 19), 22016 x 8192: 46 (16 columns 54)
+// With groups of 32 columns there is a scale to apply after every matrix product, and tiles of 256 columns lose (2048 rows, 11008 x 4096: 345; 256 columns 512).
 template <int XT> int launch_group_tile(const GroupProduct& product, int group, hipStream_t stream)
 {
     GroupProduct a = product;
     a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
-    const long long cus = compute_units(), rows64 = (a.M + 63) / 64;
-    if (rows64 * ((a.N + 255) / 256) >= cus) return launch<XT, 4, 4, 4, 1, 2, false>(a, group, stream);
-    const bool wide = rows64 * ((a.N + 31) / 32) >= cus;
-    if (a.M <= 16) return wide ? launch<XT, 1, 2, 1, 4, 3, true>(a, group, stream) : launch<XT, 1, 1, 1, 4, 3, true>(a, group, stream);
-    if (a.M <= 32) return wide ? launch<XT, 2, 2, 1, 4, 3, true>(a, group, stream) : launch<XT, 2, 1, 1, 4, 3, true>(a, group, stream);
-    if (a.M <= 48) return wide ? launch<XT, 3, 2, 1, 4, 2, true>(a, group, stream) : launch<XT, 3, 1, 1, 4, 2, true>(a, group, stream);
-    if (rows64 * ((a.N + 63) / 64) >= cus) return launch<XT, 4, 2, 2, 2, 2, true>(a, group, stream);
-    return wide ? launch<XT, 4, 2, 1, 4, 2, true>(a, group, stream) : launch<XT, 4, 1, 1, 4, 2, true>(a, group, stream);
+    const long long cus = compute_units(), rows = (a.M + 63) / 64;
+    if (a.M <= 16) return a.N >= 8192 ? launch<XT, 1, 2, 1, 8, 2>(a, stream) : launch<XT, 1, 1, 1, 8, 3>(a, stream);
+    if (a.M <= 32) return a.N >= 8192 ? launch<XT, 2, 1, 2, 4, 3>(a, stream) : launch<XT, 2, 1, 1, 8, 2>(a, stream);
+    if (a.M <= 48) return launch<XT, 3, 1, 2, 4, 2>(a, stream);
+    const bool many = 3 * rows * ((a.N + 255) / 256) >= 2 * cus, some = 4 * rows * ((a.N + 127) / 128) >= 3 * cus;
+    if (!some) return launch<XT, 4, 1, 2, 4, 2>(a, stream);
+    if (group == 32) return launch<XT, 4, 2, 4, 1, 2>(a, stream);
+    if (group == 64) return many ? launch<XT, 4, 4, 4, 1, 2, 64>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 64>(a, stream);
+    return many ? launch<XT, 4, 4, 4, 1, 2, 128>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 128>(a, stream);
 }
 #if FQ_GROUP_TYPE == 1
 template int launch_group_tile<FQ_F16>(const GroupProduct&, int, hipStream_t);
