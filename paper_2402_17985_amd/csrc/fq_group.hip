@@ -32,7 +32,13 @@ __global__ __launch_bounds__(THREADS) void group_weights_kernel(const void* __re
     const unsigned at = blockIdx.x * THREADS + threadIdx.x, row = min(at, total - 1) / units, unit = min(at, total - 1) % units;
     const bool mine = at < total && 16 * (int)unit < K;      // K is a multiple of 32: all 16 columns or none
     float w[16];
-    widen<DT>(mine ? load_raw<DT>(W, row * ldw, unit, K) : Raw<DT>{}, w);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float part[8];
+        widen<DT>(mine ? load_raw<DT, false>(row_of(W, ldw, element_bytes<DT>(), row), 2 * unit + h, K) : Raw<DT>{}, part);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[8 * h + i] = part[i];
+    }
     float lo = __builtin_inff(), hi = -__builtin_inff();
     if (mine) {
 #pragma unroll

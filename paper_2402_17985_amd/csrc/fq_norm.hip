@@ -4,9 +4,10 @@
 // A workgroup takes a row at a time, a thread 16 consecutive channels of it, which stay in registers from the load to the
 // codes; sums of squares are formed in float64, so that codes do not go by the order of a sum.  Workgroups stay for many
 // rows: gamma, the map and its multipliers are read once, and the next row is on its way while this one is reduced.
-// Slots that do not lie at their channel's own place (copies, other maps) read y out of LDS.
+// Slots that do not lie at their channel's own place (copies, padding, other maps) are worked on one by one, neighbouring threads neighbouring slots, from
+// the row in LDS; their codes meet there by sixteens.
 // A dynamic scale is a maximum over the whole tensor: a first pass stores h, every row's t and each workgroup's candidate, a
-// second one forms y again and quantizes it.
+// second one forms y again and quantizes it.  For a few rows one workgroup does both.
 #include <algorithm>
 #include <atomic>
 
@@ -16,9 +17,14 @@
 namespace fq {
 namespace {
 
-enum { ONE_PASS, FIND_SCALE, WITH_SCALE };
+enum { ONE_PASS, FIND_SCALE, WITH_SCALE, BOTH };
 constexpr int TABLE = 256;        // multipliers m(n) kept for n < 256
-constexpr int MAX_WGS = 1024;     // and candidates
+constexpr int MAX_WGS = 4096;     // and candidates
+constexpr int FEW_ROWS = 4;       // that one workgroup takes alone
+constexpr int KEPT = 4;           // slots away from their channel's place that a thread keeps in registers
+
+// floats of LDS for a row of K, and the zero behind it
+__host__ __device__ constexpr int row_places(int K) { return (K + 7) / 8 * 8 + 8; }
 
 struct Norm {
     const void *X, *R, *gamma;
@@ -31,17 +37,6 @@ struct Norm {
     uint8_t* out;
     float *s_x, *t, *found;
 };
-
-// Where channel j of the row lies in LDS: the four 16-byte pieces of a thread's channels are turned by its number, so that the threads of
-// a wave write to all banks.
-__device__ __forceinline__ int place(int j) { return (j & ~15) | ((((j >> 2) ^ (j >> 6)) & 3) << 2) | (j & 3); }
-
-__device__ __forceinline__ void store_codes(int bits, const float (&x)[16], const float (&m)[16], uint8_t* out, int Kpad, size_t M, int row, int q)
-{
-    if (bits == 8) store_group<8>(quantize16<8>(x, m), out, Kpad, M, row, q);
-    else if (bits == 4) store_group<4>(quantize16<4>(x, m), out, Kpad / 2, M, row, q);
-    else store_group<6>(quantize16<6>(x, m), out, 0, M, row, q);
-}
 
 // The sum over the workgroup of a value of each thread; `part`: a place for every wave.  The barrier also ends what the workgroup did in LDS before.
 __device__ __forceinline__ double sum_of(double v, double* part)
@@ -56,17 +51,81 @@ __device__ __forceinline__ double sum_of(double v, double* part)
     return s;
 }
 
-// GPT: groups of 16 channels a thread has (channels 16 (tid + k threads) ..)
-template <int XT, int RT, int PASS, int GPT>
+__device__ __forceinline__ float largest_of(float v, float* part)
+{
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = part[0];
+    for (int w = 1; w < (int)blockDim.x >> 6; ++w) v = fmaxf(v, part[w]);
+    return v;
+}
+
+// 1 / sqrt(v) in float64: the hardware's estimate and two steps of Newton's iteration.  Its few last bits off do not reach fp32 but next to a tie.
+__device__ __forceinline__ double inverse_root(double v)
+{
+    double y = __builtin_amdgcn_rsq(v);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) y = __builtin_fma(0.5 * y, __builtin_fma(-v * y, y, 1.0), y);
+    return y;
+}
+
+__device__ __forceinline__ float share(float v, int n) { return n == 1 ? fabsf(v) : (float)((double)fabsf(v) / (double)n); }
+
+// The largest fl32(|v| / n) seen: quotients are compared by cross multiplication in float64 (exact for n < 2^29) and divided once; rounding is monotonic.
+struct Largest {
+    float value = 0.0f, other = 0.0f;
+    int n = 1;
+    __device__ __forceinline__ void see(float v, int copies)
+    {
+        v = fabsf(v);
+        if (copies >= (1 << 29)) {
+            other = fmaxf(other, share(v, copies));
+        } else if ((double)v * (double)n > (double)value * (double)copies) {
+            value = v;
+            n = copies;
+        }
+    }
+    __device__ __forceinline__ float get() const { return fmaxf(other, share(value, n)); }
+};
+
+// 16 codes, one per byte
+__device__ __forceinline__ void store_packed(int bits, const v4u& q, uint8_t* out, int Kpad, size_t M, int row, int g)
+{
+    if (bits == 8) store_group<8>(q, out, Kpad, M, row, g);
+    else if (bits == 4) store_group<4>(q, out, Kpad / 2, M, row, g);
+    else store_group<6>(v4u{e3m2_codes(q[0]), e3m2_codes(q[1]), e3m2_codes(q[2]), e3m2_codes(q[3])}, out, 0, M, row, g);
+}
+// 8 elements to INT8 or nibbles at slot 8 g of a row
+__device__ __forceinline__ void store_eight(int bits, const float (&y)[8], const float* m, uint8_t* out, int Kpad, int row, int g)
+{
+    if (bits == 8) {
+        *reinterpret_cast<v2u*>(out + (size_t)row * Kpad + 8 * g) = v2u{quantize4<8>(y, m), quantize4<8>(y + 4, m + 4)};
+    } else {
+        const uint32_t a = quantize4<4>(y, m), b = quantize4<4>(y + 4, m + 4);
+        const uint32_t c = (a & 0x000f000fu) | ((a >> 4) & 0x00f000f0u), d = (b & 0x000f000fu) | ((b >> 4) & 0x00f000f0u);      // bytes 0 and 2: two values each
+        *reinterpret_cast<uint32_t*>(out + (size_t)row * (Kpad / 2) + 4 * g) = bytes_of(d, c, 0x06040200u);
+    }
+}
+
+// A thread has GPT times 8 channels, 8 (tid + k threads) on: neighbouring threads read neighbouring pieces.  KEEP: gamma and the multipliers of the channels' own
+// slots stay in registers.
+template <int XT, int RT, int PASS, int GPT, bool RAGGED>
 __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
 {
+    constexpr bool KEEP = GPT <= 2, FIND = PASS == FIND_SCALE || PASS == BOTH;
+    constexpr int HT = RT == NONE ? XT : RT;                        // h as it is stored
     extern __shared__ __align__(16) uint8_t lds[];
     double* part = reinterpret_cast<double*>(lds);                  // 16 waves
     float* best_of = reinterpret_cast<float*>(part + 16);           // 16 waves
-    float* table = best_of + 16;                                    // m(n)
+    float* few_t = best_of + 16;                                    // t of a few rows
+    float* table = few_t + FEW_ROWS;                                // m(n)
+    const int tid = threadIdx.x, threads = blockDim.x, K = a.K, G = (K + 7) / 8, Kpad = a.out ? a.Kpad : 0;
+    const int zero_at = 8 * G;
     float* row_y = table + TABLE;                                   // the row; behind it a zero
-    const int tid = threadIdx.x, threads = blockDim.x, K = a.K, G = (K + 15) / 16, Q = a.out ? a.Kpad / 16 : 0;
-    const int zero_at = 16 * G;
+    uint8_t* row_q = reinterpret_cast<uint8_t*>(row_y + row_places(K));     // codes of 16 slots a thread
+    const double per_channel = 1.0 / (double)K;
 
     Raw<XT> x[GPT];
     Raw<RT> r[GPT];
@@ -75,180 +134,255 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
         for (int k = 0; k < GPT; ++k) {
             const int g = tid + k * threads;
             if (g < G) {
-                x[k] = load_raw<XT>(a.X, (size_t)row * a.ldx, g, K);
-                r[k] = load_raw<RT>(a.R, (size_t)row * a.ldr, g, K);
+                x[k] = load_raw<XT, RAGGED>(row_of(a.X, a.ldx, element_bytes<XT>(), row), g, K);
+                r[k] = load_raw<RT, RAGGED>(row_of(a.R, a.ldr, element_bytes<RT>(), row), g, K);
             }
         }
     };
     fetch(blockIdx.x);
-
-    // ---- the bound and the multipliers ----
-    float bound = 0.0f;
-    if (PASS != FIND_SCALE && Q) {
-        if (PASS == ONE_PASS) {
-            bound = *a.absmax;
-            if (!(bound >= 0.0f) || bound > 3.0e38f) bound = 0.0f;     // negative / NaN / Inf static bound: treated as 0
-        } else {
-            for (int i = tid; i < a.candidates; i += threads) bound = fmaxf(bound, a.found[i]);
+    float kept_gamma[KEEP ? GPT : 1][8];
+    if constexpr (KEEP) {
 #pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) bound = fmaxf(bound, __shfl_xor(bound, off, 64));
-            if ((tid & 63) == 0) best_of[tid >> 6] = bound;
-            __syncthreads();
-            bound = best_of[0];
-            for (int w = 1; w < threads >> 6; ++w) bound = fmaxf(bound, best_of[w]);
-        }
-        const double qmax = a.bits == 8 ? 127.0 : 7.0;
-        for (int n = tid; n < TABLE; n += threads) table[n] = (n > 0 && bound != 0.0f) ? (float)(qmax / ((double)n * (double)bound)) : 0.0f;
-        if (blockIdx.x == 0 && tid == 0) *a.s_x = bound == 0.0f ? 1.0f : (float)((double)bound / qmax);
-        __syncthreads();
+        for (int k = 0; k < GPT; ++k)
+            if (tid + k * threads < G) load_any<RAGGED>(a.gamma, a.g_dtype, tid + k * threads, K, kept_gamma[k]);
     }
-    auto multiplier = [&](int n) -> float {
-        if (n <= 0 || bound == 0.0f) return 0.0f;
-        return n < TABLE ? table[n] : (float)((a.bits == 8 ? 127.0 : 7.0) / ((double)n * (double)bound));
+    auto normalise = [&](int k, float t, float (&y)[8]) {           // y holds h
+        float other[8];
+        if constexpr (!KEEP) load_any<RAGGED>(a.gamma, a.g_dtype, tid + k * threads, K, other);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = y[i] * t * (KEEP ? kept_gamma[KEEP ? k : 0][i] : other[i]);
     };
 
-    // ---- the map: slots of the thread's own channels, where they lie at their own place, and the others ----
-    float gamma[GPT][16], m[GPT][16];
-    bool own[GPT];
-    int first_other = 0;      // the thread's first group of slots that is not its own
+    // ---- the map: do the first slots lie at their channels' own places?  The slots from `base` on are the others.  (E3M2 codes are packed by sixteens: all.) ----
+    const int whole = KEEP && a.bits != FQ_BITS_I4_E3M2 ? min(K & ~15, Kpad) : 0;
+    int own_rep[KEEP ? GPT : 1][8];
+    bool apart = false, far = false;
+    if constexpr (KEEP) {
 #pragma unroll
-    for (int k = 0; k < GPT; ++k) {
-        const int g = tid + k * threads;
-        own[k] = false;
-        if (g < G) {
-            load_any(a.gamma, a.g_dtype, g, K, gamma[k]);
-            if (g < Q) {
-                int s[16], n[16];
-                load8(a.src + 16 * g, s);
-                load8(a.src + 16 * g + 8, s + 8);
-                load8(a.rep + 16 * g, n);
-                load8(a.rep + 16 * g + 8, n + 8);
-                own[k] = 16 * g + 16 <= K;
+        for (int k = 0; k < GPT; ++k) {
+            const int at = 8 * (tid + k * threads);
+            if (at < whole) {
+                int src[8];
+                load8(a.src + at, src);
+                load8(a.rep + at, own_rep[k]);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    own[k] = own[k] && s[i] == 16 * g + i;
-                    m[k][i] = PASS == FIND_SCALE ? (n[i] > 0 ? (float)n[i] : 0.0f) : multiplier(n[i]);
-                    if (PASS == FIND_SCALE && n[i] > (1 << 24)) own[k] = false;      // not a whole number in fp32
+                for (int i = 0; i < 8; ++i) {
+                    apart |= src[i] != at + i;
+                    far |= own_rep[k][i] >= TABLE;
                 }
             }
         }
-        if (own[k] && first_other == k) first_other = k + 1;
     }
-    // any slot group that is not its thread's own
-    bool others = false;
-    for (int k = 0, q = tid; q < Q; ++k, q += threads) others = others || k >= GPT || !own[k < GPT ? k : 0];
-    const bool gathers = __syncthreads_or(others);
-    if (gathers && tid == 0) row_y[zero_at] = 0.0f;
-
-    float most[GPT][16], quotient = 0.0f;
-    if (PASS == FIND_SCALE) {
-#pragma unroll
-        for (int k = 0; k < GPT; ++k)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most[k][i] = 0.0f;
+    const int base = __syncthreads_or(apart) ? 0 : whole;
+    far = __syncthreads_or(far);                                    // copy counts that the table does not have
+    const bool others = base < Kpad;
+    auto own = [&](int k) { return 8 * (tid + k * threads) < base; };
+    // In search of the bound a slot counts nothing that another slot of the same channel, at its own place and with no more copies, has counted.
+    bool to_count = false;
+    auto used = [&](int src, int rep) { return (unsigned)src < (unsigned)K && rep > 0; };
+    if (FIND) {
+        for (int p = base + tid; p < Kpad; p += threads) {
+            const int j = a.src[p], n = a.rep[p];
+            if (used(j, n) && !(j < base && a.rep[j] > 0 && a.rep[j] <= n)) to_count = true;
+        }
+        to_count = __syncthreads_or(to_count);
     }
+    if (tid == 0) row_y[zero_at] = 0.0f;
+    auto to_lds = [&](int g, const float (&y)[8]) {
+        *reinterpret_cast<v4f*>(row_y + 8 * g) = v4f{y[0], y[1], y[2], y[3]};
+        *reinterpret_cast<v4f*>(row_y + 8 * g + 4) = v4f{y[4], y[5], y[6], y[7]};
+    };
 
-    for (int row = blockIdx.x; row < a.M; row += gridDim.x) {
-        float y[GPT][16];
-        double sum = 0.0;
+    // h of a row from what fetch() brought, and the sum of its squares
+    auto residual = [&](int row, float (&y)[GPT][8], double& sum) {
 #pragma unroll
         for (int k = 0; k < GPT; ++k) {
             const int g = tid + k * threads;
             if (g >= G) continue;
             widen<XT>(x[k], y[k]);
             if constexpr (RT != NONE) {
-                float add[16];
+                float add[8];
                 widen<RT>(r[k], add);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[k][i] = y[k][i] + add[i];
+                for (int i = 0; i < 8; ++i) y[k][i] = y[k][i] + add[i];
                 const Raw<RT> h = narrow<RT>(y[k]);
-                store_raw<RT>(h, a.R_out, (size_t)row * a.ldro, g, K);
+                store_raw<RT, RAGGED>(h, row_of(a.R_out, a.ldro, element_bytes<RT>(), row), g, K);
                 widen<RT>(h, y[k]);
             }
             if (PASS != WITH_SCALE) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum = __builtin_fma((double)y[k][i], (double)y[k][i], sum);
+                for (int i = 0; i < 8; ++i) sum = __builtin_fma((double)y[k][i], (double)y[k][i], sum);
             }
         }
         if (row + (int)gridDim.x < a.M) fetch(row + gridDim.x);
-        float t;
-        if (PASS == WITH_SCALE) {
-            t = a.t[row];
-            if (gathers) strip_barrier();          // the row before is read no more
-        } else {
-            t = (float)(1.0 / sqrt(sum_of(sum, part) / (double)K + (double)a.eps));
-            if (PASS == FIND_SCALE && tid == 0) a.t[row] = t;
+    };
+    auto inverse_rms = [&](double sum) -> float { return (float)inverse_root(__builtin_fma(sum_of(sum, part), per_channel, (double)a.eps)); };
+
+    // ---- the bound ----
+    float bound = 0.0f;
+    if constexpr (FIND) {
+        float most[GPT][8];
+        Largest largest;
+#pragma unroll
+        for (int k = 0; k < GPT; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most[k][i] = 0.0f;
+        for (int row = blockIdx.x; row < a.M; row += gridDim.x) {
+            float y[GPT][8];
+            double sum = 0.0;
+            residual(row, y, sum);
+            const float t = inverse_rms(sum);
+            if (tid == 0) {
+                if (PASS == BOTH) few_t[row] = t;
+                else a.t[row] = t;
+            }
+#pragma unroll
+            for (int k = 0; k < GPT; ++k) {
+                const int g = tid + k * threads;
+                if (g >= G) continue;
+                normalise(k, t, y[k]);
+                if (to_count) to_lds(g, y[k]);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) most[k][i] = fmaxf(most[k][i], fabsf(y[k][i]));
+            }
+            strip_barrier();
+            if (!to_count) continue;
+            for (int p = base + tid; p < Kpad; p += threads) {
+                const int j = a.src[p], n = a.rep[p];
+                if (used(j, n)) largest.see(row_y[j], n);
+            }
         }
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int k = 0; k < GPT; ++k)
+                if (own(k)) {
+                    if (PASS != BOTH) load8(a.rep + 8 * (tid + k * threads), own_rep[k]);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (own_rep[k][i] > 0) largest.see(most[k][i], own_rep[k][i]);
+                }
+        }
+        bound = largest_of(largest.get(), best_of);
+        if (PASS == FIND_SCALE) {
+            if (tid == 0) a.found[blockIdx.x] = bound;
+            return;
+        }
+    } else if (Kpad) {
+        if (PASS == ONE_PASS) {
+            bound = *a.absmax;
+            if (!(bound >= 0.0f) || bound > 3.0e38f) bound = 0.0f;     // negative / NaN / Inf static bound: treated as 0
+        } else {
+            for (int i = tid; i < a.candidates; i += threads) bound = fmaxf(bound, a.found[i]);
+            bound = largest_of(bound, best_of);
+        }
+    }
+
+    // ---- multipliers ----
+    const double qmax = a.bits == 8 ? 127.0 : 7.0;
+    auto formed = [&](int n) -> float { return n > 0 && bound != 0.0f ? (float)(qmax / ((double)n * (double)bound)) : 0.0f; };
+    auto multiplier = [&](int n) -> float { return (unsigned)n < TABLE ? table[n] : formed(n); };
+    float own_m[KEEP ? GPT : 1][8], other_m[KEPT];
+    int other_at[KEPT];                  // the first of the other slots that this thread works on: places in the row, multipliers
+    if (Kpad) {
+        for (int n = tid; n < TABLE; n += threads) table[n] = formed(n);
+        if (blockIdx.x == 0 && tid == 0) *a.s_x = bound == 0.0f ? 1.0f : (float)((double)bound / qmax);
+        __syncthreads();
+        if constexpr (KEEP) {
+            if (far) {                   // each formed once, by whichever thread
+                for (int p = tid; p < base; p += threads) row_y[p] = multiplier(a.rep[p]);
+                __syncthreads();
+            }
+#pragma unroll
+            for (int k = 0; k < GPT; ++k)
+                if (own(k)) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) own_m[k][i] = far ? row_y[8 * (tid + k * threads) + i] : table[max(own_rep[k][i], 0)];
+                }
+            if (far) __syncthreads();
+        }
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) {
+            const int p = base + i * threads + tid;
+            other_at[i] = zero_at;
+            other_m[i] = 0.0f;
+            if (p < Kpad) {
+                const int j = a.src[p], n = a.rep[p];
+                if (used(j, n)) {
+                    other_at[i] = j;
+                    other_m[i] = multiplier(n);
+                }
+            }
+        }
+    }
+
+    // ---- rows ----
+    auto code = [&](float v, float m) -> uint8_t { return (uint8_t)(a.bits == 8 ? quantized_bits<8>(v, m) : quantized_bits<4>(v, m)); };
+    auto codes_of_row = [&](int row, float t, float (&y)[GPT][8]) {
 #pragma unroll
         for (int k = 0; k < GPT; ++k) {
             const int g = tid + k * threads;
             if (g >= G) continue;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[k][i] = y[k][i] * t * gamma[k][i];
-            if (PASS != FIND_SCALE && a.Y) store_any(y[k], a.Y, a.y_dtype, (size_t)row * a.ldy, g, K);
-            if (gathers) {
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) *reinterpret_cast<v4f*>(row_y + place(16 * g + i)) = v4f{y[k][i], y[k][i + 1], y[k][i + 2], y[k][i + 3]};
-            }
-            if (own[k]) {
-                if (PASS == FIND_SCALE) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) most[k][i] = fmaxf(most[k][i], fabsf(y[k][i]));
-                } else {
-                    store_codes(a.bits, y[k], m[k], a.out, a.Kpad, a.M, row, g);
-                }
+            normalise(k, t, y[k]);
+            if (a.Y) store_any<RAGGED>(y[k], row_of(a.Y, a.ldy, a.y_dtype == FQ_F32 ? 4 : 2, row), a.y_dtype, g, K);
+            if (others) to_lds(g, y[k]);
+            if constexpr (KEEP) {
+                if (own(k)) store_eight(a.bits, y[k], own_m[k], a.out, Kpad, row, g);
             }
         }
-        if (!gathers) {
-            if (PASS != WITH_SCALE) strip_barrier();      // part is read no more
-            continue;
-        }
-        strip_barrier();
-        for (int k = first_other, q = tid + first_other * threads; q < Q; ++k, q += threads) {
-            if (k < GPT && own[k < GPT ? k : 0]) continue;
-            int s[16], n[16];
-            load8(a.src + 16 * q, s);
-            load8(a.src + 16 * q + 8, s + 8);
-            load8(a.rep + 16 * q, n);
-            load8(a.rep + 16 * q + 8, n + 8);
-            float v[16], by[16];
+        strip_barrier();                 // the row lies in LDS, and the sum's parts are read no more
+        for (int from = base; from < Kpad; from += 16 * threads) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const bool used = (unsigned)s[i] < (unsigned)K && n[i] > 0;
-                v[i] = row_y[used ? place(s[i]) : zero_at];
-                if (PASS == FIND_SCALE) quotient = fmaxf(quotient, used ? (n[i] == 1 ? fabsf(v[i]) : (float)((double)fabsf(v[i]) / (double)n[i])) : 0.0f);
-                else by[i] = multiplier(n[i]);
+            for (int i = 0; i < KEPT; ++i) {
+                const int p = i * threads + tid;
+                if (from == base && from + p < Kpad) row_q[p] = code(row_y[other_at[i]], other_m[i]);
             }
-            if (PASS != FIND_SCALE) store_codes(a.bits, v, by, a.out, a.Kpad, a.M, row, q);
-        }
-    }
-
-    if (PASS == FIND_SCALE) {
-#pragma unroll
-        for (int k = 0; k < GPT; ++k)
-            if (own[k]) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) quotient = fmaxf(quotient, m[k][i] > 0.0f ? (float)((double)most[k][i] / (double)m[k][i]) : 0.0f);
+            for (int p = (from == base ? KEPT * threads : 0) + tid; p < min(Kpad - from, 16 * threads); p += threads) {
+                const int j = a.src[from + p], n = a.rep[from + p];
+                row_q[p] = used(j, n) ? code(row_y[j], multiplier(n)) : (uint8_t)0;
             }
+            strip_barrier();
+            if (from + 16 * tid < Kpad) store_packed(a.bits, *reinterpret_cast<const v4u*>(row_q + 16 * tid), a.out, Kpad, a.M, row, from / 16 + tid);
+            if (from + 16 * threads < Kpad) strip_barrier();
+        }
+    };
+    for (int row = blockIdx.x; row < a.M; row += gridDim.x) {
+        float y[GPT][8];
+        if constexpr (PASS == BOTH) {    // what this thread has stored itself
+            const float t = few_t[row];
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) quotient = fmaxf(quotient, __shfl_xor(quotient, off, 64));
-        __syncthreads();
-        if ((tid & 63) == 0) best_of[tid >> 6] = quotient;
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < threads >> 6; ++w) quotient = fmaxf(quotient, best_of[w]);
-            a.found[blockIdx.x] = quotient;
+            for (int k = 0; k < GPT; ++k) {
+                const int g = tid + k * threads;
+                if (g < G) widen<HT>(load_raw<HT, RAGGED>(row_of(RT == NONE ? a.X : a.R_out, RT == NONE ? a.ldx : a.ldro, element_bytes<HT>(), row), g, K), y[k]);
+            }
+            strip_barrier();             // the row before is read no more
+            codes_of_row(row, t, y);
+        } else {
+            double sum = 0.0;
+            residual(row, y, sum);
+            if constexpr (PASS == WITH_SCALE) {
+                const float t = a.t[row];
+                if (others) strip_barrier();
+                codes_of_row(row, t, y);
+            } else {
+                codes_of_row(row, inverse_rms(sum), y);
+            }
         }
     }
 }
 
+// Two pieces of 8 channels a thread, four of rows that 1024 threads do not hold so
+int norm_threads(int K) { return std::min(1024, ((K + 7) / 8 + 127) / 128 * 64); }
+
 template <int XT, int RT, int PASS> int launch(const Norm& a, int wgs, hipStream_t stream)
 {
-    const int G = (a.K + 15) / 16, threads = std::min(1024, (G + 63) / 64 * 64);
-    const int smem = 16 * 8 + 16 * 4 + TABLE * 4 + (16 * G + 16) * 4;
-    auto kern = G <= 1024 ? rms_norm_kernel<XT, RT, PASS, 1> : rms_norm_kernel<XT, RT, PASS, 2>;
-    static std::atomic<unsigned long long> attr_set[2];
-    if (int rc = set_lds_limit(reinterpret_cast<const void*>(kern), 136 * 1024, attr_set[G <= 1024 ? 0 : 1])) return rc;
+    const int threads = norm_threads(a.K);
+    const bool two = a.K <= 2 * 8 * threads;
+    const int smem = 16 * 8 + (16 + FEW_ROWS + TABLE + row_places(a.K)) * 4 + 16 * threads;
+    const bool ragged = a.K % 8 != 0;
+    auto kern = ragged ? (two ? rms_norm_kernel<XT, RT, PASS, 2, true> : rms_norm_kernel<XT, RT, PASS, 4, true>)
+                       : (two ? rms_norm_kernel<XT, RT, PASS, 2, false> : rms_norm_kernel<XT, RT, PASS, 4, false>);
+    static std::atomic<unsigned long long> attr_set[4];
+    if (int rc = set_lds_limit(reinterpret_cast<const void*>(kern), 152 * 1024, attr_set[(two ? 0 : 1) + (ragged ? 2 : 0)])) return rc;
     kern<<<(unsigned)wgs, threads, smem, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FQ_ERR_HIP, "norm launch failed: %s", hipGetErrorString(e));
@@ -288,11 +422,13 @@ int launch_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, con
     a.ldx = ldx; a.ldr = ldr; a.ldro = ldro; a.ldy = ldy;
     a.M = M; a.K = K; a.Kpad = Kpad; a.g_dtype = g_dtype; a.y_dtype = y_dtype; a.bits = bits; a.eps = eps;
     a.src = src; a.rep = rep; a.absmax = absmax_in; a.out = static_cast<uint8_t*>(Xq_out); a.s_x = s_x_out;
-    const int wgs = std::min(M, MAX_WGS), rt = R ? r_dtype : NONE;
+    // 16 waves a CU
+    const int wgs = std::min(M, std::min(MAX_WGS, compute_units() * std::max(1, 1024 / norm_threads(K)))), rt = R ? r_dtype : NONE;
     if (!Xq_out || absmax_in) return launch_types<ONE_PASS>(a, x_dtype, rt, wgs, stream);
     a.t = static_cast<float*>(workspace);
     a.found = a.t + round_up((size_t)M * 4, 16) / 4;
     a.candidates = wgs;
+    if (M <= FEW_ROWS) return launch_types<BOTH>(a, x_dtype, rt, 1, stream);
     if (int rc = launch_types<FIND_SCALE>(a, x_dtype, rt, wgs, stream)) return rc;
     if (R) {        // the second pass reads what the first one stored
         a.X = R_out;
