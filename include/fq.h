@@ -387,7 +387,7 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  * stay as they are (no flattening).
  *
  *   w[n,k] = S[n, k / group] * q[n,k] + B[n, k / group]        q in [-8, 7];  B NULL: no offsets
- *   Wq  [N, K / 2] bytes, two's-complement nibbles, even column in the low one; rows dense.  K a multiple of 32.
+ *   Wq  [N, K / 2] bytes, two's-complement nibbles, even column in the low one; rows dense.  K a multiple of 32, at most 2^24.
  *   S, B  [N, ceil(K / group)], dense, s_dtype F32 / F16 / BF16; group 32, 64 or 128; a row's last group may be a short one.
  *
  * fq_group_weights_i4 — offline: the weights' codes, scales and offsets.  W [N, K] F32 / F16 / BF16, row stride ldw (a multiple of 16 bytes).
@@ -397,7 +397,7 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  *   likewise (between -largest and largest);  q = clamp(rne(fl32(fl32(w - b) * fl32(1 / s))), -8, 7), 0 for s = 0  (b = 0 without offsets).
  *
  * fq_linear_group_i4 — Y[i,n] = round_to_y_dtype(sum_k X[i,k] * w[n,k] + bias[n]).
- *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
+ *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes, at most 2^24 elements); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
  *   Products of activations and codes are exact (BF16: codes enter as q + 24, whose surplus leaves with the activations' sum); sums, and scales
  *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights; no limit on M.
  *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.

@@ -12,9 +12,9 @@ from .binding import (FQ_BF16, FQ_F16, FQ_F32, FQ_I32, FqError, LIB_PATH, SYMBOL
                       fq_linear_workspace_bytes, fq_rms_norm_quant, fq_rms_norm_workspace_bytes, fq_smooth_scales, fq_threshold_boxplot, fq_version,
                       fq_weights_workspace_bytes, fq_peak_mfma, fq_peak_copy, fq_peak_gemm_ticks, fq_peak_wall_clock_khz, lib)
 from .kv_cache import FqKvCache
-from .layer import FqLinear
+from .layer import FqGroupLinear, FqLinear
 
-__all__ = ["FQ_BF16", "FQ_F16", "FQ_F32", "FQ_I32", "FqError", "FqKvCache", "FqLinear", "LIB_PATH", "SYMBOLS",
+__all__ = ["FQ_BF16", "FQ_F16", "FQ_F32", "FQ_I32", "FqError", "FqGroupLinear", "FqKvCache", "FqLinear", "LIB_PATH", "SYMBOLS",
            "fq_attn_cache", "fq_attn_cache_workspace_bytes", "fq_attn_prompt", "fq_kv_append", "fq_kv_copy_pages", "fq_rms_norm_quant",
            "fq_rms_norm_workspace_bytes", "fq_group_weights_i4", "fq_linear_group_i4",
            "fq_act_workspace_bytes", "fq_bmm_i4", "fq_bmm_i8", "fq_channel_absmax", "fq_flatten_plan", "fq_flatten_plan_xw",

@@ -13,6 +13,7 @@ int check_group(int group, int K)
 {
     if (group != 32 && group != 64 && group != 128) return fail(FQ_ERR_SHAPE, "group = %d must be 32, 64 or 128", group);
     if (K % 32 != 0) return fail(FQ_ERR_SHAPE, "K = %d must be a multiple of 32", K);
+    if (K > MAX_GROUP_WIDTH) return fail(FQ_ERR_RANGE, "K = %d: at most 2^24", K);
     return FQ_OK;
 }
 
@@ -100,6 +101,7 @@ int fq_linear_group_i4(const void* X, int x_dtype, int M, int K, int ldx, const 
     if (!rc) rc = check_dense("bias", bias, false);
     if (!rc) rc = check_dense("Y", Y, true);
     if (rc) return rc;
+    if (ldx > MAX_GROUP_WIDTH) return fail(FQ_ERR_RANGE, "X: row stride of %d elements, at most 2^24", ldx);
     if (N <= 0) return fail(FQ_ERR_SHAPE, "N = %d must be positive", N);
     if (ldy < N) return fail(FQ_ERR_SHAPE, "ldy = %d < N = %d", ldy, N);
     if (!group_holds(M, N)) return fail(FQ_ERR_RANGE, "%d x %d outputs are more than one launch holds", M, N);

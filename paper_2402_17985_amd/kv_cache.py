@@ -6,10 +6,13 @@ from . import binding as B
 class FqKvCache:
     """`pages` pages of `page_size` tokens, shared by up to `batch` sequences of at most `max_len` tokens each.
 
-    Calls go to the current stream.  attend() may run on several streams at once; reserve(), release() and append() change the table and the pages, and the
-    caller orders them with what else uses the cache.  append() and attend() copy their counts from the host, which waits for the stream: inside a captured
-    graph use the fq_* calls with counts on the device.  A sequence's last tokens (rejected drafts) are dropped by setting lengths[b] to what stays: the next
-    ones take their places; its pages stay with it."""
+    Calls go to the current stream.  attend() may run on several streams at once; reserve(), release(), append(), fork() and compact() change the table and the
+    pages, and the caller orders them with what else uses the cache.  append() and attend() copy their counts from the host, which waits for the stream (so do
+    fork() and compact() with page numbers): inside a captured graph use the fq_* calls with counts on the device.  A sequence's last tokens (rejected drafts) are dropped by setting lengths[b] to what stays: the next
+    ones take their places; its pages stay with it.
+
+    Sequences that fork() made from one another share pages.  An append copies what it would change of them first, so that each sequence keeps its own
+    past; appending takes pages for that.  (The fq_* calls know nothing of shared pages: give a sequence its own, by an append here, before they write.)"""
 
     def __init__(self, pages: int, batch: int, max_len: int, heads_kv: int, head_dim: int, page_size: int = 64, rope_cos=None, rope_sin=None,
                  interleaved: bool = False, device="cuda:0"):
@@ -27,6 +30,7 @@ class FqKvCache:
         self.held = [[] for _ in range(batch)]      # page numbers of each sequence
         self.lengths = [0] * batch
         self._free = list(range(pages - 1, -1, -1))
+        self._users = [0] * pages                   # sequences that hold a page
 
     def _i32(self, values):
         return self.torch.tensor(values, dtype=self.torch.int32, device=self.device)
@@ -52,24 +56,106 @@ class FqKvCache:
         if need - have > len(self._free):
             raise RuntimeError(f"{need - have} pages wanted, {len(self._free)} free")
         if need > have:
-            self.held[b] += [self._free.pop() for _ in range(need - have)]
+            self.held[b] += [self._take() for _ in range(need - have)]
             self.page_table[b, have:need] = self._i32(self.held[b][have:])
 
+    def _take(self) -> int:
+        page = self._free.pop()
+        self._users[page] = 1
+        return page
+
+    def _drop(self, page: int) -> None:
+        self._users[page] -= 1
+        if self._users[page] == 0:
+            self._free.append(page)
+
     def release(self, b: int) -> None:
-        """Sequence b ends: its pages are free again."""
-        self._free += reversed(self.held[b])
+        """Sequence b ends: pages that no other sequence shares are free again."""
+        for page in reversed(self.held[b]):
+            self._drop(page)
         self.held[b], self.lengths[b] = [], 0
         self.page_table[b].fill_(-1)
+
+    def fork(self, b: int, into) -> None:
+        """The sequences `into` (which must hold nothing) continue sequence b's tokens: they share its pages, and nothing is copied until one of them grows."""
+        into = list(into)
+        if len(set(into)) < len(into) or any(not 0 <= c < self.batch for c in [b] + into):
+            raise ValueError(f"fork of sequence {b} into {into} of {self.batch}")
+        if any(self.held[c] for c in into):
+            raise ValueError(f"sequences {[c for c in into if self.held[c]]} hold pages: release them first")
+        used = -(-self.lengths[b] // self.page_size)          # pages reserved ahead stay b's own
+        pages = self.held[b][:used]
+        for c in into:
+            for page in pages:
+                self._users[page] += 1
+            self.held[c], self.lengths[c] = list(pages), self.lengths[b]
+        if pages and into:
+            self.page_table[self._i64(into), :used] = self._i32(pages)
+
+    def _i64(self, values):
+        return self.torch.tensor(values, dtype=self.torch.int64, device=self.device)
+
+    def _copy(self, src, dst) -> None:
+        if src:
+            B.fq_kv_copy_pages(self.k_cache, self.v_cache, self.k_scale, self.v_scale, self._i32(src), self._i32(dst))
+
+    def _writes(self, b: int, grown: int):
+        """Places in held[b] of the shared pages that appending up to `grown` tokens writes to: whose past must stay with the others."""
+        first, end = self.lengths[b] // self.page_size, -(-grown // self.page_size)
+        return [i for i in range(first, min(end, len(self.held[b]))) if self._users[self.held[b][i]] > 1] if grown > self.lengths[b] else []
+
+    def _own(self, b: int, grown: int):
+        """Gives sequence b pages of its own where it is about to write.  Returns the (page, copy) that must be made first: of a page that it goes on
+        filling; one that it starts anew has nothing to copy."""
+        copies = []
+        for i in self._writes(b, grown):
+            old = self.held[b][i]
+            if self._users[old] == 1:         # the others have taken copies meanwhile
+                continue
+            new = self._take()
+            if self.lengths[b] > i * self.page_size:
+                copies.append((old, new))
+            self._drop(old)
+            self.held[b][i] = new
+            self.page_table[b, i] = new
+        return copies
+
+    def compact(self) -> int:
+        """Moves pages so that those in use are the first ones of the pool, and returns their number.  Sequences keep what they hold."""
+        live = sum(1 for n in self._users if n)
+        moved = [page for page in range(live, len(self._users)) if self._users[page]]
+        room = [page for page in range(live) if not self._users[page]]
+        to = dict(zip(moved, room))
+        self._copy(moved, room)
+        for old, new in to.items():
+            self._users[new], self._users[old] = self._users[old], 0
+        for b, held in enumerate(self.held):
+            if any(page in to for page in held):
+                self.held[b] = [to.get(page, page) for page in held]
+                self.page_table[b, :len(held)] = self._i32(self.held[b])
+        self._free = list(range(len(self._users) - 1, live - 1, -1))
+        return live
+
+    def _copies_wanted(self, grown) -> int:
+        """Pages that an append up to `grown` tokens takes in place of shared ones: one for each writer, but for the last of a page that all its holders write."""
+        writers = {}
+        for b, n in enumerate(grown):
+            for i in self._writes(b, n):
+                page = self.held[b][i]
+                writers[page] = writers.get(page, 0) + 1
+        return sum(min(n, self._users[page] - 1) for page, n in writers.items())
 
     def append(self, Q, K, V, new, Q_out=None, K_out=None) -> None:
         """Append new[b] tokens to every sequence b (0: none): the rows of K, V (and Q) in order.  See fq_kv_append."""
         self._check_counts("new", new, "K", K.shape[0])
         grown = [n + m for n, m in zip(self.lengths, new)]
-        wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held))
+        wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held)) + self._copies_wanted(grown)
         if wanted > len(self._free) or max(grown) > self.max_len:
             raise RuntimeError(f"{wanted} pages wanted, {len(self._free)} free; longest sequence {max(grown)} of {self.max_len}")
+        copies = [pair for b, n in enumerate(grown) for pair in self._own(b, n)]
         for b, n in enumerate(grown):
             self.reserve(b, n)
+        self._copy([old for old, _ in copies], [new for _, new in copies])
         B.fq_kv_append(Q, K, V, self._i32(self._offsets(new)), self._i32(self.lengths), max(1, max(new)), self.k_cache, self.v_cache, self.k_scale,
                        self.v_scale, self.page_table, rope_cos=self.rope_cos, rope_sin=self.rope_sin, interleaved=self.interleaved,
                        Q_out=Q_out, K_out=K_out)

@@ -1,5 +1,5 @@
-"""Buffer bookkeeping for one quantized linear layer: owns the device buffers the C ABI wants
-(map, quantized weights, scales, workspace) and forwards to the fq_* calls.  No arithmetic."""
+"""Buffer bookkeeping for one quantized linear layer (FqLinear) and for one with group-scaled 4-bit weights (FqGroupLinear): owns the
+device buffers the C ABI wants (map, quantized weights, scales, workspace) and forwards to the fq_* calls.  No arithmetic."""
 import numpy as np
 
 from . import binding as B
@@ -48,4 +48,51 @@ class FqLinear:
         if Y is None:
             Y = self.torch.empty((M, self.N), dtype=out_dtype or self.torch.bfloat16, device=X.device)
         B.fq_linear(X, self.src, self.rep, self.Wq, self.s_w, self.bits, Y, self.workspace(M), absmax_in=absmax_in)
+        return Y
+
+    def forward_norm(self, X, gamma, eps: float, R=None, R_out=None, Y=None, out_dtype=None, absmax_in=None):
+        """The layer on the root-mean-square norm of X (plus the residual R, whose sum goes to R_out; R_out=None: into R itself): the norm's result goes
+        to the product as codes.  See fq_rms_norm_quant; absmax_in bounds the norm's result, after gamma."""
+        M = X.shape[0]
+        t = self.torch
+        if Y is None:
+            Y = t.empty((M, self.N), dtype=out_dtype or t.bfloat16, device=X.device)
+        if R is not None and R_out is None:
+            R_out = R
+        # of this call: torch's allocator gives them to no other stream before the kernels are through
+        if self.bits == B.FQ_BITS_I4_E3M2:
+            Xq = t.empty((self.Kpad // 128, M, 96), dtype=t.uint8, device=X.device)
+        else:
+            Xq = t.empty((M, self.Kpad if self.bits == 8 else self.Kpad // 2), dtype=t.int8 if self.bits == 8 else t.uint8, device=X.device)
+        s_x = t.empty(1, dtype=t.float32, device=X.device)
+        ws = None if absmax_in is not None else t.empty(B.fq_rms_norm_workspace_bytes(M, self.K, self.Kpad), dtype=t.uint8, device=X.device)
+        B.fq_rms_norm_quant(X, gamma, eps, R=R, R_out=R_out, src_idx=self.src, rep=self.rep, bits=self.bits, Xq_out=Xq, s_x_out=s_x, workspace=ws, absmax_in=absmax_in)
+        if self.bits == B.FQ_BITS_I4_E3M2:
+            B.fq_gemm_i4_e3m2(Xq, self.Wq, s_x, self.s_w, None, Y)
+        else:
+            (B.fq_gemm_i8 if self.bits == 8 else B.fq_gemm_i4)(Xq, self.Wq, s_x, self.s_w, Y)
+        return Y
+
+
+class FqGroupLinear:
+    """A linear layer with 4-bit weights and a scale (and offset) for each row and group of columns; activations stay 16-bit."""
+
+    def __init__(self, W, group: int = 128, offsets: bool = False, scale_dtype=None, bias=None, device="cuda:0"):
+        """W [N, K], K a multiple of 32; group 32, 64 or 128; scale_dtype: of scales and offsets (W's type); bias fp32 [N]."""
+        import torch
+        self.torch = torch
+        self.N, self.K = W.shape
+        self.group, self.bias = group, bias
+        if group not in (32, 64, 128):
+            raise ValueError(f"groups of {group} columns: 32, 64 or 128")
+        shape = (self.N, -(-self.K // group))
+        self.Wq = torch.empty((self.N, self.K // 2), dtype=torch.uint8, device=device)
+        self.S = torch.empty(shape, dtype=scale_dtype or W.dtype, device=device)
+        self.B = torch.empty_like(self.S) if offsets else None
+        B.fq_group_weights_i4(W, group, self.Wq, self.S, B_out=self.B)
+
+    def forward(self, X, Y=None, out_dtype=None):
+        if Y is None:
+            Y = self.torch.empty((X.shape[0], self.N), dtype=out_dtype or X.dtype, device=X.device)
+        B.fq_linear_group_i4(X, self.Wq, self.S, self.group, Y, B=self.B, bias=self.bias)
         return Y

@@ -1,0 +1,232 @@
+"""Norm, group-scaled products and page copies as a serving program uses them: together with the quantized layer, the cache and its attention, from captured
+graphs, on other streams, and what the binding refuses."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2402_17985_amd as fq
+from oracle import fq_oracle as O
+from oracle import step as S
+from tests import step_util as T
+
+pytestmark = pytest.mark.gpu
+EPS = 1e-5
+
+
+def bf16(rng, *shape, scale=1.0):
+    return torch.from_numpy((scale * rng.standard_normal(shape)).astype(np.float32)).to(torch.bfloat16).to(T.DEV)
+
+
+@pytest.mark.parametrize("bits", [8, 4, fq.binding.FQ_BITS_I4_E3M2])
+@pytest.mark.parametrize("static", [False, True])
+def test_the_layer_after_its_norm(bits, static):
+    """FqLinear.forward_norm: the residual goes on in place, the product is the oracle's of the oracle's codes, bit for bit."""
+    rng = np.random.default_rng(bits)
+    M, K, N = 37, 512, 192
+    chmax = np.where(np.arange(K) % 9 == 0, 3.0, 1.0).astype(np.float32)
+    W, X, R = bf16(rng, N, K, scale=0.04), bf16(rng, M, K), bf16(rng, M, K)
+    g = bf16(rng, K)
+    layer = fq.FqLinear(W, chmax, 1.5, bits)
+    want_h, _, q, s_x = S.rms_norm_quant(X.float().cpu().numpy(), g.float().cpu().numpy(), EPS, layer.src_host, layer.rep_host, 4 if bits == 6 else bits,
+                                         2.0 if static else None, R.float().cpu().numpy(), "bf16")
+    Wq, s_w = O.flatten_weights(W.float().cpu().numpy(), layer.src_host, 4 if bits == 6 else bits)
+    y = layer.forward_norm(X, g, EPS, R=R, out_dtype=torch.float32, absmax_in=torch.tensor([2.0], device=T.DEV) if static else None)
+    assert T.same_values(R, want_h, "bf16")
+    assert np.array_equal(y.cpu().numpy(), O.dequant_out(O.gemm_i32(q, Wq), s_x, s_w, "f32"))
+
+
+@pytest.mark.parametrize("offsets", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_group_linear(group, offsets):
+    """FqGroupLinear from weights to output; the error is the weights' quantization, at most half a step of each (and the offset's and scale's roundings)."""
+    rng = np.random.default_rng(group)
+    W, X = bf16(rng, 96, 416, scale=0.05), bf16(rng, 21, 416)
+    layer = fq.FqGroupLinear(W, group, offsets, bias=torch.ones(96, device=T.DEV))
+    q, s, b = S.group_weights(W.float().cpu().numpy(), group, "bf16", offsets)
+    assert np.array_equal(layer.Wq.cpu().numpy(), S.pack(q))
+    want, size = S.linear_group(X.float().cpu().numpy(), q, s, b, group, np.ones(96, np.float32))
+    y = layer.forward(X, out_dtype=torch.float32).cpu().numpy()
+    assert np.all(np.abs(y - want) <= 200 * 2.0**-24 * size)
+    with pytest.raises(ValueError, match="groups"):
+        fq.FqGroupLinear(W, 100)
+
+
+def layer_step(rng, cache, weights, x, new):
+    """One decoder layer's attention half on the rows x (the residual stream, updated in place): what each sequence's rows become."""
+    qkv, out, gamma, hq, hkv, dim = weights
+    rows = qkv.forward_norm(torch.zeros_like(x), gamma, EPS, R=x)
+    q, k, v = (t.unflatten(1, (-1, dim)) for t in rows.split([hq * dim, hkv * dim, hkv * dim], 1))
+    cache.append(q, k, v, new)
+    y = cache.attend(q, new, dim**-0.5)
+    return x + out.forward(y.flatten(1))
+
+
+def test_a_conversation_continued_in_several_ways():
+    """Sequences that fork() made give, bit for bit, what sequences with a past of their own give; so they do after compact() and releases.
+    Every step runs norm, quantized product, append, attention and a group-scaled product."""
+    rng = np.random.default_rng(0)
+    hidden, hq, hkv, dim, page = 256, 4, 2, 64, 64
+    qkv = fq.FqLinear(bf16(rng, (hq + 2 * hkv) * dim, hidden, scale=0.06), np.full(hidden, 4.0, np.float32), 4.5, 8)
+    weights = qkv, fq.FqGroupLinear(bf16(rng, hidden, hq * dim, scale=0.06), 64), bf16(rng, hidden), hq, hkv, dim
+    bound = torch.tensor([6.0], device=T.DEV)      # one bound for all calls: a dynamic one would go by the other sequences
+    forward = qkv.forward_norm
+    qkv.forward_norm = lambda *a, **k: forward(*a, **k, absmax_in=bound)
+    forked, apart = (fq.FqKvCache(24, 3, 320, hkv, dim, page) for _ in range(2))
+    for c in (forked, apart):
+        for t in (c.k_cache, c.v_cache):
+            t.fill_(77)
+    prompt = bf16(rng, 150, hidden)
+    one = layer_step(rng, forked, weights, prompt.clone(), [150, 0, 0])
+    three = layer_step(rng, apart, weights, prompt.repeat(3, 1), [150, 150, 150])
+    assert torch.equal(one.repeat(3, 1), three)
+    forked.fork(0, [1, 2])
+    used = 24 - len(forked._free)
+    assert used == 3
+    for i, new in enumerate(([1, 1, 1], [4, 0, 1], [1, 80, 1], [1, 1, 60], [1, 1, 1])):
+        x = bf16(rng, sum(new), hidden)
+        if i == 3:
+            forked.lengths[1] = apart.lengths[1] = 100             # rejected drafts, back into what was shared
+        a, b = (layer_step(rng, c, weights, x.clone(), new) for c in (forked, apart))
+        assert torch.equal(a, b), i
+        if i == 2:
+            live = forked.compact()
+            assert live == len(set(sum(forked.held, []))) == max(max(h) for h in forked.held) + 1
+    forked.release(0)
+    x = bf16(rng, 2, hidden)
+    a, b = (layer_step(rng, c, weights, x.clone(), [0, 1, 1]) for c in (forked, apart))
+    assert torch.equal(a, b)
+
+
+def test_captured_and_replayed():
+    """A step of all calls in one graph, replayed with other inputs in the same places, with eager work between the replays."""
+    rng = np.random.default_rng(3)
+    M, K, N = 24, 640, 320
+    src, rep, _, Kpad = T.plan(rng, K, 0.2)
+    src, rep = (torch.from_numpy(a).to(T.DEV) for a in (src, rep))
+    x, r, g = bf16(rng, M, K), bf16(rng, M, K), bf16(rng, K)
+    wq, s, b = torch.randint(0, 256, (N, K // 2), dtype=torch.uint8, device=T.DEV), torch.rand(N, 5, device=T.DEV), torch.randn(N, 5, device=T.DEV)
+    one = bf16(rng, 1, K)
+    caches = [torch.randint(-128, 128, s_, dtype=torch.int8, device=T.DEV) for s_ in ((9, 2, 64, 64), (9, 2, 64, 64))] + [torch.rand(9, 2, device=T.DEV) for _ in range(2)]
+    pages = [torch.tensor(p, dtype=torch.int32, device=T.DEV) for p in ([1, 2], [3, 4])]
+    w = bf16(rng, N, K)
+
+    def outputs():
+        groups = (torch.empty(N, K // 2, dtype=torch.uint8, device=T.DEV), torch.empty(N, 5, device=T.DEV), torch.empty(N, 5, device=T.DEV))
+        return dict(r_out=torch.empty_like(r), y=torch.empty_like(x), xq=T.out_codes(8, M, Kpad), s_x=torch.empty(1, device=T.DEV), xq1=T.out_codes(8, 1, Kpad),
+                    s1=torch.empty(1, device=T.DEV), p=torch.empty(M, N, device=T.DEV), p1=torch.empty(1, N, device=T.DEV), groups=groups)
+
+    ws = [T.norm_workspace(M, K, Kpad) for _ in range(2)]
+
+    def step(o):
+        fq.fq_rms_norm_quant(x, g, EPS, R=r, R_out=o["r_out"], Y=o["y"], src_idx=src, rep=rep, Xq_out=o["xq"], s_x_out=o["s_x"], workspace=ws[0])
+        fq.fq_rms_norm_quant(one, g, EPS, src_idx=src, rep=rep, Xq_out=o["xq1"], s_x_out=o["s1"], workspace=ws[1])
+        fq.fq_linear_group_i4(o["y"], wq, s, 128, o["p"], B=b)
+        fq.fq_linear_group_i4(one, wq, s, 128, o["p1"], B=b)
+        fq.fq_group_weights_i4(w, 128, o["groups"][0], o["groups"][1], B_out=o["groups"][2])
+        fq.fq_kv_copy_pages(*caches, *pages)
+
+    flat = lambda o: [v.clone() for k, v in o.items() if k != "groups"] + [v.clone() for v in o["groups"]]  # noqa: E731
+    mine, eager = outputs(), outputs()
+    step(mine)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(mine)
+    for i in range(4):
+        for t in (x, r, one, w):
+            t.copy_(bf16(rng, *t.shape))
+        caches[0][1] = i
+        pages[0][0] = 1 if i % 2 else 5
+        graph.replay()
+        got, copied = flat(mine), [c.clone() for c in caches]
+        caches[0][3:5] = 9
+        step(eager)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(got, flat(eager))), i
+        assert all(torch.equal(a, c) for a, c in zip(copied, caches)), i
+
+
+def test_on_other_streams_at_once():
+    """Each call goes to the stream it is given, or to the current one; two norms at once with a workspace each."""
+    rng = np.random.default_rng(4)
+    M, K = 3000, 2048
+    src, rep, _, Kpad = T.plan(rng, K, 0.1)
+    src, rep = (torch.from_numpy(a).to(T.DEV) for a in (src, rep))
+    g = bf16(rng, K)
+    xs = [bf16(rng, M, K) for _ in range(2)]
+    wq, s = torch.randint(0, 256, (512, K // 2), dtype=torch.uint8, device=T.DEV), torch.rand(512, 16, device=T.DEV)
+
+    def run(x, stream=None):
+        out = T.out_codes(8, M, Kpad), torch.empty(1, device=T.DEV), torch.empty(M, 512, device=T.DEV)
+        fq.fq_rms_norm_quant(x, g, EPS, src_idx=src, rep=rep, Xq_out=out[0], s_x_out=out[1], workspace=T.norm_workspace(M, K, Kpad), stream=stream)
+        fq.fq_linear_group_i4(x, wq, s, 128, out[2], stream=stream)
+        return out
+
+    want = [run(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        got = [run(xs[0], streams[0])]
+        streams[1].wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(streams[1]):
+            got.append(run(xs[1]))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
+
+
+def test_offsets_beyond_4_gib():
+    """Rows of activations, weights and outputs that 32-bit byte offsets do not reach."""
+    K, ld, M = 64, 1 << 20, 2100                       # 4.4 GB apart
+    X = torch.zeros(M, ld, dtype=torch.bfloat16, device=T.DEV)[:, :K]
+    X[0], X[-1] = 1, 2
+    g = torch.ones(K, device=T.DEV)
+    Y = torch.zeros(M, ld, dtype=torch.bfloat16, device=T.DEV)[:, :K]
+    fq.fq_rms_norm_quant(X, g, EPS, Y=Y)
+    assert (Y[0] == 1).all() and (Y[-1] == 1).all() and not Y[1:-1].any()
+    wq, s = torch.full((256, K // 2), 0x11, dtype=torch.uint8, device=T.DEV), torch.ones(256, 1, device=T.DEV)
+    P = torch.zeros(M, ld, dtype=torch.bfloat16, device=T.DEV)[:, :256]
+    fq.fq_linear_group_i4(X, wq, s, 64, P)
+    assert (P[0] == 64).all() and (P[-1] == 128).all() and not P[1:-1].any()
+    del X, Y, P
+    N, K = 70000, 131072                               # 4.6 GB of codes
+    wq = torch.zeros(N, K // 2, dtype=torch.uint8, device=T.DEV)
+    wq[-1], wq[3] = 0x22, 0x11
+    s = torch.ones(N, K // 128, device=T.DEV)
+    for M in (1, 20, 100):
+        X, y = torch.zeros(M, K, dtype=torch.bfloat16, device=T.DEV), torch.empty(M, N, device=T.DEV)
+        X[-1, -1] = 1
+        fq.fq_linear_group_i4(X, wq, s, 128, y)
+        assert y[-1, -1] == 2 and y[-1, 3] == 1 and y.sum() == 3
+
+
+def test_binding_refusals():
+    x, g = torch.zeros(4, 64, device=T.DEV), torch.ones(64, device=T.DEV)
+    idx = torch.arange(64, dtype=torch.int32, device=T.DEV)
+    q, s = T.out_codes(8, 4, 64), torch.zeros(1, device=T.DEV)
+    norm = lambda **k: fq.fq_rms_norm_quant(**{**dict(X=x, gamma=g, eps=EPS, src_idx=idx, rep=idx, Xq_out=q, s_x_out=s, absmax_in=s), **k})  # noqa: E731
+    for k in (dict(X=x.cpu()), dict(X=x[0]), dict(X=x.t()), dict(gamma=g[:32]), dict(gamma=g.cpu()), dict(R=x), dict(R=x, R_out=x.half()), dict(R=x[:2], R_out=x[:2]),
+              dict(Y=x[:, :32]), dict(src_idx=idx.long()), dict(rep=idx[:32]), dict(rep=None), dict(s_x_out=None), dict(Xq_out=q[:3]), dict(Xq_out=q.float()),
+              dict(absmax_in=s.double()), dict(absmax_in=None, workspace=torch.zeros(1000, dtype=torch.uint8))):
+        with pytest.raises(ValueError):
+            norm(**k)
+    with pytest.raises(fq.FqError, match="workspace"):
+        norm(absmax_in=None)
+    with pytest.raises(fq.FqError, match="16 bytes"):
+        norm(X=torch.zeros(4, 65, device=T.DEV)[:, :64])
+    w, codes, scales = torch.zeros(8, 64, device=T.DEV), torch.zeros(8, 32, dtype=torch.uint8, device=T.DEV), torch.zeros(8, 2, device=T.DEV)
+    for args in ((w.cpu(), 32, codes, scales), (w, 32, codes[:, :16], scales), (w, 32, codes.to(torch.int8), scales), (w, 64, codes, scales), (w, 0, codes, scales)):
+        with pytest.raises(ValueError):
+            fq.fq_group_weights_i4(*args)
+    h, y = torch.zeros(3, 64, dtype=torch.float16, device=T.DEV), torch.zeros(3, 8, device=T.DEV)
+    for args, k in (((h.cpu(), codes, scales, 32, y), {}), ((h, codes, scales, 32, y[:2]), {}), ((h, codes, scales, 64, y), {}), ((h, codes[:, :16], scales, 32, y), {}),
+                    ((h, codes, scales, 32, y), dict(B=scales.half())), ((h, codes, scales, 32, y), dict(bias=y[0].half()))):
+        with pytest.raises(ValueError):
+            fq.fq_linear_group_i4(*args, **k)
+    with pytest.raises(fq.FqError, match="DTYPE"):
+        fq.fq_linear_group_i4(h.float(), codes, scales, 32, y)
+    k, sc = torch.zeros(3, 1, 64, 64, dtype=torch.int8, device=T.DEV), torch.zeros(3, 1, device=T.DEV)
+    i = torch.zeros(2, dtype=torch.int32, device=T.DEV)
+    for args in ((k[0], k, sc, sc, i, i), (k, k[:2], sc, sc, i, i), (k, k, sc[:2], sc, i, i), (k, k, sc, sc, i.long(), i), (k, k, sc, sc, i, i[:1]), (k, k, sc, sc, i.cpu(), i)):
+        with pytest.raises(ValueError):
+            fq.fq_kv_copy_pages(*args)

@@ -57,7 +57,7 @@ def test_weights_refusals(args, code):
     (dict(X=None), NULL), (dict(X=P + 8), ALIGN), (dict(x_dtype=fq.FQ_F32), DTYPE), (dict(x_dtype=fq.FQ_I32), DTYPE), (dict(M=0), SHAPE), (dict(K=16, ldx=16), SHAPE),
     (dict(K=72, ldx=72), SHAPE), (dict(ldx=56), SHAPE), (dict(ldx=68), SHAPE), (dict(Wq=None), NULL), (dict(Wq=P + 8), ALIGN), (dict(S=None), NULL), (dict(S=P + 2), ALIGN),
     (dict(B=P + 2), ALIGN), (dict(s_dtype=9), DTYPE), (dict(group=96), SHAPE), (dict(N=0), SHAPE), (dict(bias=P + 4), ALIGN), (dict(Y=None), NULL), (dict(Y=P + 4), ALIGN),
-    (dict(y_dtype=fq.FQ_I32), DTYPE), (dict(ldy=7), SHAPE), (dict(M=2**31 - 1, N=2**31 - 1, ldy=2**31 - 1), RANGE)])
+    (dict(y_dtype=fq.FQ_I32), DTYPE), (dict(ldy=7), SHAPE), (dict(ldx=2**24 + 8), RANGE), (dict(K=2**24 + 32, ldx=2**25), RANGE), (dict(M=2**31 - 1, N=2**31 - 1, ldy=2**31 - 1), RANGE)])
 def test_product_refusals(args, code):
     assert product(**args) == code and fq.lib().fq_last_error_string()
 
