@@ -214,26 +214,33 @@ template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP = 32> int lau
 
 }  // namespace
 
-// Tiles by how many there are.  us (bf16, groups of 128), the taken one first:
-//   64 x 256   2048 rows, 11008 x 4096: 229; 64 x 128, waves two by two along both: 331; 64 x 128, waves side by side 351
-//   64 x 128   512 rows, 4096 x 4096: 33; 64 x 256 56; 64 x 32 49.  256 rows, 11008 x 4096, has 172 tiles of 64 x 256: 57, 64 x 128 62
-//   64 x 32    128 rows, 4096 x 4096: 17; 64 x 64 24; 64 x 256 56
-//   48 rows, 4096 x 11008: 30 (16 columns 31, 64 columns 53); 24 rows, 4096 x 11008: 18 (32 columns 25), 11008 x 4096: 21 (16 columns 22)
-//   16 rows, 4096 x 11008: 13 (32 columns 19), 22016 x 8192: 46 (16 columns 54)
+// Tiles by how many there are: large ones where they fill the CUs; else the smallest of which each CU gets one at most, as a workgroup's time goes by
+// its stages (1.1 us each, however far ahead copies are issued) more than by what is in them.  us (bf16, groups of 128 or 64), the taken one first:
+//   64 x 256   2048 rows, 11008 x 4096: 229; 64 x 128, waves two by two along both: 331; 64 x 128, waves side by side 351; 128 x 256 260
+//   64 x 128   512 rows, 4096 x 4096: 33; 64 x 256 56.  128 rows, 11008 x 4096: 32; 32 x 64 41
+//   32 x 64    128 rows, 4096 x 4096: 16; 64 x 32 16; 64 x 128 31.  64 rows, 22016 x 8192: 82; 64 x 64 97; 32 x 32 111
+//   32 x 32    64 rows, 4096 x 4096: 11; 32 x 64 15; 32 x 16 15.  48 rows, 4096 x 11008: 26; 48 x 32 30; 32 x 16 31
+//   32 x 16    24 rows, 4096 x 11008: 18; 32 x 32 25.  64 rows, 1024 x 4096: 8; 32 x 32 11
+//   48 x 64    48 rows, 11008 x 4096: 18; 32 x 64 28
+//   16 x 16    16 rows, 4096 x 11008: 13; 16 x 32 17.  16 x 32   16 rows, 22016 x 8192: 40; 16 x 16 56
 // With groups of 32 columns there is a scale to apply after every matrix product, and tiles of 256 columns lose (2048 rows, 11008 x 4096: 345; 256 columns 512).
 template <int XT> int launch_group_tile(const GroupProduct& product, int group, hipStream_t stream)
 {
     GroupProduct a = product;
     a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
-    const long long cus = compute_units(), rows = (a.M + 63) / 64;
-    if (a.M <= 16) return a.N >= 8192 ? launch<XT, 1, 2, 1, 8, 2>(a, stream) : launch<XT, 1, 1, 1, 8, 3>(a, stream);
-    if (a.M <= 32) return a.N >= 8192 ? launch<XT, 2, 1, 2, 4, 3>(a, stream) : launch<XT, 2, 1, 1, 8, 2>(a, stream);
-    if (a.M <= 48) return launch<XT, 3, 1, 2, 4, 2>(a, stream);
-    const bool many = 3 * rows * ((a.N + 255) / 256) >= 2 * cus, some = 4 * rows * ((a.N + 127) / 128) >= 3 * cus;
-    if (!some) return launch<XT, 4, 1, 2, 4, 2>(a, stream);
-    if (group == 32) return launch<XT, 4, 2, 4, 1, 2>(a, stream);
-    if (group == 64) return many ? launch<XT, 4, 4, 4, 1, 2, 64>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 64>(a, stream);
-    return many ? launch<XT, 4, 4, 4, 1, 2, 128>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 128>(a, stream);
+    const long long cus = compute_units(), M = a.M, N = a.N;
+    auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+    if (M <= 16) return tiles(16, 16) <= cus ? launch<XT, 1, 1, 1, 8, 3>(a, stream) : launch<XT, 1, 1, 2, 8, 2>(a, stream);
+    if (M > 64 && 3 * tiles(64, 128) >= 2 * cus) {
+        const bool many = 3 * tiles(64, 256) >= 2 * cus;
+        if (group == 32) return launch<XT, 4, 2, 4, 1, 2>(a, stream);
+        if (group == 64) return many ? launch<XT, 4, 4, 4, 1, 2, 64>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 64>(a, stream);
+        return many ? launch<XT, 4, 4, 4, 1, 2, 128>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 128>(a, stream);
+    }
+    if (tiles(32, 16) <= cus) return launch<XT, 2, 1, 1, 8, 2>(a, stream);
+    if (tiles(32, 32) <= cus) return launch<XT, 2, 1, 2, 4, 3>(a, stream);
+    if (M > 32 && M <= 48 && tiles(32, 64) > cus) return launch<XT, 3, 1, 4, 4, 2>(a, stream);
+    return launch<XT, 2, 1, 4, 4, 2>(a, stream);
 }
 #if FQ_GROUP_TYPE == 1
 template int launch_group_tile<FQ_F16>(const GroupProduct&, int, hipStream_t);
