@@ -101,16 +101,16 @@ __device__ __forceinline__ void store_packed(int bits, const v4u& q, uint8_t* ou
 __device__ __forceinline__ void store_eight(int bits, const float (&y)[8], const float* m, uint8_t* out, int Kpad, int row, int g)
 {
     if (bits == 8) {
-        *reinterpret_cast<v2u*>(out + (size_t)row * Kpad + 8 * g) = v2u{quantize4<8>(y, m), quantize4<8>(y + 4, m + 4)};
+        *reinterpret_cast<v2u*>(out + (size_t)row * Kpad + (uint32_t)(8 * g)) = v2u{quantize4<8>(y, m), quantize4<8>(y + 4, m + 4)};
     } else {
         const uint32_t a = quantize4<4>(y, m), b = quantize4<4>(y + 4, m + 4);
         const uint32_t c = (a & 0x000f000fu) | ((a >> 4) & 0x00f000f0u), d = (b & 0x000f000fu) | ((b >> 4) & 0x00f000f0u);      // bytes 0 and 2: two values each
-        *reinterpret_cast<uint32_t*>(out + (size_t)row * (Kpad / 2) + 4 * g) = bytes_of(d, c, 0x06040200u);
+        *reinterpret_cast<uint32_t*>(out + (size_t)row * (Kpad / 2) + (uint32_t)(4 * g)) = bytes_of(d, c, 0x06040200u);
     }
 }
 
-// A thread has GPT times 8 channels, 8 (tid + k threads) on: neighbouring threads read neighbouring pieces.  KEEP: gamma and the multipliers of the channels' own
-// slots stay in registers.
+// A thread has GPT times 8 channels, 8 (tid + k threads) on: neighbouring threads read neighbouring pieces.  KEEP: gamma stays in registers, the multipliers of the
+// channels' own slots in LDS (in registers, too, the kernel spilled at the 128 that four waves a SIMD leave it).
 template <int XT, int RT, int PASS, int GPT, bool RAGGED>
 __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
 {
@@ -125,6 +125,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     const int zero_at = 8 * G;
     float* row_y = table + TABLE;                                   // the row; behind it a zero
     uint8_t* row_q = reinterpret_cast<uint8_t*>(row_y + row_places(K));     // codes of 16 slots a thread
+    float* row_m = reinterpret_cast<float*>(row_q + 16 * threads);          // KEEP: multipliers of the slots before `base`
     const double per_channel = 1.0 / (double)K;
 
     Raw<XT> x[GPT];
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     // ---- the map: do the first slots lie at their channels' own places?  The slots from `base` on are the others.  (E3M2 codes are packed by sixteens: all.) ----
     const int whole = KEEP && a.bits != FQ_BITS_I4_E3M2 ? min(K & ~15, Kpad) : 0;
     int own_rep[KEEP ? GPT : 1][8];
-    bool apart = false, far = false;
+    bool apart = false, far = false;     // far: copy counts that the table does not have
     if constexpr (KEEP) {
 #pragma unroll
         for (int k = 0; k < GPT; ++k) {
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
         }
     }
     const int base = __syncthreads_or(apart) ? 0 : whole;
-    far = __syncthreads_or(far);                                    // copy counts that the table does not have
+    if (PASS != FIND_SCALE) far = __syncthreads_or(far);
     const bool others = base < Kpad;
     auto own = [&](int k) { return 8 * (tid + k * threads) < base; };
     // In search of the bound a slot counts nothing that another slot of the same channel, at its own place and with no more copies, has counted.
@@ -272,7 +273,12 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
             bound = *a.absmax;
             if (!(bound >= 0.0f) || bound > 3.0e38f) bound = 0.0f;     // negative / NaN / Inf static bound: treated as 0
         } else {
-            for (int i = tid; i < a.candidates; i += threads) bound = fmaxf(bound, a.found[i]);
+#pragma unroll 8
+            for (int i = tid; i < a.candidates / 4; i += threads) {
+                const v4f c = reinterpret_cast<const v4f*>(a.found)[i];
+                bound = fmaxf(bound, fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3])));
+            }
+            if (tid < a.candidates % 4) bound = fmaxf(bound, a.found[a.candidates / 4 * 4 + tid]);
             bound = largest_of(bound, best_of);
         }
     }
@@ -281,24 +287,28 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     const double qmax = a.bits == 8 ? 127.0 : 7.0;
     auto formed = [&](int n) -> float { return n > 0 && bound != 0.0f ? (float)(qmax / ((double)n * (double)bound)) : 0.0f; };
     auto multiplier = [&](int n) -> float { return (unsigned)n < TABLE ? table[n] : formed(n); };
-    float own_m[KEEP ? GPT : 1][8], other_m[KEPT];
+    float other_m[KEPT];
     int other_at[KEPT];                  // the first of the other slots that this thread works on: places in the row, multipliers
     if (Kpad) {
         for (int n = tid; n < TABLE; n += threads) table[n] = formed(n);
         if (blockIdx.x == 0 && tid == 0) *a.s_x = bound == 0.0f ? 1.0f : (float)((double)bound / qmax);
         __syncthreads();
         if constexpr (KEEP) {
-            if (far) {                   // each formed once, by whichever thread
-                for (int p = tid; p < base; p += threads) row_y[p] = multiplier(a.rep[p]);
+            if (far) {
+                for (int p = tid; p < base; p += threads) row_m[p] = multiplier(a.rep[p]);
                 __syncthreads();
+            } else {                     // a thread's own, which it alone reads
+#pragma unroll
+                for (int k = 0; k < GPT; ++k)
+                    if (own(k)) {
+                        float m[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) m[i] = table[max(own_rep[k][i], 0)];
+                        v4f* to = reinterpret_cast<v4f*>(row_m + 8 * (tid + k * threads));
+                        to[0] = v4f{m[0], m[1], m[2], m[3]};
+                        to[1] = v4f{m[4], m[5], m[6], m[7]};
+                    }
             }
-#pragma unroll
-            for (int k = 0; k < GPT; ++k)
-                if (own(k)) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) own_m[k][i] = far ? row_y[8 * (tid + k * threads) + i] : table[max(own_rep[k][i], 0)];
-                }
-            if (far) __syncthreads();
         }
 #pragma unroll
         for (int i = 0; i < KEPT; ++i) {
@@ -326,7 +336,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
             if (a.Y) store_any<RAGGED>(y[k], row_of(a.Y, a.ldy, a.y_dtype == FQ_F32 ? 4 : 2, row), a.y_dtype, g, K);
             if (others) to_lds(g, y[k]);
             if constexpr (KEEP) {
-                if (own(k)) store_eight(a.bits, y[k], own_m[k], a.out, Kpad, row, g);
+                if (own(k)) store_eight(a.bits, y[k], row_m + 8 * g, a.out, Kpad, row, g);
             }
         }
         strip_barrier();                 // the row lies in LDS, and the sum's parts are read no more
@@ -377,7 +387,7 @@ template <int XT, int RT, int PASS> int launch(const Norm& a, int wgs, hipStream
 {
     const int threads = norm_threads(a.K);
     const bool two = a.K <= 2 * 8 * threads;
-    const int smem = 16 * 8 + (16 + FEW_ROWS + TABLE + row_places(a.K)) * 4 + 16 * threads;
+    const int smem = 16 * 8 + (16 + FEW_ROWS + TABLE + row_places(a.K) + (two ? row_places(a.K) : 0)) * 4 + 16 * threads;
     const bool ragged = a.K % 8 != 0;
     auto kern = ragged ? (two ? rms_norm_kernel<XT, RT, PASS, 2, true> : rms_norm_kernel<XT, RT, PASS, 4, true>)
                        : (two ? rms_norm_kernel<XT, RT, PASS, 2, false> : rms_norm_kernel<XT, RT, PASS, 4, false>);
