@@ -156,6 +156,16 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
 
     // ---- the map: do the first slots lie at their channels' own places?  The slots from `base` on are the others.  (E3M2 codes are packed by sixteens: all.) ----
     const int whole = KEEP && a.bits != FQ_BITS_I4_E3M2 ? min(K & ~15, Kpad) : 0;
+    int other_src[KEPT], other_rep[KEPT];      // the first of the others that this thread works on, if they begin at `whole`: on their way while the row is
+    auto load_others = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) {
+            const int p = base + i * threads + tid;
+            other_src[i] = p < Kpad ? a.src[p] : -1;
+            other_rep[i] = p < Kpad ? a.rep[p] : 0;
+        }
+    };
+    load_others(whole);
     int own_rep[KEEP ? GPT : 1][8];
     bool apart = false, far = false;     // far: copy counts that the table does not have
     if constexpr (KEEP) {
@@ -176,16 +186,21 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     }
     const int base = __syncthreads_or(apart) ? 0 : whole;
     if (PASS != FIND_SCALE) far = __syncthreads_or(far);
+    if (base != whole) load_others(base);
     const bool others = base < Kpad;
     auto own = [&](int k) { return 8 * (tid + k * threads) < base; };
     // In search of the bound a slot counts nothing that another slot of the same channel, at its own place and with no more copies, has counted.
     bool to_count = false;
     auto used = [&](int src, int rep) { return (unsigned)src < (unsigned)K && rep > 0; };
     if (FIND) {
-        for (int p = base + tid; p < Kpad; p += threads) {
-            const int j = a.src[p], n = a.rep[p];
-            if (used(j, n) && !(j < base && a.rep[j] > 0 && a.rep[j] <= n)) to_count = true;
-        }
+        auto counts = [&](int j, int n) {
+            if (!used(j, n)) return false;
+            const int own = j < base ? a.rep[j] : 0;
+            return own <= 0 || own > n;
+        };
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i) to_count |= counts(other_src[i], other_rep[i]);
+        for (int p = base + KEPT * threads + tid; p < Kpad; p += threads) to_count |= counts(a.src[p], a.rep[p]);
         to_count = __syncthreads_or(to_count);
     }
     if (tid == 0) row_y[zero_at] = 0.0f;
@@ -312,16 +327,9 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
         }
 #pragma unroll
         for (int i = 0; i < KEPT; ++i) {
-            const int p = base + i * threads + tid;
-            other_at[i] = zero_at;
-            other_m[i] = 0.0f;
-            if (p < Kpad) {
-                const int j = a.src[p], n = a.rep[p];
-                if (used(j, n)) {
-                    other_at[i] = j;
-                    other_m[i] = multiplier(n);
-                }
-            }
+            const bool is = used(other_src[i], other_rep[i]);
+            other_at[i] = is ? other_src[i] : zero_at;
+            other_m[i] = is ? multiplier(other_rep[i]) : 0.0f;
         }
     }
 
