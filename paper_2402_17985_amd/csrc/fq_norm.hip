@@ -7,7 +7,11 @@
 // Slots that do not lie at their channel's own place (copies, padding, other maps) are worked on one by one, neighbouring threads neighbouring slots, from
 // the row in LDS; their codes meet there by sixteens.
 // A dynamic scale is a maximum over the whole tensor: a first pass stores h, every row's t and each workgroup's candidate, a
-// second one forms y again and quantizes it.  For a few rows one workgroup does both.
+// second one forms y again and quantizes it.  One workgroup does both for a row or two.
+// Bound by bytes: bf16 with a residual, static, 8192 x 4096 55 us (4.4 TB/s read and written), 8192 x 8192 102 (4.8), fp32 8192 x 4096 92 (4.8): the rate of
+// a copy.  Dynamic 8192 x 4096: 45 and 32 us in the two kernels, 4.4 and 3.3 TB/s.  4099 x 5003 with an fp32 residual, bf16 out: 98 (2.9 TB/s).
+// One row of 4096, dynamic: 10 us, 48 x 5120 static 7: latency (the map, the row, two or three reductions over the workgroup).
+// With 16 channels in a row to a thread, two loads of 32-byte strides, the address unit worked lane by lane: 8192 x 4096 94 us instead of 72.
 #include <algorithm>
 #include <atomic>
 
@@ -20,7 +24,7 @@ namespace {
 enum { ONE_PASS, FIND_SCALE, WITH_SCALE, BOTH };
 constexpr int TABLE = 256;        // multipliers m(n) kept for n < 256
 constexpr int MAX_WGS = 4096;     // and candidates
-constexpr int FEW_ROWS = 4;       // that one workgroup takes alone
+constexpr int FEW_ROWS = 2;       // that one workgroup takes alone
 constexpr int KEPT = 4;           // slots away from their channel's place that a thread keeps in registers
 
 // floats of LDS for a row of K, and the zero behind it
@@ -446,7 +450,8 @@ int launch_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, con
     a.t = static_cast<float*>(workspace);
     a.found = a.t + round_up((size_t)M * 4, 16) / 4;
     a.candidates = wgs;
-    if (M <= FEW_ROWS) return launch_types<BOTH>(a, x_dtype, rt, 1, stream);
+    // us, one workgroup / two launches: 1 x 4096 10 / 13, 2 x 4096 12.7 / 13, 3 x 4096 15.5 / 13, 2 x 8192 15.7 / 15.3, 1 x 16384 17 / 19.7
+    if (M <= (K <= 4096 ? FEW_ROWS : 1)) return launch_types<BOTH>(a, x_dtype, rt, 1, stream);
     if (int rc = launch_types<FIND_SCALE>(a, x_dtype, rt, wgs, stream)) return rc;
     if (R) {        // the second pass reads what the first one stored
         a.X = R_out;
