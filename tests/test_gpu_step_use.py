@@ -51,10 +51,10 @@ def test_group_linear(group, offsets):
         fq.FqGroupLinear(W, 100)
 
 
-def layer_step(rng, cache, weights, x, new):
+def layer_step(cache, weights, x, new):
     """One decoder layer's attention half on the rows x (the residual stream, updated in place): what each sequence's rows become."""
-    qkv, out, gamma, hq, hkv, dim = weights
-    rows = qkv.forward_norm(torch.zeros_like(x), gamma, EPS, R=x)
+    qkv, out, gamma, bound, hq, hkv, dim = weights
+    rows = qkv.forward_norm(torch.zeros_like(x), gamma, EPS, R=x, absmax_in=bound)
     q, k, v = (t.unflatten(1, (-1, dim)) for t in rows.split([hq * dim, hkv * dim, hkv * dim], 1))
     cache.append(q, k, v, new)
     y = cache.attend(q, new, dim**-0.5)
@@ -67,17 +67,15 @@ def test_a_conversation_continued_in_several_ways():
     rng = np.random.default_rng(0)
     hidden, hq, hkv, dim, page = 256, 4, 2, 64, 64
     qkv = fq.FqLinear(bf16(rng, (hq + 2 * hkv) * dim, hidden, scale=0.06), np.full(hidden, 4.0, np.float32), 4.5, 8)
-    weights = qkv, fq.FqGroupLinear(bf16(rng, hidden, hq * dim, scale=0.06), 64), bf16(rng, hidden), hq, hkv, dim
     bound = torch.tensor([6.0], device=T.DEV)      # one bound for all calls: a dynamic one would go by the other sequences
-    forward = qkv.forward_norm
-    qkv.forward_norm = lambda *a, **k: forward(*a, **k, absmax_in=bound)
+    weights = qkv, fq.FqGroupLinear(bf16(rng, hidden, hq * dim, scale=0.06), 64), bf16(rng, hidden), bound, hq, hkv, dim
     forked, apart = (fq.FqKvCache(24, 3, 320, hkv, dim, page) for _ in range(2))
     for c in (forked, apart):
         for t in (c.k_cache, c.v_cache):
             t.fill_(77)
     prompt = bf16(rng, 150, hidden)
-    one = layer_step(rng, forked, weights, prompt.clone(), [150, 0, 0])
-    three = layer_step(rng, apart, weights, prompt.repeat(3, 1), [150, 150, 150])
+    one = layer_step(forked, weights, prompt.clone(), [150, 0, 0])
+    three = layer_step(apart, weights, prompt.repeat(3, 1), [150, 150, 150])
     assert torch.equal(one.repeat(3, 1), three)
     forked.fork(0, [1, 2])
     used = 24 - len(forked._free)
@@ -86,14 +84,14 @@ def test_a_conversation_continued_in_several_ways():
         x = bf16(rng, sum(new), hidden)
         if i == 3:
             forked.lengths[1] = apart.lengths[1] = 100             # rejected drafts, back into what was shared
-        a, b = (layer_step(rng, c, weights, x.clone(), new) for c in (forked, apart))
+        a, b = (layer_step(c, weights, x.clone(), new) for c in (forked, apart))
         assert torch.equal(a, b), i
         if i == 2:
             live = forked.compact()
             assert live == len(set(sum(forked.held, []))) == max(max(h) for h in forked.held) + 1
     forked.release(0)
     x = bf16(rng, 2, hidden)
-    a, b = (layer_step(rng, c, weights, x.clone(), [0, 1, 1]) for c in (forked, apart))
+    a, b = (layer_step(c, weights, x.clone(), [0, 1, 1]) for c in (forked, apart))
     assert torch.equal(a, b)
 
 
