@@ -65,9 +65,9 @@ def test_weights_far_from_one(s_dtype, offsets):
     check_weights(W, "f32", 64, s_dtype, offsets)
 
 
-def product(M, N, K, group, x="bf16", s="bf16", offsets=False, bias=False, y="bf16", seed=0, extra=0, mean=0.0, ldy=0):
+def product(M, N, K, group, x="bf16", s="bf16", offsets=False, bias=False, y="bf16", seed=0, extra=0, mean=0.0, ldy=0, scale=1.0):
     rng = np.random.default_rng(seed)
-    X = S.round_to(T.values(rng, (M, K), x) + np.float32(mean), x)
+    X = S.round_to(T.values(rng, (M, K), x, scale) + np.float32(mean), x)
     groups = -(-K // group)
     q = rng.integers(-8, 8, (N, K)).astype(np.int8)
     sc = S.round_to(np.exp(0.5 * rng.standard_normal((N, groups))).astype(np.float32) / np.float32(4.6 * np.sqrt(K)), s)
@@ -121,6 +121,31 @@ def test_activations_of_one_sign(x):
     """What bf16 codes carry too much, 24 times the sum of the activations, is then many times the result."""
     for M in (1, 40, 150):
         product(M, 64, 2048, 128, x, "f32", y="f32", mean=4.0)
+
+
+@pytest.mark.parametrize("offsets", [False, True])
+@pytest.mark.parametrize("x,scale", [("f16", 2.0**-18), ("f16", 2.0**12), ("bf16", 2.0**-100), ("bf16", 2.0**100)])
+def test_magnitudes(x, scale, offsets):
+    """Among them activations that are subnormal in fp16: most of the first case's."""
+    for M in (1, 12, 40, 150):
+        product(M, 48, 1024, 64, x, "f32", offsets, y="f32", scale=scale, seed=M)
+
+
+@pytest.mark.parametrize("x,dt", [("f16", torch.float16), ("bf16", torch.bfloat16)])
+def test_few_and_many_rows_agree(x, dt):
+    """The same rows through the kernels for one token, a few and many: the sums differ by their order only."""
+    X = torch.randn(300, 1184, device=T.DEV).to(dt)
+    wq = torch.randint(0, 256, (530, 592), dtype=torch.uint8, device=T.DEV)
+    s, b = torch.rand(530, 19, device=T.DEV), torch.randn(530, 19, device=T.DEV)
+    out = []
+    for rows in (1, 7, 16, 20, 45, 60, 300):
+        y = torch.empty(rows, 530, device=T.DEV)
+        fq.fq_linear_group_i4(X[:rows], wq, s, 64, y, B=b)
+        out.append(y)
+    size = X[:1].float().abs() @ (8 * s + b.abs()).repeat_interleave(64, 1)[:, :1184].t() * 4
+    for y in out[:-1]:
+        assert ((y[0] - out[-1][0]).abs() <= 300 * 2.0**-24 * size[0]).all()
+        assert torch.allclose(y, out[-1][:len(y)], rtol=1e-3, atol=1e-2 * float(size.mean()))
 
 
 def test_each_code_at_each_place():
