@@ -369,7 +369,7 @@ int fq_linear_fused_a_i8(const void* X, int x_dtype, int M, int K, int ldx, cons
  *
  * X [M, K], R, R_out [M, K], Y [M, K]: F32 / F16 / BF16 each, 16-byte aligned, row strides of a multiple of 16 bytes (R_out has R's type).
  *   Elements between K and a stride are neither read nor written.  gamma [K], g_dtype F32 / F16 / BF16, dense.  eps > 0, finite.
- *   K <= 32768; map, Kpad and bits as for fq_flatten_quant_act (src_idx, rep unused without Xq_out).
+ *   K <= 32768, M < 2^31 - 4096; map, Kpad and bits as for fq_flatten_quant_act (src_idx, rep unused without Xq_out).
  *   Sums X + R must be finite in r_dtype, and a row's root mean square below 2^126 (t_i is subnormal beyond).
  * R_out may be R or X itself, Y may be X or R itself (same address, type and stride; Y and R_out apart); else outputs must not overlap
  *   inputs or each other.
@@ -388,7 +388,7 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  *
  *   w[n,k] = S[n, k / group] * q[n,k] + B[n, k / group]        q in [-8, 7];  B NULL: no offsets
  *   Wq  [N, K / 2] bytes, two's-complement nibbles, even column in the low one; rows dense.  K a multiple of 32, at most 2^24.
- *   S, B  [N, ceil(K / group)], dense, s_dtype F32 / F16 / BF16; group 32, 64 or 128; a row's last group may be a short one.
+ *   S, B  [N, ceil(K / group)], dense, finite, s_dtype F32 / F16 / BF16; group 32, 64 or 128; a row's last group may be a short one.
  *
  * fq_group_weights_i4 — offline: the weights' codes, scales and offsets.  W [N, K] F32 / F16 / BF16, row stride ldw (a multiple of 16 bytes).
  *   Over a row's group, without offsets (B_out == NULL):  s = fl32(max|w| / 7);

@@ -1,4 +1,4 @@
-// What the kernels of fq_linear_group_i4 share (GPU code only; everything has internal linkage).
+// What the kernels of fq_linear_group_i4 share (GPU code only).
 #pragma once
 #include "fq_internal.h"
 
@@ -49,11 +49,7 @@ struct GroupProduct {
         }
         return r;
     }
-    // a single one, and its value
-    __device__ __forceinline__ uint32_t one_scale(const void* base, size_t at) const
-    {
-        return s_dtype == FQ_F32 ? static_cast<const uint32_t*>(base)[at] : static_cast<const uint16_t*>(base)[at];
-    }
+    // the value of a single one
     __device__ __forceinline__ float value(uint32_t v) const
     {
         return s_dtype == FQ_F32 ? __uint_as_float(v) : s_dtype == FQ_BF16 ? __uint_as_float(v << 16) : (float)__builtin_bit_cast(_Float16, (uint16_t)v);
@@ -102,7 +98,7 @@ namespace {
 template <int XT> struct GroupMma;
 template <> struct GroupMma<FQ_BF16> {
     typedef v8bf v8;
-    static constexpr bool SURPLUS = true;      // widen() gives q + 24, exactly; less() is the activations times -24
+    static constexpr bool SURPLUS = true;      // widen() gives q + 24, exactly; a product with all(true), -24 everywhere, takes the surplus out
     // A nibble in the top four mantissa bits of 16 makes 16 + u.  The multiplication brings a byte's low nibble to bits 3 .. 6 and its high one to
     // bits 19 .. 22; it takes the byte as its operand, so two codes cost two instructions (shifts, masks and a subtraction in fp32: seven).
     static __device__ __forceinline__ v8 widen(uint32_t w)
@@ -113,7 +109,6 @@ template <> struct GroupMma<FQ_BF16> {
         for (int p = 0; p < 4; ++p) r[p] = ((((w >> (8 * p)) & 0xffu) * 0x8008u) & MASK) ^ BASE;
         return __builtin_bit_cast(v8, r);
     }
-    static __device__ __forceinline__ v8 none() { return __builtin_bit_cast(v8, v4u{0, 0, 0, 0}); }
     static __device__ __forceinline__ v8 all(bool less) { const uint32_t v = less ? 0xc1c0c1c0u : 0x3f803f80u; return __builtin_bit_cast(v8, v4u{v, v, v, v}); }
     static __device__ __forceinline__ v4f mul(v8 x, v8 w, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0); }
 };
@@ -131,7 +126,6 @@ template <> struct GroupMma<FQ_F16> {
         }
         return __builtin_bit_cast(v8, r);
     }
-    static __device__ __forceinline__ v8 none() { return __builtin_bit_cast(v8, v4u{0, 0, 0, 0}); }
     static __device__ __forceinline__ v8 all(bool) { return __builtin_bit_cast(v8, v4u{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}); }
     static __device__ __forceinline__ v4f mul(v8 x, v8 w, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, w, c, 0, 0, 0); }
 };

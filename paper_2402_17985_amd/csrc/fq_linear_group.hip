@@ -5,8 +5,8 @@
 // The call is the stream of its weights.  A workgroup goes through tiles of 16 columns; of each its waves have a stretch of the reduction, and their sums
 // meet in LDS.  A wave takes steps of 128 columns, four ahead in registers, across the end of a tile: the next tile's weights travel while sums
 // meet.  X lies in LDS, staged once for all tiles while the first weights are on their way.
-// us (TB/s of weights and scales): one token bf16 4096 x 4096 4.4 (replayed from a graph, one launch 1.5 of them), 11008 x 4096 7.9 (2.9), 22016 x 8192
-// 22 (4.2), 5 tokens fp16 with offsets 22016 x 8192 36 (2.8).  The vector pipe is busy for 47 % of the cycles (61 instructions a step, 32 of them codes to
+// us (TB/s of weights and scales): one token bf16 4096 x 4096 4.2 (replayed from a graph, one launch 1.5 of them), 11008 x 4096 7.8 (2.9), 22016 x 8192
+// 21 (4.4), 5 tokens fp16 with offsets 22016 x 8192 35 (2.8).  The vector pipe is busy for 47 % of the cycles (61 instructions a step, 32 of them codes to
 // numbers); the rest is the waves' own chains, the last of 2.7 rounds of tiles and the way to the first weights.
 // Loads go by lane order: neighbouring lanes read neighbouring pieces, and lanes exchange them afterwards.  In the order that the matrix
 // instruction wants, a load of 64 lanes is worked on lane by lane: the address unit was busy for 57 % of 18 us (16 rows, 11008 x 4096).
@@ -19,7 +19,9 @@
 namespace fq {
 namespace {
 
-constexpr int AHEAD = 4;      // steps in registers, a chunk
+// Steps in registers, a chunk.  Two chunks ahead are slower, as the loop that keeps two sets of registers apart is longer: 22016 x 8192, one row 23 us
+// (21), 8 rows 29 (25), 5 of fp16 with offsets 40 (35).
+constexpr int AHEAD = 4;
 
 // Rows of X in LDS: 16 bytes more than whole steps, so that 16 rows are read from all banks
 constexpr int x_pitch(int K) { return (K + 127) / 128 * 256 + 16; }
@@ -174,8 +176,8 @@ template <int XT, int NW> int launch(GroupProduct a, int group, int wgs, hipStre
 
 }  // namespace
 
-// Two workgroups of eight waves a CU as long as X leaves them the room, one of sixteen up to all of LDS (8 rows, 22016 x 8192: 37 us; one of eight 32 ... 46
-// by the tiles); else, and beyond 16 rows, the tiles of fq_linear_group_tile.hip.
+// Two workgroups of eight waves a CU as long as X leaves them the room, one of sixteen up to nearly all of LDS (8 rows, 22016 x 8192:
+// 25 us; the tiles 39 or more); else, and beyond 16 rows, the tiles of fq_linear_group_tile.hip.
 int launch_linear_group(const void* X, int x_dtype, int M, int K, int ldx, const void* Wq, const void* S, const void* B, int s_dtype, int group, int N,
                         const float* bias, void* Y, int y_dtype, int ldy, hipStream_t stream)
 {

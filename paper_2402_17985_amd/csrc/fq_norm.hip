@@ -17,14 +17,14 @@
 
 #include "fq_internal.h"
 #include "fq_rows.h"
+#include "fq_rules.h"
 
 namespace fq {
 namespace {
 
 enum { ONE_PASS, FIND_SCALE, WITH_SCALE, BOTH };
 constexpr int TABLE = 256;        // multipliers m(n) kept for n < 256
-constexpr int MAX_WGS = 4096;     // and candidates
-constexpr int FEW_ROWS = 2;       // that one workgroup takes alone
+constexpr int ALONE = 2;          // rows that one workgroup takes
 constexpr int KEPT = 4;           // slots away from their channel's place that a thread keeps in registers
 
 // floats of LDS for a row of K, and the zero behind it
@@ -124,7 +124,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     double* part = reinterpret_cast<double*>(lds);                  // 16 waves
     float* best_of = reinterpret_cast<float*>(part + 16);           // 16 waves
     float* few_t = best_of + 16;                                    // t of a few rows
-    float* table = few_t + FEW_ROWS;                                // m(n)
+    float* table = few_t + ALONE;                                // m(n)
     const int tid = threadIdx.x, threads = blockDim.x, K = a.K, G = (K + 7) / 8, Kpad = a.out ? a.Kpad : 0;
     const int zero_at = 8 * G;
     float* row_y = table + TABLE;                                   // the row; behind it a zero
@@ -399,7 +399,7 @@ template <int XT, int RT, int PASS> int launch(const Norm& a, int wgs, hipStream
 {
     const int threads = norm_threads(a.K);
     const bool two = a.K <= 2 * 8 * threads;
-    const int smem = 16 * 8 + (16 + FEW_ROWS + TABLE + row_places(a.K) + (two ? row_places(a.K) : 0)) * 4 + 16 * threads;
+    const int smem = 16 * 8 + (16 + ALONE + TABLE + row_places(a.K) + (two ? row_places(a.K) : 0)) * 4 + 16 * threads;
     const bool ragged = a.K % 8 != 0;
     auto kern = ragged ? (two ? rms_norm_kernel<XT, RT, PASS, 2, true> : rms_norm_kernel<XT, RT, PASS, 4, true>)
                        : (two ? rms_norm_kernel<XT, RT, PASS, 2, false> : rms_norm_kernel<XT, RT, PASS, 4, false>);
@@ -433,7 +433,7 @@ template <int PASS> int launch_types(const Norm& a, int x_dtype, int r_dtype, in
 }  // namespace
 
 // every row's t, and a candidate for the bound from each workgroup
-size_t rms_norm_workspace(int M) { return round_up((size_t)M * 4, 16) + MAX_WGS * 4; }
+size_t rms_norm_workspace(int M) { return round_up((size_t)M * 4, 16) + NORM_WGS * 4; }
 
 int launch_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, const void* R, int r_dtype, int ldr, void* R_out, int ldro,
                           const void* gamma, int g_dtype, float eps, void* Y, int y_dtype, int ldy, const int32_t* src, const int32_t* rep,
@@ -445,13 +445,13 @@ int launch_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, con
     a.M = M; a.K = K; a.Kpad = Kpad; a.g_dtype = g_dtype; a.y_dtype = y_dtype; a.bits = bits; a.eps = eps;
     a.src = src; a.rep = rep; a.absmax = absmax_in; a.out = static_cast<uint8_t*>(Xq_out); a.s_x = s_x_out;
     // 16 waves a CU
-    const int wgs = std::min(M, std::min(MAX_WGS, compute_units() * std::max(1, 1024 / norm_threads(K)))), rt = R ? r_dtype : NONE;
+    const int wgs = std::min(M, std::min(NORM_WGS, compute_units() * std::max(1, 1024 / norm_threads(K)))), rt = R ? r_dtype : NONE;
     if (!Xq_out || absmax_in) return launch_types<ONE_PASS>(a, x_dtype, rt, wgs, stream);
     a.t = static_cast<float*>(workspace);
     a.found = a.t + round_up((size_t)M * 4, 16) / 4;
     a.candidates = wgs;
     // us, one workgroup / two launches: 1 x 4096 10 / 13, 2 x 4096 12.7 / 13, 3 x 4096 15.5 / 13, 2 x 8192 15.7 / 15.3, 1 x 16384 17 / 19.7
-    if (M <= (K <= 4096 ? FEW_ROWS : 1)) return launch_types<BOTH>(a, x_dtype, rt, 1, stream);
+    if (M <= (K <= 4096 ? ALONE : 1)) return launch_types<BOTH>(a, x_dtype, rt, 1, stream);
     if (int rc = launch_types<FIND_SCALE>(a, x_dtype, rt, wgs, stream)) return rc;
     if (R) {        // the second pass reads what the first one stored
         a.X = R_out;

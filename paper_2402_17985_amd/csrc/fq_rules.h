@@ -232,6 +232,9 @@ inline AbsmaxGrid absmax_grid(long long M, long long K, long long ld, int vec, l
 // Tiles of group-scaled weights (256 rows) and of activations (64 rows) are addressed from their first row with 32 bits.
 constexpr int MAX_GROUP_WIDTH = 1 << 24;
 
+// The norm's workgroups, which go through the rows, and the rows whose numbers stay below 2^31 when a workgroup looks for its next one.
+constexpr int NORM_WGS = 4096, MAX_NORM_ROWS = 2147483647 - NORM_WGS;
+
 // Products with group-scaled 4-bit weights: a workgroup of 512 threads for at least 16 columns and 16 rows.
 inline bool group_holds(long long M, long long N) { return launch_holds(((M + 15) / 16) * ((N + 15) / 16), 512); }
 

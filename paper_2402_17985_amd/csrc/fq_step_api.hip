@@ -50,6 +50,7 @@ int fq_rms_norm_quant(const void* X, int x_dtype, int M, int K, int ldx, const v
     if (rc) return rc;
     if (!float_dtype(g_dtype)) return fail(FQ_ERR_DTYPE, "gamma: dtype %d is not F32/F16/BF16", g_dtype);
     if (K > 32768) return fail(FQ_ERR_RANGE, "K = %d: at most 32768", K);
+    if (M > MAX_NORM_ROWS) return fail(FQ_ERR_RANGE, "M = %d: at most %d", M, MAX_NORM_ROWS);
     if (!(eps > 0.0f) || std::isinf(eps)) return fail(FQ_ERR_RANGE, "eps = %g must be positive and finite", (double)eps);
     if (!Y && !Xq_out) return fail(FQ_ERR_NULL, "neither Y nor Xq_out is wanted");
     if (Y && (rc = check_matrix("Y", Y, y_dtype, M, K, ldy))) return rc;

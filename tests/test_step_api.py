@@ -91,3 +91,11 @@ def test_workspace_is_checked_against_the_query():
     need = fq.fq_rms_norm_workspace_bytes(4, 64, 128)
     assert norm(workspace_bytes=need - 1) == WORKSPACE
     assert fq.fq_rms_norm_workspace_bytes(0, 64, 128) == 16      # sizes that the call refuses
+
+
+def test_rows_are_counted_in_32_bits():
+    """A workgroup adds their number, up to 4096, to a row's to find its next one."""
+    for rows in (2**31 - 1, 2**31 - 4096):
+        assert norm(M=rows, absmax_in=P) == RANGE and norm(M=rows, workspace_bytes=1 << 40) == RANGE
+    if not torch.cuda.is_available():
+        assert norm(M=2**31 - 4097, absmax_in=P) == HIP
