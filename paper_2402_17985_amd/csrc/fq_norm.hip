@@ -25,6 +25,8 @@ namespace {
 enum { ONE_PASS, FIND_SCALE, WITH_SCALE, BOTH };
 constexpr int TABLE = 256;        // multipliers m(n) kept for n < 256
 constexpr int ALONE = 2;          // rows that one workgroup takes
+constexpr int ALONE_PLACES = 4;   // of their t in LDS: what follows begins at a multiple of 16 bytes
+static_assert(ALONE <= ALONE_PLACES && (16 + ALONE_PLACES + TABLE) % 4 == 0, "LDS");
 constexpr int KEPT = 4;           // slots away from their channel's place that a thread keeps in registers
 
 // floats of LDS for a row of K, and the zero behind it
@@ -124,7 +126,7 @@ __global__ __launch_bounds__(1024) void rms_norm_kernel(Norm a)
     double* part = reinterpret_cast<double*>(lds);                  // 16 waves
     float* best_of = reinterpret_cast<float*>(part + 16);           // 16 waves
     float* few_t = best_of + 16;                                    // t of a few rows
-    float* table = few_t + ALONE;                                // m(n)
+    float* table = few_t + ALONE_PLACES;                         // m(n)
     const int tid = threadIdx.x, threads = blockDim.x, K = a.K, G = (K + 7) / 8, Kpad = a.out ? a.Kpad : 0;
     const int zero_at = 8 * G;
     float* row_y = table + TABLE;                                   // the row; behind it a zero
@@ -399,7 +401,7 @@ template <int XT, int RT, int PASS> int launch(const Norm& a, int wgs, hipStream
 {
     const int threads = norm_threads(a.K);
     const bool two = a.K <= 2 * 8 * threads;
-    const int smem = 16 * 8 + (16 + ALONE + TABLE + row_places(a.K) + (two ? row_places(a.K) : 0)) * 4 + 16 * threads;
+    const int smem = 16 * 8 + (16 + ALONE_PLACES + TABLE + row_places(a.K) + (two ? row_places(a.K) : 0)) * 4 + 16 * threads;
     const bool ragged = a.K % 8 != 0;
     auto kern = ragged ? (two ? rms_norm_kernel<XT, RT, PASS, 2, true> : rms_norm_kernel<XT, RT, PASS, 4, true>)
                        : (two ? rms_norm_kernel<XT, RT, PASS, 2, false> : rms_norm_kernel<XT, RT, PASS, 4, false>);
