@@ -27,11 +27,11 @@ __device__ __forceinline__ void dma4(const uint8_t* uniform_base, uint32_t lane_
 }
 
 // Bytes of LDS: a wave's codes and scales of a stage; a stage; the whole
-constexpr int own_bytes(int NT, int PER, bool offset) { return NT * 1024 + (NT * PER / 4) * 256 * (offset ? 2 : 1); }
+constexpr int own_bytes(int NT, int PER, bool offset) { return NT * 1024 + (NT * PER + 3) / 4 * 256 * (offset ? 2 : 1); }
 constexpr int stage_bytes(int MT, int NT, int WN, int WK, int PER, bool offset) { return 16 * MT * 256 * WK + WN * WK * own_bytes(NT, PER, offset); }
 constexpr int sums_bytes(int MT, int NT, int WN, int WK) { return WK * 16 * MT * (16 * NT * WN + 4) * 4; }
 
-// GROUP = 32 serves groups of any size: every product of 32 columns takes its scale.
+// GROUP = 32 serves groups of any size: every product of 32 columns takes its scale.  (NT * PER < 4: the copies of scales bring some of the columns behind, too.)
 template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP, bool OFFSET>
 __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupProduct a)
 {
@@ -40,9 +40,9 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
     constexpr int THREADS = 64 * WN * WK, PER = 128 / GROUP, EACH = 4 / PER;
     constexpr bool TURN = GROUP != 128;                          // product j takes columns 32 j .. 32 j + 31, of one group
     constexpr int ROWS = 16 * MT, PITCH = 256 * WK, X_BYTES = ROWS * PITCH, COPIES = X_BYTES / 1024 / (WN * WK);
-    constexpr int SCALES = NT * PER / 4, OWN = own_bytes(NT, PER, OFFSET), STAGE = stage_bytes(MT, NT, WN, WK, PER, OFFSET);
+    constexpr int SCALES = (NT * PER + 3) / 4, OWN = own_bytes(NT, PER, OFFSET), STAGE = stage_bytes(MT, NT, WN, WK, PER, OFFSET);
     constexpr int IN_STAGE = COPIES + NT + SCALES * (OFFSET ? 2 : 1);      // copies of a wave
-    static_assert(X_BYTES % (1024 * WN * WK) == 0 && NT * PER % 4 == 0, "whole copies a wave");
+    static_assert(X_BYTES % (1024 * WN * WK) == 0, "whole copies a wave");
     static_assert((S - 2) * IN_STAGE < 64, "copies are counted in six bits");
     extern __shared__ __align__(16) uint8_t lds[];
     const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, c = lane >> 4;
@@ -214,33 +214,43 @@ template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP = 32> int lau
 
 }  // namespace
 
-// Tiles by how many there are: large ones where they fill the CUs; else the smallest of which each CU gets one at most, as a workgroup's time goes by
-// its stages (1.1 us each, however far ahead copies are issued) more than by what is in them.  us (bf16, groups of 128 or 64), the taken one first:
-//   64 x 256   2048 rows, 11008 x 4096: 229; 64 x 128, waves two by two along both: 331; 64 x 128, waves side by side 351; 128 x 256 260
-//   64 x 128   512 rows, 4096 x 4096: 33; 64 x 256 56.  128 rows, 11008 x 4096: 32; 32 x 64 41
-//   32 x 64    128 rows, 4096 x 4096: 16; 64 x 32 16; 64 x 128 31.  64 rows, 22016 x 8192: 82; 64 x 64 97; 32 x 32 111
-//   32 x 32    64 rows, 4096 x 4096: 11; 32 x 64 15; 32 x 16 15.  48 rows, 4096 x 11008: 26; 48 x 32 30; 32 x 16 31
-//   32 x 16    24 rows, 4096 x 11008: 18; 32 x 32 25.  64 rows, 1024 x 4096: 8; 32 x 32 11
-//   48 x 64    48 rows, 11008 x 4096: 18; 32 x 64 28
-//   16 x 16    16 rows, 4096 x 11008: 13; 16 x 32 17.  16 x 32   16 rows, 22016 x 8192: 40; 16 x 16 56
-// With groups of 32 columns there is a scale to apply after every matrix product, and tiles of 256 columns lose (2048 rows, 11008 x 4096: 345; 256 columns 512).
+// Tiles by how many there are: the smallest of which each CU gets one at most, as a workgroup's time goes by its stages more than by what is in them
+// (32 x 32, 512 or 768 columns a stage: 1.0 or 1.35 us; without the copies of X 15 % less, without those of the scales 4 %).
+// us (bf16, groups of 128 or as given), the taken one first:
+//   16 x 16    16 rows, 4096 x 11008: 11; 16 x 32 15
+//   16 x 32    16 rows, 22016 x 8192: 39; 16 x 16 50.  As for groups of 32 whatever their size: with groups of 128 for themselves 44
+//   32 x 16    24 rows, 4096 x 11008: 16; 32 x 32 19.  64 rows, 1024 x 4096: 6.4; 32 x 32 8.7
+//   32 x 32    64 rows, 4096 x 4096: 9.6; 32 x 64 13.  512 columns a stage with groups of 128, three stages; else 768, two: the last, and the other one, over 4096 x
+//              11008 with groups of 32 24 and 28, 64 22 and 25, 128 20 and 22, but 128 over 4096 x 4096 10.7 and 9.9, 8192 x 8192 (32 rows) 17.7 and 16.5
+//   32 x 64    128 rows, 4096 x 4096: 13; 32 x 128 16
+//   48 x 64    48 rows, 11008 x 4096: 15.5; 32 x 128 16.4.  22016 x 8192: 65; 32 x 128 71
+//   32 x 128   256 rows, 4096 x 4096: 17; 64 x 128 21; 32 x 64 26.  128 rows, 11008 x 4096: 31; 64 x 128 38.  512 rows, 4096 x 4096: 33; 64 x 128 31
+// Groups of 64 and 128 columns have kernels of their own: 64 rows, 4096 x 4096, groups of 128: 9.6; as for groups of 32 12. <int XT, int GROUP> int launch_small(const GroupProduct& a, long long cus, hipStream_t stream)
+{
+    const long long M = a.M, N = a.N;
+    auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
+    if (M <= 16) return tiles(16, 16) <= cus ? launch<XT, 1, 1, 1, 8, 3, GROUP>(a, stream) : launch<XT, 1, 1, 2, 8, 2, 32>(a, stream);
+    if (tiles(32, 16) <= cus) return launch<XT, 2, 1, 1, 8, 2, GROUP>(a, stream);
+    if (tiles(32, 32) <= cus) return GROUP == 128 ? launch<XT, 2, 1, 2, 4, 3, 128>(a, stream) : launch<XT, 2, 1, 2, 6, 2, GROUP>(a, stream);
+    if (tiles(32, 64) <= cus) return launch<XT, 2, 1, 4, 4, 2, GROUP>(a, stream);
+    if (M > 32 && M <= 48) return launch<XT, 3, 1, 4, 4, 2, GROUP>(a, stream);
+    return launch<XT, 2, 2, 4, 4, 2, GROUP>(a, stream);
+}
+// Large tiles where the smaller ones would take turns on the CUs: us, 64 x 256 with two waves along the reduction / with one / 32 x 128:
+// 256 rows, 11008 x 4096 45 / 57 / 47; 1024 rows, 4096 x 4096 46 / 58 / 69; 512 rows, 11008 x 4096 87 / 75 / 91; 2048 rows, 11008 x 4096 255 / 232 / 329.
+// With groups of 32 columns there is a scale to apply after every matrix product, and large tiles of 128 columns are best (2048 rows, 11008 x 4096: 345; 256 columns
+// 512), from more of them on: 64 x 128 / 32 x 128, 256 rows, 11008 x 4096 75 / 68, 384 rows 105 / 112, 512 rows 102 / 133.
 template <int XT> int launch_group_tile(const GroupProduct& product, int group, hipStream_t stream)
 {
     GroupProduct a = product;
     a.group_shift = group == 32 ? 5 : group == 64 ? 6 : 7;
     const long long cus = compute_units(), M = a.M, N = a.N;
-    auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
-    if (M <= 16) return tiles(16, 16) <= cus ? launch<XT, 1, 1, 1, 8, 3>(a, stream) : launch<XT, 1, 1, 2, 8, 2>(a, stream);
-    if (M > 64 && 3 * tiles(64, 128) >= 2 * cus) {
-        const bool many = 3 * tiles(64, 256) >= 2 * cus;
-        if (group == 32) return launch<XT, 4, 2, 4, 1, 2>(a, stream);
-        if (group == 64) return many ? launch<XT, 4, 4, 4, 1, 2, 64>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 64>(a, stream);
-        return many ? launch<XT, 4, 4, 4, 1, 2, 128>(a, stream) : launch<XT, 4, 4, 2, 2, 2, 128>(a, stream);
-    }
-    if (tiles(32, 16) <= cus) return launch<XT, 2, 1, 1, 8, 2>(a, stream);
-    if (tiles(32, 32) <= cus) return launch<XT, 2, 1, 2, 4, 3>(a, stream);
-    if (M > 32 && M <= 48 && tiles(32, 64) > cus) return launch<XT, 3, 1, 4, 4, 2>(a, stream);
-    return launch<XT, 2, 1, 4, 4, 2>(a, stream);
+    const long long large = (M + 63) / 64 * ((N + 127) / 128);
+    if (M <= 48 || 2 * large <= (group == 32 ? 3 : 2) * cus)
+        return group == 32 ? launch_small<XT, 32>(a, cus, stream) : group == 64 ? launch_small<XT, 64>(a, cus, stream) : launch_small<XT, 128>(a, cus, stream);
+    if (group == 32) return launch<XT, 4, 2, 4, 1, 2>(a, stream);
+    if ((M + 63) / 64 * ((N + 255) / 256) <= cus) return group == 64 ? launch<XT, 4, 4, 4, 2, 2, 64>(a, stream) : launch<XT, 4, 4, 4, 2, 2, 128>(a, stream);
+    return group == 64 ? launch<XT, 4, 4, 4, 1, 2, 64>(a, stream) : launch<XT, 4, 4, 4, 1, 2, 128>(a, stream);
 }
 #if FQ_GROUP_TYPE == 1
 template int launch_group_tile<FQ_F16>(const GroupProduct&, int, hipStream_t);

@@ -183,3 +183,12 @@ def test_a_row_does_not_go_by_its_neighbours():
     rows, cols = [i for i in range(70) if i not in (7, 69)], [j for j in range(50) if j != 11]
     assert torch.equal(got[rows][:, cols], want[rows][:, cols])
     assert not torch.isfinite(got[7]).any() and not torch.isfinite(got[69]).any() and not torch.isfinite(got[:, 11]).any()
+
+
+@pytest.mark.parametrize("offsets", [False, True])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(15, 50, 9248), (16, 4130, 5152), (20, 4130, 800), (33, 2070, 1440), (20, 8200, 416), (40, 8200, 544), (20, 16500, 288), (70, 10000, 672),
+                                   (70, 16500, 416), (130, 9000, 1184), (70, 33000, 160)])
+def test_product_tiles(M, N, K, group, offsets):
+    """Numbers of tiles that take each of the kernels' tiles on a device of 256 compute units, both sides of every rule."""
+    product(M, N, K, group, offsets=offsets, seed=M + N + K)
