@@ -225,7 +225,8 @@ template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP = 32> int lau
 //   32 x 64    128 rows, 4096 x 4096: 13; 32 x 128 16
 //   48 x 64    48 rows, 11008 x 4096: 15.5; 32 x 128 16.4.  22016 x 8192: 65; 32 x 128 71
 //   32 x 128   256 rows, 4096 x 4096: 17; 64 x 128 21; 32 x 64 26.  128 rows, 11008 x 4096: 31; 64 x 128 38.  512 rows, 4096 x 4096: 33; 64 x 128 31
-// Groups of 64 and 128 columns have kernels of their own: 64 rows, 4096 x 4096, groups of 128: 9.6; as for groups of 32 12. <int XT, int GROUP> int launch_small(const GroupProduct& a, long long cus, hipStream_t stream)
+// Groups of 64 and 128 columns have kernels of their own: 64 rows, 4096 x 4096, groups of 128: 9.6; as for groups of 32 12.
+template <int XT, int GROUP> int launch_small(const GroupProduct& a, long long cus, hipStream_t stream)
 {
     const long long M = a.M, N = a.N;
     auto tiles = [&](int rows, int cols) { return ((M + rows - 1) / rows) * ((N + cols - 1) / cols); };
