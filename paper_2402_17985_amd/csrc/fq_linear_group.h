@@ -96,25 +96,27 @@ namespace {
 // Eight codes (a word of nibbles, two's complement) as eight 16-bit numbers in the columns' order: a byte's two nibbles into the halves of a register.
 // u = q + 8 is q with its highest bit turned.
 template <int XT> struct GroupMma;
+// q + 24: a nibble in the top four mantissa bits of 16 makes 16 + u.  The multiplication brings a byte's low nibble there in the low half and its high one in the
+// high half; it takes the byte as its operand, so two codes cost two instructions (shifts, masks and a subtraction in fp32: seven).
+template <uint32_t FACTOR, uint32_t MASK, uint32_t BASE> __device__ __forceinline__ v4u surplus_codes(uint32_t w)
+{
+    v4u r;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) r[p] = ((((w >> (8 * p)) & 0xffu) * FACTOR) & MASK) ^ BASE;
+    return r;
+}
 template <> struct GroupMma<FQ_BF16> {
     typedef v8bf v8;
     static constexpr bool SURPLUS = true;      // widen() gives q + 24, exactly; a product with all(true), -24 everywhere, takes the surplus out
-    // A nibble in the top four mantissa bits of 16 makes 16 + u.  The multiplication brings a byte's low nibble to bits 3 .. 6 and its high one to
-    // bits 19 .. 22; it takes the byte as its operand, so two codes cost two instructions (shifts, masks and a subtraction in fp32: seven).
-    static __device__ __forceinline__ v8 widen(uint32_t w)
-    {
-        constexpr uint32_t MASK = 0x00780078u, BASE = 0x41c041c0u;
-        v4u r;
-#pragma unroll
-        for (int p = 0; p < 4; ++p) r[p] = ((((w >> (8 * p)) & 0xffu) * 0x8008u) & MASK) ^ BASE;
-        return __builtin_bit_cast(v8, r);
-    }
+    static __device__ __forceinline__ v8 widen(uint32_t w) { return widen24(w); }
+    static __device__ __forceinline__ v8 widen24(uint32_t w) { return __builtin_bit_cast(v8, surplus_codes<0x8008u, 0x00780078u, 0x41c041c0u>(w)); }
     static __device__ __forceinline__ v8 all(bool less) { const uint32_t v = less ? 0xc1c0c1c0u : 0x3f803f80u; return __builtin_bit_cast(v8, v4u{v, v, v, v}); }
     static __device__ __forceinline__ v4f mul(v8 x, v8 w, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w, c, 0, 0, 0); }
 };
 template <> struct GroupMma<FQ_F16> {
     typedef v8h v8;
-    static constexpr bool SURPLUS = false;     // widen() gives q: there is a packed subtraction
+    static constexpr bool SURPLUS = false;     // widen() gives q: there is a packed subtraction, the third instruction for two codes
+    static __device__ __forceinline__ v8 widen24(uint32_t w) { return __builtin_bit_cast(v8, surplus_codes<0x40040u, 0x03c003c0u, 0x4e004e00u>(w)); }
     // nibbles at bits 0 .. 3 of 1024 and at bits 4 .. 7 of 64 count 1 where they are
     static __device__ __forceinline__ v8 widen(uint32_t w)
     {

@@ -38,6 +38,7 @@ __global__ __launch_bounds__(NW * 64) void linear_group_kernel(GroupProduct a)
     typedef typename M_::v8 v8;
     constexpr int THREADS = NW * 64, SUMS = sums_of(NW);
     constexpr int PER = 128 / GROUP, EACH = 4 / PER;            // groups in a step of 128 columns, products (32 columns) in a group
+    constexpr bool SURPLUS = OFFSET || M_::SURPLUS;             // codes as q + 24, which costs less where the activations' sum is there anyway
     extern __shared__ __align__(16) uint8_t lds[];
     v4f* red = reinterpret_cast<v4f*>(lds);                     // SUMS times [NW][64]
     uint8_t* x_lds = lds + SUMS * NW * 1024;
@@ -93,17 +94,16 @@ __global__ __launch_bounds__(NW * 64) void linear_group_kernel(GroupProduct a)
         if (TURN) transpose_quarters(codes);
 #pragma unroll
         for (int g = 0; g < PER; ++g) {
-            v4f p = {0.0f, 0.0f, 0.0f, 0.0f}, less = p, sum = p;
+            v4f p = {0.0f, 0.0f, 0.0f, 0.0f}, sum = p;
 #pragma unroll
             for (int j = EACH * g; j < EACH * (g + 1); ++j) {
                 const v8 xf = *reinterpret_cast<const v8*>(x_at + 256 * k + 2 * x_next * j);
-                p = M_::mul(xf, M_::widen(codes[j]), p);
-                if (M_::SURPLUS) less = M_::mul(xf, M_::all(true), less);
-                if (OFFSET) sum = M_::mul(xf, M_::all(false), sum);
+                p = M_::mul(xf, SURPLUS ? M_::widen24(codes[j]) : M_::widen(codes[j]), p);
+                if (SURPLUS) sum = M_::mul(xf, M_::all(false), sum);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                acc[e] = __builtin_fmaf(s[g], M_::SURPLUS ? p[e] + less[e] : p[e], acc[e]);
+                acc[e] = __builtin_fmaf(s[g], SURPLUS ? __builtin_fmaf(-24.0f, sum[e], p[e]) : p[e], acc[e]);
                 if (OFFSET) acc[e] = __builtin_fmaf(b[g], sum[e], acc[e]);
             }
         }
