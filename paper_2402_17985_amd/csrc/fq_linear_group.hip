@@ -6,8 +6,8 @@
 // meet in LDS.  A wave takes steps of 128 columns, four ahead in registers, across the end of a tile: the next tile's weights travel while sums
 // meet.  X lies in LDS, staged once for all tiles while the first weights are on their way.
 // us (TB/s of weights and scales): one token bf16 4096 x 4096 4.2 (replayed from a graph, one launch 1.5 of them), 11008 x 4096 7.8 (2.9), 22016 x 8192
-// 21 (4.4), 5 tokens fp16 with offsets 22016 x 8192 35 (2.8).  The vector pipe is busy for 47 % of the cycles (61 instructions a step, 32 of them codes to
-// numbers); the rest is the waves' own chains, the last of 2.7 rounds of tiles and the way to the first weights.
+// 21 (4.4), 5 tokens fp16 with offsets 22016 x 8192 34 (3.0).  The vector pipe is busy for 50 % of the last one's cycles (some 80 instructions a step, 32 of them codes
+// to numbers), the matrix pipe for 16 %; the rest is the waves' own chains, the last of 2.7 (5.4) rounds of tiles and the way to the first weights.
 // Loads go by lane order: neighbouring lanes read neighbouring pieces, and lanes exchange them afterwards.  In the order that the matrix
 // instruction wants, a load of 64 lanes is worked on lane by lane: the address unit was busy for 57 % of 18 us (16 rows, 11008 x 4096).
 #include <algorithm>
