@@ -144,6 +144,9 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
         };
         v8 x[2][4];
         operands(0, x[0]);
+        // Where a CU has several workgroups, one that multiplies goes before one that widens codes, so that they fall out of step: 2048 rows, 11008 x 4096 with
+        // groups of 128 / 64 / 32 224 / 271 / 341 us instead of 237 / 291 / 348 (matrix instructions alone before the others: 235 / 283 / 344).
+        if (WK == 1) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             if (i + 1 < MT) operands(i + 1, x[(i + 1) % 2]);
@@ -170,6 +173,7 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
             }
             if (MT * NT > 8) __builtin_amdgcn_sched_barrier(0);      // large tiles: operands of two blocks of rows are enough in registers
         }
+        if (WK == 1) __builtin_amdgcn_s_setprio(0);
     }
     __syncthreads();
 
