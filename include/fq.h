@@ -400,7 +400,7 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes, at most 2^24 elements); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
  *   Products of activations and codes are exact (BF16, and F16 with offsets: codes may enter as q + 24, whose surplus leaves with the activations' sum); sums, and scales
  *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights; no limit on M.
- *   (So the activations' sum over a group, 32 times their magnitude, must be finite in fp32.)
+ *   (So the activations' sum over a group, 32 times their magnitude, and 32 times a scale must be finite in fp32.)
  *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.
  * ------------------------------------------------------------------------------------------- */
 int fq_group_weights_i4(const void* W, int w_dtype, int N, int K, int ldw, int group, void* Wq_out, void* S_out, void* B_out, int s_dtype,

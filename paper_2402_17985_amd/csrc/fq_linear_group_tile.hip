@@ -134,7 +134,9 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
 #pragma unroll
             for (int g = 0; g < PER; ++g) {
                 s[j][g] = a.value(scales[g]);
+                // An offset takes the surplus out as well, without a product of its own (2048 rows, 11008 x 4096 with groups of 128 245 us instead of 261)
                 b[j][g] = OFFSET ? a.value(scales[SCALES * 64 + g]) : 0.0f;
+                if (OFFSET && M_::SURPLUS) b[j][g] = __builtin_fmaf(-24.0f, s[j][g], b[j][g]);
             }
         }
         const uint8_t* x_at = here + r * PITCH;
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
                 v4f p[NT], less = {0.0f, 0.0f, 0.0f, 0.0f}, sum = less;
 #pragma unroll
                 for (int q = EACH * g; q < EACH * (g + 1); ++q) {
-                    if (M_::SURPLUS) less = M_::mul(xf[q], M_::all(true), less);
+                    if (M_::SURPLUS && !OFFSET) less = M_::mul(xf[q], M_::all(true), less);
                     if (OFFSET) sum = M_::mul(xf[q], M_::all(false), sum);
                 }
 #pragma unroll
