@@ -38,6 +38,7 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
     typedef GroupMma<XT> M_;
     typedef typename M_::v8 v8;
     constexpr int THREADS = 64 * WN * WK, PER = 128 / GROUP, EACH = 4 / PER;
+    constexpr bool SURPLUS = OFFSET || M_::SURPLUS;              // codes as q + 24 (2048 rows, 11008 x 4096, fp16 with offsets: 251 us, as q 261)
     constexpr bool TURN = GROUP != 128;                          // product j takes columns 32 j .. 32 j + 31, of one group
     constexpr int ROWS = 16 * MT, PITCH = 256 * WK, X_BYTES = ROWS * PITCH, COPIES = X_BYTES / 1024 / (WN * WK);
     constexpr int SCALES = (NT * PER + 3) / 4, OWN = own_bytes(NT, PER, OFFSET), STAGE = stage_bytes(MT, NT, WN, WK, PER, OFFSET);
@@ -129,14 +130,14 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
             v4u codes = *reinterpret_cast<const v4u*>(own + j * 1024 + 64 * r + 16 * (c ^ (r >> 2)));
             if (TURN) transpose_quarters(codes);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) wf[j][q] = M_::widen(codes[q]);
+            for (int q = 0; q < 4; ++q) wf[j][q] = SURPLUS ? M_::widen24(codes[q]) : M_::widen(codes[q]);
             const uint32_t* scales = reinterpret_cast<const uint32_t*>(own + NT * 1024) + (16 * j + r) * PER;
 #pragma unroll
             for (int g = 0; g < PER; ++g) {
                 s[j][g] = a.value(scales[g]);
                 // An offset takes the surplus out as well, without a product of its own (2048 rows, 11008 x 4096 with groups of 128 245 us instead of 261)
                 b[j][g] = OFFSET ? a.value(scales[SCALES * 64 + g]) : 0.0f;
-                if (OFFSET && M_::SURPLUS) b[j][g] = __builtin_fmaf(-24.0f, s[j][g], b[j][g]);
+                if (OFFSET) b[j][g] = __builtin_fmaf(-24.0f, s[j][g], b[j][g]);
             }
         }
         const uint8_t* x_at = here + r * PITCH;
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(64 * WN * WK) void linear_group_tile_kernel(GroupPr
                 v4f p[NT], less = {0.0f, 0.0f, 0.0f, 0.0f}, sum = less;
 #pragma unroll
                 for (int q = EACH * g; q < EACH * (g + 1); ++q) {
-                    if (M_::SURPLUS && !OFFSET) less = M_::mul(xf[q], M_::all(true), less);
+                    if (SURPLUS && !OFFSET) less = M_::mul(xf[q], M_::all(true), less);
                     if (OFFSET) sum = M_::mul(xf[q], M_::all(false), sum);
                 }
 #pragma unroll
