@@ -104,21 +104,17 @@ class FqKvCache:
         first, end = self.lengths[b] // self.page_size, -(-grown // self.page_size)
         return [i for i in range(first, min(end, len(self.held[b]))) if self._users[self.held[b][i]] > 1] if grown > self.lengths[b] else []
 
-    def _own(self, b: int, grown: int):
-        """Gives sequence b pages of its own where it is about to write.  Returns the (page, copy) that must be made first: of a page that it goes on
-        filling; one that it starts anew has nothing to copy."""
-        copies = []
-        for i in self._writes(b, grown):
-            old = self.held[b][i]
-            if self._users[old] == 1:         # the others have taken copies meanwhile
-                continue
-            new = self._take()
-            if self.lengths[b] > i * self.page_size:
-                copies.append((old, new))
-            self._drop(old)
-            self.held[b][i] = new
-            self.page_table[b, i] = new
-        return copies
+    def _replaced(self, grown):
+        """(sequence, place in held[b]) of the shared pages for which an append up to `grown` tokens needs pages of the sequence's own: one for each
+        writer, but for the last of a page that all its holders write, which keeps it."""
+        left, places = {}, []               # left: holders of a page that would still share it
+        for b, n in enumerate(grown):
+            for i in self._writes(b, n):
+                page = self.held[b][i]
+                left[page] = left.get(page, self._users[page]) - 1
+                if left[page]:
+                    places.append((b, i))
+        return places
 
     def compact(self) -> int:
         """Moves pages so that those in use are the first ones of the pool, and returns their number.  Sequences keep what they hold."""
@@ -136,26 +132,25 @@ class FqKvCache:
         self._free = list(range(len(self._users) - 1, live - 1, -1))
         return live
 
-    def _copies_wanted(self, grown) -> int:
-        """Pages that an append up to `grown` tokens takes in place of shared ones: one for each writer, but for the last of a page that all its holders write."""
-        writers = {}
-        for b, n in enumerate(grown):
-            for i in self._writes(b, n):
-                page = self.held[b][i]
-                writers[page] = writers.get(page, 0) + 1
-        return sum(min(n, self._users[page] - 1) for page, n in writers.items())
-
     def append(self, Q, K, V, new, Q_out=None, K_out=None) -> None:
         """Append new[b] tokens to every sequence b (0: none): the rows of K, V (and Q) in order.  See fq_kv_append."""
         self._check_counts("new", new, "K", K.shape[0])
         grown = [n + m for n, m in zip(self.lengths, new)]
-        wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held)) + self._copies_wanted(grown)
+        replaced = self._replaced(grown)
+        wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held)) + len(replaced)
         if wanted > len(self._free) or max(grown) > self.max_len:
             raise RuntimeError(f"{wanted} pages wanted, {len(self._free)} free; longest sequence {max(grown)} of {self.max_len}")
-        copies = [pair for b, n in enumerate(grown) for pair in self._own(b, n)]
+        # Copies go before any change of what the sequences hold: where one is refused, no past is lost.  (A page that a sequence starts anew has nothing to copy.)
+        own = [(b, i, self.held[b][i], page) for (b, i), page in zip(replaced, reversed(self._free))]
+        copies = [(old, page) for b, i, old, page in own if self.lengths[b] > i * self.page_size]
+        self._copy([old for old, _ in copies], [page for _, page in copies])
+        for b, i, old, page in own:
+            self._take()
+            self._drop(old)
+            self.held[b][i] = page
+            self.page_table[b, i] = page
         for b, n in enumerate(grown):
             self.reserve(b, n)
-        self._copy([old for old, _ in copies], [new for _, new in copies])
         B.fq_kv_append(Q, K, V, self._i32(self._offsets(new)), self._i32(self.lengths), max(1, max(new)), self.k_cache, self.v_cache, self.k_scale,
                        self.v_scale, self.page_table, rope_cos=self.rope_cos, rope_sin=self.rope_sin, interleaved=self.interleaved,
                        Q_out=Q_out, K_out=K_out)
