@@ -31,6 +31,7 @@ class FqKvCache:
         self.lengths = [0] * batch
         self._free = list(range(pages - 1, -1, -1))
         self._users = [0] * pages                   # sequences that hold a page
+        self._shared = 0                            # pages that several hold
 
     def _i32(self, values):
         return self.torch.tensor(values, dtype=self.torch.int32, device=self.device)
@@ -68,6 +69,8 @@ class FqKvCache:
         self._users[page] -= 1
         if self._users[page] == 0:
             self._free.append(page)
+        elif self._users[page] == 1:
+            self._shared -= 1
 
     def release(self, b: int) -> None:
         """Sequence b ends: pages that no other sequence shares are free again."""
@@ -88,6 +91,7 @@ class FqKvCache:
         for c in into:
             for page in pages:
                 self._users[page] += 1
+                self._shared += self._users[page] == 2
             self.held[c], self.lengths[c] = list(pages), self.lengths[b]
         if pages and into:
             self.page_table[self._i64(into), :used] = self._i32(pages)
@@ -102,14 +106,14 @@ class FqKvCache:
     def _writes(self, b: int, grown: int):
         """Places in held[b] of the shared pages that appending up to `grown` tokens writes to: whose past must stay with the others."""
         first, end = self.lengths[b] // self.page_size, -(-grown // self.page_size)
-        return [i for i in range(first, min(end, len(self.held[b]))) if self._users[self.held[b][i]] > 1] if grown > self.lengths[b] else []
+        return [i for i in range(first, min(end, len(self.held[b]))) if self._users[self.held[b][i]] > 1]
 
     def _replaced(self, grown):
         """(sequence, place in held[b]) of the shared pages for which an append up to `grown` tokens needs pages of the sequence's own: one for each
         writer, but for the last of a page that all its holders write, which keeps it."""
         left, places = {}, []               # left: holders of a page that would still share it
         for b, n in enumerate(grown):
-            for i in self._writes(b, n):
+            for i in self._writes(b, n) if n > self.lengths[b] else ():
                 page = self.held[b][i]
                 left[page] = left.get(page, self._users[page]) - 1
                 if left[page]:
@@ -136,21 +140,24 @@ class FqKvCache:
         """Append new[b] tokens to every sequence b (0: none): the rows of K, V (and Q) in order.  See fq_kv_append."""
         self._check_counts("new", new, "K", K.shape[0])
         grown = [n + m for n, m in zip(self.lengths, new)]
-        replaced = self._replaced(grown)
-        wanted = sum(max(0, -(-n // self.page_size) - len(h)) for n, h in zip(grown, self.held)) + len(replaced)
-        if wanted > len(self._free) or max(grown) > self.max_len:
-            raise RuntimeError(f"{wanted} pages wanted, {len(self._free)} free; longest sequence {max(grown)} of {self.max_len}")
+        replaced = self._replaced(grown) if self._shared else []
+        places = replaced + [(b, i) for b, (n, h) in enumerate(zip(grown, self.held)) for i in range(len(h), -(-n // self.page_size))]
+        wanted, free = len(places), len(self._free)
+        if wanted > free or max(grown) > self.max_len:
+            raise RuntimeError(f"{wanted} pages wanted, {free} free; longest sequence {max(grown)} of {self.max_len}")
+        fresh = self._free[free - wanted:][::-1]
         # Copies go before any change of what the sequences hold: where one is refused, no past is lost.  (A page that a sequence starts anew has nothing to copy.)
-        own = [(b, i, self.held[b][i], page) for (b, i), page in zip(replaced, reversed(self._free))]
-        copies = [(old, page) for b, i, old, page in own if self.lengths[b] > i * self.page_size]
+        copies = [(self.held[b][i], page) for (b, i), page in zip(replaced, fresh) if self.lengths[b] > i * self.page_size]
         self._copy([old for old, _ in copies], [page for _, page in copies])
-        for b, i, old, page in own:
-            self._take()
-            self._drop(old)
-            self.held[b][i] = page
-            self.page_table[b, i] = page
-        for b, n in enumerate(grown):
-            self.reserve(b, n)
+        del self._free[free - wanted:]
+        for (b, i), page in zip(places, fresh):
+            self._users[page] = 1
+            if i < len(self.held[b]):
+                self._drop(self.held[b][i])
+            self.held[b][i:i + 1] = [page]
+        if places:                              # one write to the device for all sequences
+            at, pages = self._i32([[b * self.page_table.shape[1] + i for b, i in places], fresh])
+            self.page_table.view(-1)[at] = pages
         B.fq_kv_append(Q, K, V, self._i32(self._offsets(new)), self._i32(self.lengths), max(1, max(new)), self.k_cache, self.v_cache, self.k_scale,
                        self.v_scale, self.page_table, rope_cos=self.rope_cos, rope_sin=self.rope_sin, interleaved=self.interleaved,
                        Q_out=Q_out, K_out=K_out)
