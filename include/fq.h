@@ -399,9 +399,10 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  * fq_linear_group_i4 — Y[i,n] = round_to_y_dtype(sum_k X[i,k] * w[n,k] + bias[n]).
  *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes, at most 2^24 elements); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
  *   Products of activations and codes are exact (BF16, and F16 with offsets: codes may enter as q + 24, whose surplus leaves with the activations' sum); sums, and scales
- *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights; no limit on M.
+ *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights.
  *   (So the activations' sum over a group, 32 times their magnitude, and 32 times a scale must be finite in fp32.)
- *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.
+ *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.  M and N are at most 2^31 - 257 each, and calls whose tiles
+ *   are more than one launch holds are refused: none of fewer than 2^24 tiles of 64 x 128 outputs, or, of up to 48 rows, of fewer than 2^27 columns.
  * ------------------------------------------------------------------------------------------- */
 int fq_group_weights_i4(const void* W, int w_dtype, int N, int K, int ldw, int group, void* Wq_out, void* S_out, void* B_out, int s_dtype,
                         void* stream);

@@ -9,6 +9,7 @@
 
 #include "fq_gemm_common.h"
 #include "fq_linear_group.h"
+#include "fq_rules.h"
 
 namespace fq {
 namespace {
@@ -205,10 +206,12 @@ template <int XT, int MT, int NT, int WN, int WK, int S, int GROUP, bool OFFSET>
     constexpr int SMEM = std::max(S * stage_bytes(MT, NT, WN, WK, 128 / GROUP, OFFSET), sums_bytes(MT, NT, WN, WK));
     static_assert(SMEM <= 160 * 1024, "LDS of a CU");
     auto kern = linear_group_tile_kernel<XT, MT, NT, WN, WK, S, GROUP, OFFSET>;
+    const long long tiles_n = ((long long)a.N + 16 * NT * WN - 1) / (16 * NT * WN), tiles = tiles_n * (((long long)a.M + 16 * MT - 1) / (16 * MT));
+    if (!launch_holds(tiles, 64 * WN * WK)) return fail(FQ_ERR_RANGE, "%d x %d outputs are more than one launch holds", a.M, a.N);
+    a.tiles_n = (int)tiles_n;
+    a.tiles = (int)tiles;
     static std::atomic<unsigned long long> attr_set;
     if (int rc = set_lds_limit(reinterpret_cast<const void*>(kern), SMEM, attr_set)) return rc;
-    a.tiles_n = (a.N + 16 * NT * WN - 1) / (16 * NT * WN);
-    a.tiles = a.tiles_n * ((a.M + 16 * MT - 1) / (16 * MT));
     kern<<<(unsigned)a.tiles, 64 * WN * WK, SMEM, stream>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(FQ_ERR_HIP, "group-scaled layer launch failed: %s", hipGetErrorString(e));

@@ -235,7 +235,7 @@ constexpr int MAX_GROUP_WIDTH = 1 << 24;
 // The norm's workgroups, which go through the rows, and the rows whose numbers stay below 2^31 when a workgroup looks for its next one.
 constexpr int NORM_WGS = 4096, MAX_NORM_ROWS = 2147483647 - NORM_WGS;
 
-// Products with group-scaled 4-bit weights: a workgroup of 512 threads for at least 16 columns and 16 rows.
-inline bool group_holds(long long M, long long N) { return launch_holds(((M + 15) / 16) * ((N + 15) / 16), 512); }
+// Products with group-scaled 4-bit weights: rows and columns that still count in 31 bits when filled up to whole tiles (64 x 256 at most).
+constexpr int MAX_GROUP_SIDE = 2147483647 - 256;
 
 }  // namespace fq

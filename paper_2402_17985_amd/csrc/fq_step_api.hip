@@ -105,7 +105,7 @@ int fq_linear_group_i4(const void* X, int x_dtype, int M, int K, int ldx, const 
     if (ldx > MAX_GROUP_WIDTH) return fail(FQ_ERR_RANGE, "X: row stride of %d elements, at most 2^24", ldx);
     if (N <= 0) return fail(FQ_ERR_SHAPE, "N = %d must be positive", N);
     if (ldy < N) return fail(FQ_ERR_SHAPE, "ldy = %d < N = %d", ldy, N);
-    if (!group_holds(M, N)) return fail(FQ_ERR_RANGE, "%d x %d outputs are more than one launch holds", M, N);
+    if (M > MAX_GROUP_SIDE || N > MAX_GROUP_SIDE) return fail(FQ_ERR_RANGE, "%d x %d outputs: at most %d each way", M, N, MAX_GROUP_SIDE);
     return launch_linear_group(X, x_dtype, M, K, ldx, Wq, S, B, s_dtype, group, N, bias, Y, y_dtype, ldy, static_cast<hipStream_t>(stream));
 }
 
