@@ -73,10 +73,10 @@ def weights_of(q, s, b, group):
     return wide(s) * q + (0.0 if b is None else wide(b))
 
 
-def linear_group(x, q, s, b, group, bias=None):
-    """float64: x times the weights' transpose, plus bias; and the sum of the absolute values of what is added up, codes as q + 24."""
+def linear_group(x, q, s, b, group, bias=None, surplus=24):
+    """float64: x times the weights' transpose, plus bias; and the sum of the absolute values of what is added up, codes as q + surplus."""
     y = x.astype(np.float64) @ weights_of(q, s, b, group).T
-    size = np.abs(x.astype(np.float64)) @ weights_of(np.abs(q.astype(np.int16)) + 48, np.abs(s), None if b is None else np.abs(b), group).T
+    size = np.abs(x.astype(np.float64)) @ weights_of(np.abs(q.astype(np.int16)) + 2 * surplus, np.abs(s), None if b is None else np.abs(b), group).T
     return (y, size) if bias is None else (y + bias.astype(np.float64), size + np.abs(bias))
 
 
