@@ -678,6 +678,8 @@ def fq_rms_norm_quant(X, gamma, eps: float, R=None, R_out=None, Y=None, src_idx=
             raise ValueError(f"Xq_out must be contiguous bytes for {M} rows of {Kpad} slots on the current device, cuda:{here}")
         xq, s_x = Xq_out.data_ptr(), _array(s_x_out, "s_x_out", here, torch.float32, s_x_out.shape)
         if absmax_in is not None:
+            if absmax_in.numel() == 0:
+                raise ValueError("absmax_in holds no value")
             bound = _array(absmax_in, "absmax_in", here, torch.float32, absmax_in.shape)
     if workspace is not None:
         if workspace.get_device() != here or not workspace.is_contiguous():
