@@ -395,11 +395,12 @@ size_t fq_rms_norm_workspace_bytes(int M, int K, int Kpad);
  *                       with offsets, lo and hi being its least and largest element:  s = fl32(fl32(hi - lo) / 15);
  *   s is rounded to s_dtype, at most that type's largest finite value, and 0 where below 2^-126;  b = fl32(lo + fl32(8 s)), rounded
  *   likewise (between -largest and largest);  q = clamp(rne(fl32(fl32(w - b) * fl32(1 / s))), -8, 7), 0 for s = 0  (b = 0 without offsets).
+ *   Rows filled up to whole groups hold fewer than 2^35 weights (else FQ_ERR_RANGE).
  *
  * fq_linear_group_i4 — Y[i,n] = round_to_y_dtype(sum_k X[i,k] * w[n,k] + bias[n]).
  *   X [M, K] F16 / BF16, row stride ldx (a multiple of 16 bytes, at most 2^24 elements); Y [M, N] F32 / F16 / BF16, row stride ldy >= N; bias fp32 [N] or NULL.
- *   Products of activations and codes are exact (BF16, and F16 with offsets: codes may enter as q + 24, whose surplus leaves with the activations' sum); sums, and scales
- *   times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights.
+ *   Products of activations and codes are exact (BF16, and F16 with offsets: codes may enter as q + 24, whose surplus leaves with the activations' sum, and whose
+ *   roundings go by sum |X| (|q| + 48) S, not by sum |X q S|); sums, and scales times sums, accumulate in fp32; nothing else is rounded before Y.  One token or a few: the stream of the weights.
  *   (So the activations' sum over a group, 32 times their magnitude, and 32 times a scale must be finite in fp32.)
  *   Y must not overlap X.  No workspace.  M * ldx, N * K / 2 and M * ldy may exceed 2^32.  M and N are at most 2^31 - 257 each, and calls whose tiles
  *   are more than one launch holds are refused: none of fewer than 2^24 tiles of 64 x 128 outputs, or, of up to 48 rows, of fewer than 2^27 columns.

@@ -1,8 +1,8 @@
 // fq_rms_norm_quant: residual addition, root-mean-square norm, and the flattened, per-tensor quantized activation.
 //
 // arXiv 2402.17985 Sec. 4.1 Eq. 3 and Sec. 2.1 Eq. 1 (flatten and quantize), applied to y = fl32(fl32(h t) gamma), t = 1 / rms(h).
-// A workgroup takes a row at a time, a thread 16 consecutive channels of it, which stay in registers from the load to the
-// codes; sums of squares are formed in float64, so that codes do not go by the order of a sum.  Workgroups stay for many
+// A workgroup takes a row at a time, a thread two pieces (four of rows beyond 16384 channels) of eight channels of it, as many pieces apart as there are
+// threads, which stay in registers from the load to the codes; sums of squares are formed in float64, so that codes do not go by the order of a sum.  Workgroups stay for many
 // rows: gamma, the map and its multipliers are read once, and the next row is on its way while this one is reduced.
 // Slots that do not lie at their channel's own place (copies, padding, other maps) are worked on one by one, neighbouring threads neighbouring slots, from
 // the row in LDS; their codes meet there by sixteens.
@@ -10,8 +10,11 @@
 // second one forms y again and quantizes it.  One workgroup does both for a row or two.
 // Bound by bytes: bf16 with a residual, static, 8192 x 4096 55 us (4.4 TB/s read and written), 8192 x 8192 102 (4.8), fp32 8192 x 4096 92 (4.8): the rate of
 // a copy.  Dynamic 8192 x 4096: 45 and 32 us in the two kernels, 4.4 and 3.3 TB/s.  4099 x 5003 with an fp32 residual, bf16 out: 98 (2.9 TB/s).
+// Nibbles, static and dynamic 8192 x 4096: 51 and 72 us.  E3M2 storage packs codes by sixteens, which no thread has: every slot goes one by one through LDS,
+// 105 and 181 us, one row of 4096 20, 48 x 5120 static 11.
 // One row of 4096, dynamic: 10 us, 48 x 5120 static 7: latency (the map, the row, two or three reductions over the workgroup).
-// With 16 channels in a row to a thread, two loads of 32-byte strides, the address unit worked lane by lane: 8192 x 4096 94 us instead of 72.
+// Sixteen consecutive channels to a thread, two loads of 32-byte strides, kept the address unit busy lane by lane (dynamic 8192 x 4096, both kernels: 94 us, against 72
+// with pieces of eight at that time).
 #include <algorithm>
 #include <atomic>
 
